@@ -229,7 +229,6 @@ def prepare(case, seed):
     if kind in ("score", "loss"):
         T, V = case["T"], case["V"]
         st["desc"] = lobra.make_logprob_desc(case["dtype"], T, V, top_k=case.get("top_k", 0))
-        st["ws"] = empty(max(lobra.lobra_token_logprob_workspace_bytes(st["desc"]), 16), dtype=torch.uint8)
         st.update(logp=empty(T), lse=empty(T), ent=empty(T) if kind == "score" or case["entropy"] else None)
         if kind == "score":
             k = case["top_k"]
@@ -280,13 +279,12 @@ def run(st):
 def _own_logprob(st):
     from paper_2509_01193_amd import binding as lobra
     if st["case"]["kind"] == "score":
-        lobra.lobra_token_logprob_fwd(st["desc"], st["logits"], st["target"], st["logp"], st["lse"], st["ent"], st["top_logp"], st["top_id"],
-                                      st["ws"])
+        lobra.lobra_token_logprob_fwd(st["desc"], st["logits"], st["target"], st["logp"], st["lse"], st["ent"], st["top_logp"], st["top_id"])
         out = dict(logp=st["logp"], lse=st["lse"], entropy=st["ent"])
         if st["case"]["top_k"]:
             out.update(top_logp=st["top_logp"], top_id=st["top_id"])
         return out
-    lobra.lobra_token_logprob_fwd(st["desc"], st["logits"], st["target"], st["logp"], st["lse"], st["ent"], ws=st["ws"])
+    lobra.lobra_token_logprob_fwd(st["desc"], st["logits"], st["target"], st["logp"], st["lse"], st["ent"])
     lobra.lobra_token_logprob_bwd(st["desc"], st["logits"], st["target"], st["lse"], st["ent"], st["dlogp"], st["dentropy"], st["dlogits"])
     out = dict(logp=st["logp"], lse=st["lse"], dlogits=st["dlogits"])
     if st["ent"] is not None:
