@@ -234,7 +234,7 @@ def prepare(case, seed):
             k = case["top_k"]
             st.update(top_logp=empty(T, k) if k else None, top_id=empty(T, k, dtype=torch.int32) if k else None)
         else:
-            st["dlogits"] = empty(T, V, dtype=dt)
+            st.update(rest=empty(T), dlogits=empty(T, V, dtype=dt))
     elif kind == "clip":
         st["outs"] = [torch.empty_like(g) if case["out"] else None for g in st["grads"]]
         st["set"] = lobra.GradSet([(g, o, st["rank_off"]) for g, o in zip(st["grads"], st["outs"])], case["tasks"])
@@ -279,13 +279,15 @@ def run(st):
 def _own_logprob(st):
     from paper_2509_01193_amd import binding as lobra
     if st["case"]["kind"] == "score":
-        lobra.lobra_token_logprob_fwd(st["desc"], st["logits"], st["target"], st["logp"], st["lse"], st["ent"], st["top_logp"], st["top_id"])
+        lobra.lobra_token_logprob_fwd(st["desc"], st["logits"], st["target"], st["logp"], st["lse"], None, st["ent"], st["top_logp"],
+                                      st["top_id"])
         out = dict(logp=st["logp"], lse=st["lse"], entropy=st["ent"])
         if st["case"]["top_k"]:
             out.update(top_logp=st["top_logp"], top_id=st["top_id"])
         return out
-    lobra.lobra_token_logprob_fwd(st["desc"], st["logits"], st["target"], st["logp"], st["lse"], st["ent"])
-    lobra.lobra_token_logprob_bwd(st["desc"], st["logits"], st["target"], st["lse"], st["ent"], st["dlogp"], st["dentropy"], st["dlogits"])
+    lobra.lobra_token_logprob_fwd(st["desc"], st["logits"], st["target"], st["logp"], st["lse"], st["rest"], st["ent"])
+    lobra.lobra_token_logprob_bwd(st["desc"], st["logits"], st["target"], st["lse"], st["rest"], st["ent"], st["dlogp"], st["dentropy"],
+                                  st["dlogits"])
     out = dict(logp=st["logp"], lse=st["lse"], dlogits=st["dlogits"])
     if st["ent"] is not None:
         out["entropy"] = st["ent"]
