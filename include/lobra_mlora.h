@@ -70,7 +70,7 @@ typedef enum {
     LOBRA_ERR_WORKSPACE = -7, /* workspace NULL or too small: lobra_mlora_workspace_bytes / _plan_sizes say what is enough */
     LOBRA_ERR_ALIGN = -8,     /* a pointer not 16-byte aligned, or bf16 d_in/d_out not a multiple of 8 */
     LOBRA_ERR_HIP = -9,       /* a HIP runtime call failed (no device, launch error, ...) */
-    LOBRA_ERR_PLAN = -10,     /* plan is NULL, host-only, or was built for another device */
+    LOBRA_ERR_PLAN = -10,     /* plan (or gradient set) is NULL, host-only, or was built for another device */
     LOBRA_ERR_NOMEM = -11     /* host or device allocation for the plan failed */
 } lobra_status;
 
@@ -309,6 +309,132 @@ LOBRA_API lobra_status lobra_mlora_adam_step(const lobra_mlora_plan *plan, const
                                    float *master_B, float *m_A, float *v_A, float *m_B, float *v_B,
                                    void *A, void *B, void *hip_stream);
 
+/* ---- the rest of a joint fine-tuning step around the LoRA linears (section 2.1: the layer's place in a replica's forward and backward
+ * pass; section 5.1: Adam) ------------------------------------------------------------------------------------------------
+ *
+ * Gated feed-forward block: gate and up projection of an MLP with their adapters, activation and product, of a plan with
+ * n_proj = 2 (projection 0 = gate, 1 = up; f = d_out / 2):
+ *     [g | u] = the layer's y;   h = a(g) u                        forward
+ *     dg = dh u a'(g),  du = dh a(g);  dx, dA, dB = the layer's gradients of dy = [dg | du]
+ * a = LOBRA_ACT_SILU: g / (1 + exp(-g)); LOBRA_ACT_GELU_TANH: g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2.
+ *   gu    : device [T, 2 f], element type of the plan: [g | u], each rounded once, which backward starts from; NULL (serving): not kept
+ *   h     : device [T, f], overwritten; from the fp32 projections where the product's kernel activates them itself, else from [g | u] as
+ *           rounded to the element type
+ *   ws    : lobra_mlora_gated_workspace_bytes (save_gu: whether gu will be given) says what is enough (LOBRA_ERR_WORKSPACE
+ *           below that); with h_save it is as in lobra_mlora_plan_fwd
+ *   dh    : device [T, f];  dgu : device [T, 2 f], overwritten with [dg | du], may be gu itself
+ * The other arguments, and ws of the backward call, are those of lobra_mlora_plan_fwd / _bwd.  LOBRA_ERR_SHAPE for a plan with
+ * another n_proj or an unknown activation. */
+typedef enum { LOBRA_ACT_SILU = 0, LOBRA_ACT_GELU_TANH = 1 } lobra_activation;
+LOBRA_API lobra_status lobra_mlora_gated_workspace_bytes(const lobra_mlora_plan *plan, int32_t save_gu, size_t *fwd_bytes);
+LOBRA_API lobra_status lobra_mlora_gated_fwd(const lobra_mlora_plan *plan, int32_t act, const void *x, const void *W,
+                                   const void *A, const void *B, const float *s, void *gu, void *h,
+                                   void *h_save, void *ws, size_t ws_bytes, void *hip_stream);
+LOBRA_API lobra_status lobra_mlora_gated_bwd(const lobra_mlora_plan *plan, int32_t act, const void *x, const void *W,
+                                   const void *A, const void *B, const float *s, const void *gu, const void *dh,
+                                   const void *h_saved, void *dgu, void *dx, float *dA, float *dB, uint32_t flags,
+                                   void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Norms after one residual block and before the next, with the block's gate and residual scale, in one pass.  For a token i of
+ * task t, with rms(v) = sqrt(mean(v^2) + eps) over the d = d_in channels of the plan (any plan of the batch whose layer reads x):
+ *     r'_i = r_i + alpha gate_t w_post (b_i / rms(b_i))        x_i = w_pre (r'_i / rms(r'_i))
+ * b is the block's output, r the residual before it.  r' is rounded to the plan's element type first and then normed, in backward
+ * as in forward.  A token without a task has the gate 1.
+ *   r, b, r_out, x  : device [T, d];  w_post, w_pre : device [d];  gate : device [n_tasks, d]; all of the plan's element type
+ *   b = NULL        : no block before (r' = r; r_out is not written, and rstd_post, w_post and gate are ignored)
+ *   w_post = NULL   : the block's output is not normed (r' = r + alpha gate_t b; no rstd_post)
+ *   gate = NULL     : 1 for every token
+ *   w_pre = NULL    : no norm behind (neither x nor rstd_pre is written)
+ *   r_out           : may be r
+ *   rstd_post, rstd_pre : device fp32 [T], 1 / rms(b_i) and 1 / rms(r'_i) for backward; NULL: not kept
+ * Backward, from dr_out and dx, the gradients of r' (as the residual goes on; NULL: none) and of x:
+ *   r_out               : r' (with b = NULL: r)
+ *   dr                  : device [T, d], the gradient of r', which is that of r; may be dr_out
+ *   db                  : device [T, d], the gradient of b; may be dx
+ *   dgate, dw_post, dw_pre : device fp32 [n_tasks, d], [d], [d], overwritten, or added to with LOBRA_FLAG_ACCUMULATE_GRADS; NULL: not
+ *                         wanted.  (rows of a task without tokens: 0, or left alone)
+ *   ws                  : lobra_mlora_block_norm_workspace_bytes; may be NULL when none of the three is wanted
+ * Sums over channels and tokens are held in fp32, in a fixed order: bit-identical from run to run.  LOBRA_ERR_SHAPE for d above
+ * LOBRA_MAX_NORM_WIDTH; LOBRA_ERR_NULL where the gradient of a gain or gate that is not there is asked for. */
+enum { LOBRA_MAX_NORM_WIDTH = 16384 };
+typedef struct {
+    float eps, alpha;        /* eps >= 0, both finite */
+} lobra_block_norm_config;
+LOBRA_API lobra_status lobra_mlora_block_norm_workspace_bytes(const lobra_mlora_plan *plan, size_t *bwd_bytes);
+LOBRA_API lobra_status lobra_mlora_block_norm_fwd(const lobra_mlora_plan *plan, const lobra_block_norm_config *cfg, const void *r,
+                                        const void *b, const void *w_post, const void *gate, const void *w_pre, void *r_out,
+                                        void *x, float *rstd_post, float *rstd_pre, void *hip_stream);
+LOBRA_API lobra_status lobra_mlora_block_norm_bwd(const lobra_mlora_plan *plan, const lobra_block_norm_config *cfg, const void *r_out,
+                                        const void *b, const void *w_post, const void *gate, const void *w_pre,
+                                        const float *rstd_post, const float *rstd_pre, const void *dr_out, const void *dx,
+                                        void *dr, void *db, float *dgate, float *dw_post, float *dw_pre, uint32_t flags,
+                                        void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Log probabilities of given tokens under rows of logits, with entropy and the likeliest alternatives, and the gradient: the loss of a
+ * training step, and what a serving interface reports.  Per row i with logits z (p = softmax(z), in fp32):
+ *     lse = ln sum_j exp(z_j)    logp = z_target - lse    entropy = - sum_j p_j ln p_j
+ *     dz_j = dlogp (1[j = target] - p_j) - dentropy p_j (ln p_j + entropy)
+ * A target outside [0, V) (a prompt or pad token) is none: logp is 0, and dlogp of that row is ignored.  Logits of -inf (barred tokens)
+ * have p = 0 and gradient 0.  A row of nothing else: lse = -inf, logp = -inf, entropy = 0, gradient 0.  A row with NaN or +inf:
+ * lse, logp and entropy are NaN.
+ *   logits              : device, row i at logits + i ld elements, 16-byte aligned (ld need not keep the rows aligned)
+ *   target              : device int32 [T], or NULL: no row has one
+ *   logp, lse, entropy  : device fp32 [T], each may be NULL
+ *   lse_rest            : device fp32 [T] or NULL: what lse loses in its rounding to fp32.  With it backward's p is as exact for logits
+ *                         far from 0 as near it (rows of the type's lowest value are uniform ones); without, p is off by an ulp of lse
+ *   top_logp, top_id    : device fp32 / int32 [T, top_k]: the top_k largest logits by value, the lowest index first among equals, as log
+ *                         probabilities; a place for which no logit is left (top_k > V, NaN) holds -1 and -inf.  Either may be NULL
+ *   lse, lse_rest, entropy : in backward what forward wrote (lse_rest may be NULL; entropy only with dentropy)
+ *   dlogp, dentropy     : device fp32 [T], either may be NULL (0).  A row in which both are 0 gets a gradient of 0, whatever its logits
+ *   dlogits             : device, row pitch ld, overwritten in columns 0 .. V - 1; may be logits itself */
+enum { LOBRA_MAX_TOP = 32, LOBRA_MAX_VOCAB = 1 << 24 };
+typedef struct {
+    int32_t dtype;           /* lobra_dtype of logits and dlogits */
+    int32_t V;               /* 1 .. LOBRA_MAX_VOCAB */
+    int64_t T;               /* rows, 0 <= T < 2^31 */
+    int64_t ld;              /* row pitch in elements, >= V (0: V), T ld < 2^60 */
+    int32_t top_k;           /* 0 .. LOBRA_MAX_TOP */
+} lobra_logprob_desc;
+LOBRA_API lobra_status lobra_token_logprob_fwd(const lobra_logprob_desc *desc, const void *logits, const int32_t *target,
+                                     float *logp, float *lse, float *lse_rest, float *entropy, float *top_logp, int32_t *top_id,
+                                     void *hip_stream);
+LOBRA_API lobra_status lobra_token_logprob_bwd(const lobra_logprob_desc *desc, const void *logits, const int32_t *target,
+                                     const float *lse, const float *lse_rest, const float *entropy, const float *dlogp,
+                                     const float *dentropy, void *dlogits, void *hip_stream);
+
+/* Norms of the tasks' gradients over many tensors, and clipping.  The set lists the gradients of all layers (dA and dB of each);
+ * every tensor says with the rank_off of its layer which of its rows belong to which task.  Per task t
+ *     norm_t = |grad_scale_t| sqrt(sum over all tensors and rows of t of g^2)
+ *     clip_scale_t = grad_scale_t min(1, max_norm_t / norm_t)
+ * which is what lobra_mlora_adam_step takes as its grad_scale, so that clipping costs no pass of its own.  A norm that is not finite
+ * stops its task alone: clip_scale_t = 0 and step_out_t = 0, at which Adam leaves the task's rows as they are (else step_out_t = step_t).
+ * Squares are summed in fp64: no gradient that fp32 holds overflows or vanishes, and the order is fixed.
+ *   max_norm    : device fp32 [n_tasks]; NULL, or a value that is negative or NaN: no limit
+ *   grad_scale  : device fp32 [n_tasks] or NULL (1);  step, step_out : device int32 [n_tasks], step_out may be step; both or neither
+ *   norm, clip_scale : device fp32 [n_tasks], either may be NULL.  clip_scale may be grad_scale
+ *   flags       : LOBRA_FLAG_JOINT_NORM: one norm over all tasks, which is then every task's norm_t
+ *   tensors with `out`: receive clip_scale_t g (0 where clip_scale_t = 0); out may be grad
+ *   ws          : lobra_grad_set_workspace_bytes
+ * A set is made like a plan: _create allocates a device buffer and blocks; _init places *bytes of lobra_grad_set_device_bytes in
+ * memory of the caller by an asynchronous copy.  It holds the tensors' addresses, not the tensors. */
+enum { LOBRA_FLAG_JOINT_NORM = 4 };
+typedef struct {
+    const float *grad;       /* device [R, D], 16-byte aligned */
+    float *out;              /* device [R, D], 16-byte aligned, or NULL */
+    int32_t D;               /* 1 .. LOBRA_MAX_WIDTH */
+    const int32_t *rank_off; /* HOST [n_tasks + 1], rank_off[0] = 0, non-decreasing: rows of task t; R = rank_off[n_tasks], R D < 2^40 */
+} lobra_grad_tensor;
+typedef struct lobra_grad_set lobra_grad_set;
+LOBRA_API lobra_status lobra_grad_set_device_bytes(const lobra_grad_tensor *tensors, int32_t n_tensors, int32_t n_tasks, size_t *bytes);
+LOBRA_API lobra_status lobra_grad_set_create(const lobra_grad_tensor *tensors, int32_t n_tensors, int32_t n_tasks, lobra_grad_set **out);
+LOBRA_API lobra_status lobra_grad_set_init(const lobra_grad_tensor *tensors, int32_t n_tensors, int32_t n_tasks, void *device_mem,
+                                 size_t device_bytes, void *hip_stream, lobra_grad_set **out);
+LOBRA_API lobra_status lobra_grad_set_destroy(lobra_grad_set *set);
+LOBRA_API lobra_status lobra_grad_set_workspace_bytes(const lobra_grad_set *set, size_t *bytes);
+LOBRA_API lobra_status lobra_grad_clip(const lobra_grad_set *set, const float *max_norm, const float *grad_scale, const int32_t *step,
+                             float *norm, float *clip_scale, int32_t *step_out, uint32_t flags, void *ws, size_t ws_bytes,
+                             void *hip_stream);
+
 /* Host-side dynamic bucketing (paper section 4.3, "Dynamic Bucketing"): the caller's step right before
  * the layer when chunks are padded.  Given the lengths of a batch and U candidate boundaries
  * u_1 < ... < u_U, choose at most R of them so that padding every sequence to the closest chosen
@@ -349,7 +475,7 @@ LOBRA_API lobra_status lobra_padded_segments(int64_t n_seq, const int32_t *padde
  * (host, may be NULL) counts the launches seen.  n_pairs = 0 or events = NULL detaches.
  * A plan with a trace attached must not be used from two threads at once. */
 enum { LOBRA_K_SHRINK = 1, LOBRA_K_GEMM = 2, LOBRA_K_GRAD_STAGE1 = 3, LOBRA_K_GRAD_STAGE2 = 4,
-       LOBRA_K_TOKEN_TASK = 5, LOBRA_K_ADAM = 6, LOBRA_K_SHRINK_GEMM = 7 };
+       LOBRA_K_TOKEN_TASK = 5, LOBRA_K_ADAM = 6, LOBRA_K_SHRINK_GEMM = 7, LOBRA_K_GATED = 8, LOBRA_K_BLOCK_NORM = 9 };
 LOBRA_API lobra_status lobra_mlora_plan_set_trace(lobra_mlora_plan *plan, void *const *events,
                                         int32_t n_pairs, int32_t *kernel_ids,
                                         int32_t *n_launched);

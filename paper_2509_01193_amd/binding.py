@@ -16,13 +16,15 @@ LIB_PATH = os.environ.get("LOBRA_MLORA_LIB") or os.path.join(_HERE, "liblobra_ml
 
 OK = 0
 F32, BF16 = 0, 1
-FLAG_ACCUMULATE_GRADS, FLAG_NO_DX = 1, 2
+FLAG_ACCUMULATE_GRADS, FLAG_NO_DX, FLAG_JOINT_NORM = 1, 2, 4
+ACT_SILU, ACT_GELU_TANH = 0, 1
 PLAN_HOST_ONLY, PLAN_PLAIN_KERNELS = 1, 2
 Q_SEGMENTS, Q_ROWBLOCK_SEG, Q_TOKEN_BLOCKS, Q_GRAD_CHUNKS, Q_TASK_CHUNKS, Q_BLOCK_RUNS = 0, 1, 2, 3, 4, 5
 Q_BLOCK_ORDER, Q_RUN_ORDER = 6, 7
 Q_SLICED, Q_FUSED_WG_RUNS, Q_FUSED_RUN_ROW, Q_FUSED_COUNT, Q_FUSED_TASK_ROW = 8, 9, 10, 11, 12
 Q_GEMM_TILE_ROWS, Q_BESIDE, Q_PRODUCT_TABLES = 13, 14, 15
 MAX_RANK = 128
+MAX_TOP, MAX_VOCAB, MAX_NORM_WIDTH = 32, 1 << 24, 16384
 
 EXPORTS = [
     "lobra_mlora_validate", "lobra_mlora_workspace_bytes", "lobra_mlora_fwd", "lobra_mlora_bwd", "lobra_token_task_map",
@@ -30,6 +32,11 @@ EXPORTS = [
     "lobra_mlora_plan_sizes", "lobra_mlora_plan_query", "lobra_mlora_plan_fwd", "lobra_mlora_plan_bwd",
     "lobra_mlora_plan_token_task_map", "lobra_mlora_fwd_static_ws", "lobra_mlora_adam_step", "lobra_dynamic_buckets",
     "lobra_padded_segments",
+    "lobra_mlora_gated_workspace_bytes", "lobra_mlora_gated_fwd", "lobra_mlora_gated_bwd",
+    "lobra_mlora_block_norm_workspace_bytes", "lobra_mlora_block_norm_fwd", "lobra_mlora_block_norm_bwd",
+    "lobra_token_logprob_fwd", "lobra_token_logprob_bwd",
+    "lobra_grad_set_device_bytes", "lobra_grad_set_create", "lobra_grad_set_init", "lobra_grad_set_destroy",
+    "lobra_grad_set_workspace_bytes", "lobra_grad_clip",
     "lobra_mlora_plan_set_trace", "lobra_status_string", "lobra_version",
 ]
 
@@ -48,6 +55,20 @@ class Desc(ctypes.Structure):
 class AdamConfig(ctypes.Structure):
     _fields_ = [("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
                 ("weight_decay", ctypes.c_float)]
+
+
+class BlockNormConfig(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("alpha", ctypes.c_float)]
+
+
+class LogprobDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("V", ctypes.c_int32), ("T", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("top_k", ctypes.c_int32)]
+
+
+class GradTensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("D", ctypes.c_int32),
+                ("rank_off", ctypes.POINTER(ctypes.c_int32))]
 
 
 class LobraError(RuntimeError):
@@ -99,6 +120,21 @@ def lib():
         L.lobra_mlora_plan_init.argtypes = [ctypes.POINTER(Desc), u32, vp, sz, vp, ctypes.POINTER(vp)]
         L.lobra_mlora_adam_step.restype = ctypes.c_int
         L.lobra_mlora_adam_step.argtypes = [vp, ctypes.POINTER(AdamConfig)] + [vp] * 13 + [vp]
+        L.lobra_mlora_gated_workspace_bytes.argtypes = [vp, ctypes.c_int32, szp]
+        L.lobra_mlora_gated_fwd.argtypes = [vp, ctypes.c_int32] + [vp] * 9 + [sz, vp]
+        L.lobra_mlora_gated_bwd.argtypes = [vp, ctypes.c_int32] + [vp] * 12 + [u32, vp, sz, vp]
+        L.lobra_mlora_block_norm_workspace_bytes.argtypes = [vp, szp]
+        L.lobra_mlora_block_norm_fwd.argtypes = [vp, ctypes.POINTER(BlockNormConfig)] + [vp] * 9 + [vp]
+        L.lobra_mlora_block_norm_bwd.argtypes = [vp, ctypes.POINTER(BlockNormConfig)] + [vp] * 14 + [u32, vp, sz, vp]
+        L.lobra_token_logprob_fwd.argtypes = [ctypes.POINTER(LogprobDesc)] + [vp] * 8 + [vp]
+        L.lobra_token_logprob_bwd.argtypes = [ctypes.POINTER(LogprobDesc)] + [vp] * 8 + [vp]
+        i32, gtp = ctypes.c_int32, ctypes.POINTER(GradTensor)
+        L.lobra_grad_set_device_bytes.argtypes = [gtp, i32, i32, szp]
+        L.lobra_grad_set_create.argtypes = [gtp, i32, i32, ctypes.POINTER(vp)]
+        L.lobra_grad_set_init.argtypes = [gtp, i32, i32, vp, sz, vp, ctypes.POINTER(vp)]
+        L.lobra_grad_set_destroy.argtypes = [vp]
+        L.lobra_grad_set_workspace_bytes.argtypes = [vp, szp]
+        L.lobra_grad_clip.argtypes = [vp] * 7 + [u32, vp, sz, vp]
         L.lobra_status_string.restype = ctypes.c_char_p
         L.lobra_status_string.argtypes = [ctypes.c_int]
         L.lobra_version.restype = ctypes.c_int
@@ -310,6 +346,152 @@ def lobra_mlora_adam_step(plan: Plan, cfg: AdamConfig, lr, step, grad_scale, dA,
     return st
 
 
+# ---- the steps around the linears -----------------------------------------------------------------------------------------
+def lobra_mlora_gated_workspace_bytes(plan: Plan, save: bool) -> int:
+    """Bytes of ws for lobra_mlora_gated_fwd; save: whether gu will be given."""
+    n = ctypes.c_size_t()
+    _check(lib().lobra_mlora_gated_workspace_bytes(plan.handle, int(bool(save)), ctypes.byref(n)), "lobra_mlora_gated_workspace_bytes")
+    return n.value
+
+
+def lobra_mlora_gated_fwd(plan: Plan, act, x, W, A, B, s, gu, h, h_save=None, ws=None, stream=None, check=True):
+    """h = a(g) u of the plan's gate and up projection; gu [T, 2 f] keeps [g | u] for backward, or None.  Returns the status."""
+    st = lib().lobra_mlora_gated_fwd(plan.handle, int(act), _ptr(x), _ptr(W), _ptr(A), _ptr(B), _ptr(s), _ptr(gu), _ptr(h), _ptr(h_save),
+                                     _ptr(ws), _nbytes(ws), _stream(stream))
+    if check:
+        _check(st, "lobra_mlora_gated_fwd")
+    return st
+
+
+def lobra_mlora_gated_bwd(plan: Plan, act, x, W, A, B, s, gu, dh, h_saved, dgu, dx, dA, dB, flags=0, ws=None, stream=None, check=True):
+    """dgu = [dg | du] (may be gu), then the layer's dx, dA, dB.  Returns the status."""
+    st = lib().lobra_mlora_gated_bwd(plan.handle, int(act), _ptr(x), _ptr(W), _ptr(A), _ptr(B), _ptr(s), _ptr(gu), _ptr(dh), _ptr(h_saved),
+                                     _ptr(dgu), _ptr(dx), _ptr(dA), _ptr(dB), int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
+    if check:
+        _check(st, "lobra_mlora_gated_bwd")
+    return st
+
+
+def lobra_mlora_block_norm_workspace_bytes(plan: Plan) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().lobra_mlora_block_norm_workspace_bytes(plan.handle, ctypes.byref(n)), "lobra_mlora_block_norm_workspace_bytes")
+    return n.value
+
+
+def lobra_mlora_block_norm_fwd(plan: Plan, cfg: BlockNormConfig, r, b, w_post, gate, w_pre, r_out, x, rstd_post=None, rstd_pre=None,
+                               stream=None, check=True):
+    """r_out = r + alpha gate_t w_post b / rms(b), x = w_pre r_out / rms(r_out).  Returns the status."""
+    st = lib().lobra_mlora_block_norm_fwd(plan.handle, ctypes.byref(cfg), _ptr(r), _ptr(b), _ptr(w_post), _ptr(gate), _ptr(w_pre), _ptr(r_out),
+                                          _ptr(x), _ptr(rstd_post), _ptr(rstd_pre), _stream(stream))
+    if check:
+        _check(st, "lobra_mlora_block_norm_fwd")
+    return st
+
+
+def lobra_mlora_block_norm_bwd(plan: Plan, cfg: BlockNormConfig, r_out, b, w_post, gate, w_pre, rstd_post, rstd_pre, dr_out, dx, dr, db,
+                               dgate=None, dw_post=None, dw_pre=None, flags=0, ws=None, stream=None, check=True):
+    st = lib().lobra_mlora_block_norm_bwd(plan.handle, ctypes.byref(cfg), _ptr(r_out), _ptr(b), _ptr(w_post), _ptr(gate), _ptr(w_pre),
+                                          _ptr(rstd_post), _ptr(rstd_pre), _ptr(dr_out), _ptr(dx), _ptr(dr), _ptr(db), _ptr(dgate), _ptr(dw_post),
+                                          _ptr(dw_pre), int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
+    if check:
+        _check(st, "lobra_mlora_block_norm_bwd")
+    return st
+
+
+def make_logprob_desc(dtype, T, V, ld=0, top_k=0) -> LogprobDesc:
+    """`dtype` is "f32"/"bf16" or the enum value; ld = row pitch of the logits in elements (0: V)."""
+    return LogprobDesc(int({"f32": F32, "bf16": BF16}.get(dtype, dtype)), int(V), int(T), int(ld), int(top_k))
+
+
+def _rows_ptr(t, desc: LogprobDesc):
+    """A [T, V] tensor of the descriptor's type whose rows are ld elements apart (a slice of wider rows, for one)."""
+    if t is None or isinstance(t, int):
+        return _ptr(t)
+    import torch
+    assert t.dtype == (torch.float32 if desc.dtype == F32 else torch.bfloat16), "logits of another type than the descriptor's"
+    assert tuple(t.shape) == (desc.T, desc.V), "logits of another shape than the descriptor's"
+    assert desc.T <= 1 or t.stride(0) == (desc.ld or desc.V), "rows of logits are not ld elements apart"
+    assert desc.V <= 1 or t.stride(1) == 1, "rows of logits must be contiguous"
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def lobra_token_logprob_fwd(desc: LogprobDesc, logits, target, logp=None, lse=None, lse_rest=None, entropy=None, top_logp=None, top_id=None,
+                            stream=None, check=True):
+    """logp = ln softmax(logits)[target], lse, entropy and the top_k likeliest tokens of every row.  Returns the status."""
+    st = lib().lobra_token_logprob_fwd(ctypes.byref(desc), _rows_ptr(logits, desc), _ptr(target), _ptr(logp), _ptr(lse), _ptr(lse_rest), _ptr(entropy),
+                                       _ptr(top_logp), _ptr(top_id), _stream(stream))
+    if check:
+        _check(st, "lobra_token_logprob_fwd")
+    return st
+
+
+def lobra_token_logprob_bwd(desc: LogprobDesc, logits, target, lse, lse_rest, entropy, dlogp, dentropy, dlogits, stream=None, check=True):
+    """dlogits (may be logits) from dlogp and dentropy.  Returns the status."""
+    st = lib().lobra_token_logprob_bwd(ctypes.byref(desc), _rows_ptr(logits, desc), _ptr(target), _ptr(lse), _ptr(lse_rest), _ptr(entropy), _ptr(dlogp),
+                                       _ptr(dentropy), _rows_ptr(dlogits, desc), _stream(stream))
+    if check:
+        _check(st, "lobra_token_logprob_bwd")
+    return st
+
+
+def make_grad_tensors(tensors):
+    """(array of GradTensor, keepalive) of [(grad, out or None, rank_off)]: fp32 tensors [R, D]."""
+    arr, keep = (GradTensor * max(len(tensors), 1))(), []
+    for i, (g, out, rank_off) in enumerate(tensors):
+        ro = _i32(rank_off)
+        keep += [g, out, ro]
+        arr[i].grad, arr[i].out, arr[i].D = _ptr(g), _ptr(out), int(g.shape[1])
+        arr[i].rank_off = ro.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+        assert tuple(g.shape) == (int(ro[-1]), g.shape[1]) and (out is None or out.shape == g.shape), "a gradient of another shape than its ranks'"
+    return arr, keep
+
+
+class GradSet:
+    """Owns a ``lobra_grad_set``: the gradients of all layers, [(grad, out or None, rank_off)], with the tensors kept alive."""
+
+    def __init__(self, tensors, n_tasks, device_mem=None, stream=None):
+        """device_mem (a device uint8 tensor of at least grad_set_device_bytes(...)): lobra_grad_set_init places the set there with
+        an asynchronous copy on `stream`; None: lobra_grad_set_create allocates."""
+        arr, self._keep = make_grad_tensors(tensors)
+        self.handle, self.n_tasks = ctypes.c_void_p(), int(n_tasks)
+        if device_mem is None:
+            _check(lib().lobra_grad_set_create(arr, len(tensors), self.n_tasks, ctypes.byref(self.handle)), "lobra_grad_set_create")
+        else:
+            self._keep.append(device_mem)
+            _check(lib().lobra_grad_set_init(arr, len(tensors), self.n_tasks, _ptr(device_mem), _nbytes(device_mem), _stream(stream),
+                                             ctypes.byref(self.handle)), "lobra_grad_set_init")
+        n = ctypes.c_size_t()
+        _check(lib().lobra_grad_set_workspace_bytes(self.handle, ctypes.byref(n)), "lobra_grad_set_workspace_bytes")
+        self.ws_bytes = n.value
+
+    def close(self):
+        if getattr(self, "handle", None) is not None and self.handle.value:
+            lib().lobra_grad_set_destroy(self.handle)
+            self.handle = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def grad_set_device_bytes(tensors, n_tasks) -> int:
+    arr, _keep = make_grad_tensors(tensors)
+    n = ctypes.c_size_t()
+    _check(lib().lobra_grad_set_device_bytes(arr, len(tensors), int(n_tasks), ctypes.byref(n)), "lobra_grad_set_device_bytes")
+    return n.value
+
+
+def lobra_grad_clip(gset: GradSet, max_norm, grad_scale, step, norm, clip_scale, step_out, flags=0, ws=None, stream=None, check=True):
+    """Every task's gradient norm, and the factor (for lobra_mlora_adam_step's grad_scale) that clips it.  Returns the status."""
+    st = lib().lobra_grad_clip(gset.handle, _ptr(max_norm), _ptr(grad_scale), _ptr(step), _ptr(norm), _ptr(clip_scale), _ptr(step_out), int(flags),
+                               _ptr(ws), _nbytes(ws), _stream(stream))
+    if check:
+        _check(st, "lobra_grad_clip")
+    return st
+
+
 def lobra_dynamic_buckets(seq_len, bounds, R):
     """Host-side dynamic bucketing: returns (chosen boundaries ascending, total pad tokens)."""
     L = lib()
@@ -443,7 +625,7 @@ class DeviceProblem:
 # ---------------------------------------------------------------------------------------------
 # launch trace: per-kernel durations from HIP events recorded on the stream the kernels run on
 # ---------------------------------------------------------------------------------------------
-KERNEL_NAMES = {1: "shrink", 2: "gemm", 3: "grad_stage1", 4: "grad_stage2", 5: "token_task", 6: "adam", 7: "shrink_gemm"}
+KERNEL_NAMES = {1: "shrink", 2: "gemm", 3: "grad_stage1", 4: "grad_stage2", 5: "token_task", 6: "adam", 7: "shrink_gemm", 8: "gated", 9: "block_norm"}
 
 
 class LaunchTrace:

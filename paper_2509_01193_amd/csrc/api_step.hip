@@ -1,0 +1,380 @@
+// extern "C" entry points of the steps around the LoRA linears: the gated feed-forward block, the norms around a residual block, log
+// probabilities, gradient norms and clipping.  Argument checks on the host, then launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "api_common.h"
+
+using namespace lobra;
+
+namespace {
+
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+
+// ---- gated feed-forward block ------------------------------------------------------------------------------------------------
+
+// The plan is one of gate and up projection, and the activation is known.
+lobra_status gated_check(const Plan& p, int32_t act)
+{
+    if (p.n_proj != 2 || (act != LOBRA_ACT_SILU && act != LOBRA_ACT_GELU_TANH)) return LOBRA_ERR_SHAPE;
+    return LOBRA_OK;
+}
+
+// Bytes in front of the layer's own workspace for [g | u] where the caller does not keep it.
+size_t gated_scratch(const Plan& p)
+{
+    return align256(size_t(p.desc.T) * size_t(p.desc.d_out) * (p.desc.dtype == LOBRA_F32 ? 4 : 2));
+}
+
+// ---- norms ----------------------------------------------------------------------------------------------------------------
+
+lobra_status block_norm_check(const Plan& p, const lobra_block_norm_config* cfg)
+{
+    if (!cfg) return LOBRA_ERR_NULL;
+    if (!(cfg->eps >= 0.f) || !std::isfinite(cfg->eps) || !std::isfinite(cfg->alpha) || p.desc.d_in > LOBRA_MAX_NORM_WIDTH) return LOBRA_ERR_SHAPE;
+    return LOBRA_OK;
+}
+
+// ---- log probabilities --------------------------------------------------------------------------------------------------------
+
+lobra_status logprob_shape(const lobra_logprob_desc* d, LogprobShape* s)
+{
+    if (!d) return LOBRA_ERR_NULL;
+    if (d->dtype != LOBRA_F32 && d->dtype != LOBRA_BF16) return LOBRA_ERR_DTYPE;
+    const int64_t ld = d->ld == 0 ? d->V : d->ld;
+    if (d->V < 1 || d->V > LOBRA_MAX_VOCAB || d->T < 0 || d->T >= (int64_t(1) << 31) || ld < d->V || d->top_k < 0 || d->top_k > LOBRA_MAX_TOP)
+        return LOBRA_ERR_SHAPE;
+    if (d->T > 0 && ld >= (int64_t(1) << 60) / d->T) return LOBRA_ERR_SHAPE;
+    *s = LogprobShape{d->dtype, d->V, d->top_k, d->T, ld};
+    return LOBRA_OK;
+}
+
+}  // namespace
+
+// The tensors of a set, cut into pieces of one task each.
+struct lobra_grad_set {
+    std::vector<unsigned char> blob;         // what the device has: the pieces, then task_piece [n_tasks + 1]
+    size_t o_task_piece = 0;
+    int32_t n_pieces = 0, n_tasks = 0;
+    bool any_out = false;
+    int device = -1;
+    void* dev = nullptr;
+    bool owns = false;
+};
+
+namespace {
+
+// Elements of a piece: some eight workgroups per compute unit, of a few loads a thread at least, and not so large that the last
+// ones are alone.
+int64_t piece_elements(int64_t total)
+{
+    const int64_t n = (total / 2048 + 1023) / 1024 * 1024;
+    return std::min<int64_t>(std::max<int64_t>(n, 2048), 32768);
+}
+
+lobra_status make_set(const lobra_grad_tensor* tensors, int32_t n_tensors, int32_t n_tasks, lobra_grad_set** out)
+{
+    if (n_tensors < 0 || n_tasks < 0 || n_tasks >= 1 << 23) return LOBRA_ERR_SHAPE;
+    if (n_tensors > 0 && !tensors) return LOBRA_ERR_NULL;
+    int64_t total = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) {
+        const lobra_grad_tensor& g = tensors[i];
+        if (!g.rank_off) return LOBRA_ERR_NULL;
+        if (g.D < 1 || g.D > LOBRA_MAX_WIDTH) return LOBRA_ERR_SHAPE;
+        if (g.rank_off[0] != 0) return LOBRA_ERR_RANK;
+        for (int32_t t = 0; t < n_tasks; ++t)
+            if (g.rank_off[t + 1] < g.rank_off[t]) return LOBRA_ERR_RANK;
+        const int64_t n = int64_t(g.rank_off[n_tasks]) * g.D;
+        if (n >= int64_t(1) << 40) return LOBRA_ERR_SHAPE;
+        if (n > 0 && !g.grad) return LOBRA_ERR_NULL;
+        if (!aligned16(g.grad) || !aligned16(g.out)) return LOBRA_ERR_ALIGN;
+        total += n;
+    }
+    const int64_t per = piece_elements(total);
+    if (total / per + int64_t(n_tensors) * n_tasks >= int64_t(1) << 23) return LOBRA_ERR_SHAPE;     // (a launch holds less than 2^32 threads)
+    lobra_grad_set* s = new (std::nothrow) lobra_grad_set();
+    if (!s) return LOBRA_ERR_NOMEM;
+    try {
+        std::vector<GradPiece> pieces;
+        std::vector<int32_t> task_piece(size_t(n_tasks) + 1, 0);
+        for (int32_t t = 0; t < n_tasks; ++t) {
+            for (int32_t i = 0; i < n_tensors; ++i) {
+                const lobra_grad_tensor& g = tensors[i];
+                const int64_t end = int64_t(g.rank_off[t + 1]) * g.D;
+                for (int64_t at = int64_t(g.rank_off[t]) * g.D; at < end;) {
+                    const int64_t next = std::min(end, (at / per + 1) * per);       // (pieces begin at multiples of `per`: aligned)
+                    pieces.push_back(GradPiece{g.grad + at, g.out ? g.out + at : nullptr, int32_t(next - at), t});
+                    at = next;
+                }
+                s->any_out = s->any_out || g.out;
+            }
+            task_piece[size_t(t) + 1] = int32_t(pieces.size());
+        }
+        s->n_pieces = int32_t(pieces.size());
+        s->n_tasks = n_tasks;
+        s->o_task_piece = pieces.size() * sizeof(GradPiece);
+        s->blob.resize(s->o_task_piece + task_piece.size() * sizeof(int32_t));
+        if (!pieces.empty()) std::memcpy(s->blob.data(), pieces.data(), s->o_task_piece);
+        std::memcpy(s->blob.data() + s->o_task_piece, task_piece.data(), task_piece.size() * sizeof(int32_t));
+    } catch (const std::bad_alloc&) {
+        delete s;
+        return LOBRA_ERR_NOMEM;
+    }
+    *out = s;
+    return LOBRA_OK;
+}
+
+// Partial sums, then the tasks' factors.
+size_t clip_ws_bytes(const lobra_grad_set& s)
+{
+    return align256(size_t(s.n_pieces) * sizeof(double)) + size_t(s.n_tasks) * sizeof(float);
+}
+
+}  // namespace
+
+extern "C" {
+
+lobra_status lobra_mlora_gated_workspace_bytes(const lobra_mlora_plan* plan, int32_t save_gu, size_t* fwd_bytes)
+{
+    if (!plan) return LOBRA_ERR_PLAN;
+    if (!fwd_bytes) return LOBRA_ERR_NULL;
+    if (plan->n_proj != 2) return LOBRA_ERR_SHAPE;
+    *fwd_bytes = (save_gu ? 0 : gated_scratch(*plan)) + plan->fwd_ws_bytes;
+    return LOBRA_OK;
+}
+
+lobra_status lobra_mlora_gated_fwd(const lobra_mlora_plan* plan, int32_t act, const void* x, const void* W, const void* A, const void* B,
+                                   const float* s, void* gu, void* h, void* h_save, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    lobra_status rs = runnable(plan);
+    if (rs != LOBRA_OK) return rs;
+    const Plan& p = *plan;
+    if ((rs = gated_check(p, act)) != LOBRA_OK) return rs;
+    if (p.desc.T == 0) return LOBRA_OK;
+    if (!h) return LOBRA_ERR_NULL;
+    if (!aligned16(h) || !aligned16(gu) || !aligned16(ws)) return LOBRA_ERR_ALIGN;
+    const size_t own = gu ? 0 : gated_scratch(p);
+    if (own > 0 && (!ws || ws_bytes < own)) return LOBRA_ERR_WORKSPACE;
+    void* const y = gu ? gu : ws;
+    char* const rest = ws ? static_cast<char*>(ws) + own : nullptr;
+    if ((rs = lobra_mlora_plan_fwd(plan, x, W, A, B, s, y, h_save, rest, ws_bytes - own, hip_stream)) != LOBRA_OK) return rs;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_activate(p.desc.dtype, act, p.desc.T, p.dg, y, h, st));
+    return LOBRA_OK;
+}
+
+lobra_status lobra_mlora_gated_bwd(const lobra_mlora_plan* plan, int32_t act, const void* x, const void* W, const void* A, const void* B,
+                                   const float* s, const void* gu, const void* dh, const void* h_saved, void* dgu, void* dx, float* dA, float* dB,
+                                   uint32_t flags, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    lobra_status rs = runnable(plan);
+    if (rs != LOBRA_OK) return rs;
+    const Plan& p = *plan;
+    if ((rs = gated_check(p, act)) != LOBRA_OK) return rs;
+    if (p.desc.T > 0) {
+        if (!gu || !dh || !dgu) return LOBRA_ERR_NULL;
+        if (!aligned16(gu) || !aligned16(dh) || !aligned16(dgu)) return LOBRA_ERR_ALIGN;
+    }
+    if ((rs = plan_bwd_check(p, x, W, A, B, s, dgu, h_saved, dx, dA, dB, flags, ws, ws_bytes)) != LOBRA_OK) return rs;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (p.desc.T > 0) LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_derive(p.desc.dtype, act, p.desc.T, p.dg, gu, dh, dgu, st));
+    return lobra_mlora_plan_bwd(plan, x, W, A, B, s, dgu, h_saved, dx, dA, dB, flags, ws, ws_bytes, hip_stream);
+}
+
+lobra_status lobra_mlora_block_norm_workspace_bytes(const lobra_mlora_plan* plan, size_t* bwd_bytes)
+{
+    if (!plan) return LOBRA_ERR_PLAN;
+    if (!bwd_bytes) return LOBRA_ERR_NULL;
+    if (plan->desc.d_in > LOBRA_MAX_NORM_WIDTH) return LOBRA_ERR_SHAPE;
+    *bwd_bytes = block_norm_part_bytes(plan->desc.T, plan->desc.d_in, int32_t(plan->cseg_task.size()), plan->desc.dtype);
+    return LOBRA_OK;
+}
+
+lobra_status lobra_mlora_block_norm_fwd(const lobra_mlora_plan* plan, const lobra_block_norm_config* cfg, const void* r, const void* b,
+                                        const void* w_post, const void* gate, const void* w_pre, void* r_out, void* x, float* rstd_post,
+                                        float* rstd_pre, void* hip_stream)
+{
+    lobra_status rs = runnable(plan);
+    if (rs != LOBRA_OK) return rs;
+    const Plan& p = *plan;
+    if ((rs = block_norm_check(p, cfg)) != LOBRA_OK) return rs;
+    if (p.desc.T == 0) return LOBRA_OK;
+    if (!r || (b && !r_out) || (w_pre && !x)) return LOBRA_ERR_NULL;
+    for (const void* q : {r, b, w_post, gate, w_pre, static_cast<const void*>(r_out), static_cast<const void*>(x)})
+        if (!aligned16(q)) return LOBRA_ERR_ALIGN;
+    if (!aligned4(rstd_post) || !aligned4(rstd_pre)) return LOBRA_ERR_ALIGN;
+    if (!b && !w_pre) return LOBRA_OK;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const PlanDev pd = device_view(p);
+    const BlockNorm bn{cfg->eps, cfg->alpha, w_post, gate, w_pre, b && w_post, b != nullptr};
+    LOBRA_LAUNCH(p, st, LOBRA_K_BLOCK_NORM, block_norm_fwd(pd, p.desc.dtype, bn, r, b, r_out, x, rstd_post, rstd_pre, st));
+    return LOBRA_OK;
+}
+
+lobra_status lobra_mlora_block_norm_bwd(const lobra_mlora_plan* plan, const lobra_block_norm_config* cfg, const void* r_out, const void* b,
+                                        const void* w_post, const void* gate, const void* w_pre, const float* rstd_post, const float* rstd_pre,
+                                        const void* dr_out, const void* dx, void* dr, void* db, float* dgate, float* dw_post, float* dw_pre,
+                                        uint32_t flags, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    lobra_status rs = runnable(plan);
+    if (rs != LOBRA_OK) return rs;
+    const Plan& p = *plan;
+    if ((rs = block_norm_check(p, cfg)) != LOBRA_OK) return rs;
+    const bool post = b && w_post;
+    // what has no norm, or no gate, has no gradient of it
+    if ((dgate && (!b || !gate)) || (dw_post && !post) || (dw_pre && (!w_pre || !dx))) return LOBRA_ERR_NULL;
+    if (p.desc.T > 0) {
+        if (!dr || (b && !db) || (dx && (!w_pre || !r_out || !rstd_pre)) || (post && !rstd_post)) return LOBRA_ERR_NULL;
+    }
+    for (const void* q : {r_out, b, w_post, gate, w_pre, dr_out, dx, static_cast<const void*>(dr), static_cast<const void*>(db),
+                          static_cast<const void*>(dgate), static_cast<const void*>(dw_post), static_cast<const void*>(dw_pre),
+                          static_cast<const void*>(ws)})
+        if (!aligned16(q)) return LOBRA_ERR_ALIGN;
+    if (!aligned4(rstd_post) || !aligned4(rstd_pre)) return LOBRA_ERR_ALIGN;
+    if ((dgate || dw_post || dw_pre) &&
+        (!ws || ws_bytes < block_norm_part_bytes(p.desc.T, p.desc.d_in, int32_t(p.cseg_task.size()), p.desc.dtype)))
+        return LOBRA_ERR_WORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const PlanDev pd = device_view(p);
+    const BlockNorm bn{cfg->eps, cfg->alpha, w_post, gate, w_pre, post, b != nullptr};
+    LOBRA_LAUNCH(p, st, LOBRA_K_BLOCK_NORM,
+                 block_norm_bwd(pd, p.desc.dtype, bn, r_out, b, rstd_post, rstd_pre, dr_out, dx, dr, db, dgate, dw_post, dw_pre,
+                                (flags & LOBRA_FLAG_ACCUMULATE_GRADS) != 0, static_cast<float*>(ws), st));
+    return LOBRA_OK;
+}
+
+lobra_status lobra_token_logprob_fwd(const lobra_logprob_desc* desc, const void* logits, const int32_t* target, float* logp, float* lse,
+                                     float* lse_rest, float* entropy, float* top_logp, int32_t* top_id, void* hip_stream)
+{
+    LogprobShape s;
+    const lobra_status rs = logprob_shape(desc, &s);
+    if (rs != LOBRA_OK) return rs;
+    if (s.T == 0) return LOBRA_OK;
+    if (!logits) return LOBRA_ERR_NULL;
+    if (!aligned16(logits)) return LOBRA_ERR_ALIGN;
+    for (const void* q : {static_cast<const void*>(target), static_cast<const void*>(logp), static_cast<const void*>(lse),
+                          static_cast<const void*>(lse_rest), static_cast<const void*>(entropy), static_cast<const void*>(top_logp), static_cast<const void*>(top_id)})
+        if (!aligned4(q)) return LOBRA_ERR_ALIGN;
+    LOBRA_HIP(logprob_fwd(s, logits, target, LogprobOut{logp, lse, lse_rest, entropy, top_logp, top_id}, static_cast<hipStream_t>(hip_stream)));
+    return LOBRA_OK;
+}
+
+lobra_status lobra_token_logprob_bwd(const lobra_logprob_desc* desc, const void* logits, const int32_t* target, const float* lse,
+                                     const float* lse_rest, const float* entropy, const float* dlogp, const float* dentropy, void* dlogits,
+                                     void* hip_stream)
+{
+    LogprobShape s;
+    const lobra_status rs = logprob_shape(desc, &s);
+    if (rs != LOBRA_OK) return rs;
+    if (s.T == 0) return LOBRA_OK;
+    if (!logits || !lse || !dlogits || (dentropy && !entropy)) return LOBRA_ERR_NULL;
+    if (!aligned16(logits) || !aligned16(dlogits)) return LOBRA_ERR_ALIGN;
+    for (const void* q : {static_cast<const void*>(target), static_cast<const void*>(lse), static_cast<const void*>(lse_rest),
+                          static_cast<const void*>(entropy),
+                          static_cast<const void*>(dlogp), static_cast<const void*>(dentropy)})
+        if (!aligned4(q)) return LOBRA_ERR_ALIGN;
+    LOBRA_HIP(logprob_bwd(s, logits, target, LogprobGrad{lse, lse_rest, entropy, dlogp, dentropy}, dlogits, static_cast<hipStream_t>(hip_stream)));
+    return LOBRA_OK;
+}
+
+lobra_status lobra_grad_set_device_bytes(const lobra_grad_tensor* tensors, int32_t n_tensors, int32_t n_tasks, size_t* bytes)
+{
+    if (!bytes) return LOBRA_ERR_NULL;
+    lobra_grad_set* s = nullptr;
+    const lobra_status rs = make_set(tensors, n_tensors, n_tasks, &s);
+    if (rs != LOBRA_OK) return rs;
+    *bytes = s->blob.size();
+    delete s;
+    return LOBRA_OK;
+}
+
+lobra_status lobra_grad_set_create(const lobra_grad_tensor* tensors, int32_t n_tensors, int32_t n_tasks, lobra_grad_set** out)
+{
+    if (!out) return LOBRA_ERR_NULL;
+    lobra_grad_set* s = nullptr;
+    lobra_status rs = make_set(tensors, n_tensors, n_tasks, &s);
+    if (rs != LOBRA_OK) return rs;
+    if (hipGetDevice(&s->device) != hipSuccess) rs = LOBRA_ERR_HIP;
+    else if (hipMalloc(&s->dev, s->blob.size()) != hipSuccess) rs = LOBRA_ERR_NOMEM;
+    else if (hipMemcpy(s->dev, s->blob.data(), s->blob.size(), hipMemcpyHostToDevice) != hipSuccess) {
+        (void)hipFree(s->dev);
+        rs = LOBRA_ERR_HIP;
+    }
+    if (rs != LOBRA_OK) {
+        delete s;
+        return rs;
+    }
+    s->owns = true;
+    *out = s;
+    return LOBRA_OK;
+}
+
+lobra_status lobra_grad_set_init(const lobra_grad_tensor* tensors, int32_t n_tensors, int32_t n_tasks, void* device_mem, size_t device_bytes,
+                                 void* hip_stream, lobra_grad_set** out)
+{
+    if (!out) return LOBRA_ERR_NULL;
+    lobra_grad_set* s = nullptr;
+    lobra_status rs = make_set(tensors, n_tensors, n_tasks, &s);
+    if (rs != LOBRA_OK) return rs;
+    if (!device_mem || device_bytes < s->blob.size()) rs = LOBRA_ERR_WORKSPACE;
+    else if (!aligned16(device_mem)) rs = LOBRA_ERR_ALIGN;
+    else if (hipGetDevice(&s->device) != hipSuccess) rs = LOBRA_ERR_HIP;
+    // the source of the copy is the set's own host image, which lives as long as the set
+    else if (hipMemcpyAsync(device_mem, s->blob.data(), s->blob.size(), hipMemcpyHostToDevice, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+        rs = LOBRA_ERR_HIP;
+    if (rs != LOBRA_OK) {
+        delete s;
+        return rs;
+    }
+    s->dev = device_mem;
+    *out = s;
+    return LOBRA_OK;
+}
+
+lobra_status lobra_grad_set_destroy(lobra_grad_set* set)
+{
+    if (!set) return LOBRA_OK;
+    const lobra_status rs = set->owns && hipFree(set->dev) != hipSuccess ? LOBRA_ERR_HIP : LOBRA_OK;
+    delete set;
+    return rs;
+}
+
+lobra_status lobra_grad_set_workspace_bytes(const lobra_grad_set* set, size_t* bytes)
+{
+    if (!set) return LOBRA_ERR_PLAN;
+    if (!bytes) return LOBRA_ERR_NULL;
+    *bytes = clip_ws_bytes(*set);
+    return LOBRA_OK;
+}
+
+lobra_status lobra_grad_clip(const lobra_grad_set* set, const float* max_norm, const float* grad_scale, const int32_t* step, float* norm,
+                             float* clip_scale, int32_t* step_out, uint32_t flags, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    if (!set || !set->dev) return LOBRA_ERR_PLAN;
+    int dev = -1;
+    LOBRA_HIP(hipGetDevice(&dev));
+    if (dev != set->device) return LOBRA_ERR_PLAN;
+    if (set->n_tasks == 0) return LOBRA_OK;
+    if ((step == nullptr) != (step_out == nullptr)) return LOBRA_ERR_NULL;
+    for (const void* q : {static_cast<const void*>(max_norm), static_cast<const void*>(grad_scale), static_cast<const void*>(step),
+                          static_cast<const void*>(norm), static_cast<const void*>(clip_scale), static_cast<const void*>(step_out)})
+        if (!aligned4(q)) return LOBRA_ERR_ALIGN;
+    if (!aligned16(ws)) return LOBRA_ERR_ALIGN;
+    if (!ws || ws_bytes < clip_ws_bytes(*set)) return LOBRA_ERR_WORKSPACE;
+    const char* d = static_cast<const char*>(set->dev);
+    double* partial = static_cast<double*>(ws);
+    float* scale = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(size_t(set->n_pieces) * sizeof(double)));
+    LOBRA_HIP(grad_clip(reinterpret_cast<const GradPiece*>(d), reinterpret_cast<const int32_t*>(d + set->o_task_piece), set->n_pieces, set->n_tasks,
+                        set->any_out, max_norm, grad_scale, step, norm, clip_scale, step_out, (flags & LOBRA_FLAG_JOINT_NORM) != 0, partial, scale,
+                        static_cast<hipStream_t>(hip_stream)));
+    return LOBRA_OK;
+}
+
+}  // extern "C"

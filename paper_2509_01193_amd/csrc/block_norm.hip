@@ -1,0 +1,486 @@
+// Norms after one residual block and before the next, with the block's gate and residual scale, in one pass.
+//     n = 1 / rms(b)   r' = r + alpha gate_t w_post b n   m = 1 / rms(r')   x = w_pre r' m
+// Backward, with bh = b n, rh = r' m, u = w_pre dx, q = alpha gate_t w_post:
+//     g = dr' + m (u - rh mean(u rh))            -> dr
+//     db = n (q g - bh mean(q g bh))             (no post norm: db = alpha gate_t g)
+//     dgate_t = alpha w_post sum_t g bh   dw_post = alpha sum gate_t g bh   dw_pre = sum dx rh
+// The two means of backward are one reduction: with s1 = sum u rh, s2 = sum q bh (dr' + m u), s3 = sum q bh rh, mean(u rh) = s1 / d and
+// mean(q g bh) = (s2 - m s1 / d s3) / d.
+// A row lives in the registers of a team of threads - a wave, or a workgroup - from its read to its write; rows wider than a workgroup
+// holds are read again instead.  Backward's teams take neighbouring rows and keep the sums over tokens in registers from row to row; they
+// write them out where their rows end, the gate's also where a segment ends (slot: team + segment, which no two runs share), and a second
+// launch adds them in order.
+// Bound: memory, 4 T d elements forward and 6 T d backward.
+#include "kernels.h"
+#include "row_common.h"
+
+namespace lobra {
+
+using namespace rows;
+
+namespace {
+
+// N consecutive elements of E: a 16-byte packet, or a single element where rows keep no such alignment.
+template <typename E, int N> struct Piece {
+    static __device__ __forceinline__ void load(const E* p, float (&v)[N]) { Packet<E>::widen(*reinterpret_cast<const u32x4*>(p), v); }
+    static __device__ __forceinline__ void store(E* p, const float (&v)[N]) { *reinterpret_cast<u32x4*>(p) = Packet<E>::narrow(v); }
+};
+template <typename E> struct Piece<E, 1> {
+    static __device__ __forceinline__ void load(const E* p, float (&v)[1]) { v[0] = Elem<E>::load(p, 0); }
+    static __device__ __forceinline__ void store(E* p, const float (&v)[1]) { Elem<E>::store(p, 0, v[0]); }
+};
+// v as the element type holds it
+template <typename E> __device__ __forceinline__ float rounded(float v);
+template <> __device__ __forceinline__ float rounded<float>(float v) { return v; }
+template <> __device__ __forceinline__ float rounded<uint16_t>(float v) { return float((__bf16)v); }
+
+// Sums over a team of NT threads (64: a wave).  lds: one array of K NT / 64 floats per call site and parity of the row.
+template <int NT, int K> __device__ __forceinline__ void team_sum(float (&v)[K], float* lds)
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
+    if constexpr (NT > 64) {
+        const int w = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) lds[w * K + k] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = 0.f;
+#pragma unroll
+            for (int o = 0; o < NT / 64; ++o) v[k] += lds[o * K + k];
+        }
+    }
+}
+
+template <typename E> struct NormArgs {
+    const E *r, *b, *w_post, *gate, *w_pre;
+    E *r_out, *x;
+    float *rstd_post, *rstd_pre;
+    int32_t d;
+    float eps, alpha;
+    bool post;
+};
+
+// task of a row, -1: none
+__device__ __forceinline__ int32_t row_task(const PlanDev& pd, int32_t row) { return pd.cseg_task[segment_of_row(pd, row)]; }
+
+// I pieces of N elements per thread hold a row of up to NT I N; BT / NT teams per workgroup, a row each.
+template <typename E, int N, int NT, int I>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT)
+void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a)
+{
+    constexpr int BT = NT < 256 ? 256 : NT;
+    __shared__ float lds[2][NT / 64];
+    const int32_t row = int32_t(blockIdx.x) * (BT / NT) + int32_t(threadIdx.x) / NT, t = threadIdx.x % NT;
+    if (row >= pd.T) return;                          // (whole waves; with NT > 64 a workgroup has one row)
+    const size_t base = size_t(row) * a.d;
+    float v[I][N], bv[I][N];
+    float sums[1];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int32_t c = (t + i * NT) * N;
+        if (c < a.d) {
+            Piece<E, N>::load(a.r + base + c, v[i]);
+            if (a.b) Piece<E, N>::load(a.b + base + c, bv[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[i][e] = bv[i][e] = 0.f;
+        }
+    }
+    if (a.b) {
+        float n = 1.f;
+        if (a.post) {
+            sums[0] = 0.f;
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) sums[0] = fmaf(bv[i][e], bv[i][e], sums[0]);
+            team_sum<NT, 1>(sums, lds[0]);
+            n = 1.f / sqrtf(sums[0] / float(a.d) + a.eps);
+            if (t == 0 && a.rstd_post) a.rstd_post[row] = n;
+        }
+        const int32_t task = a.gate ? row_task(pd, row) : -1;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int32_t c = (t + i * NT) * N;
+            if (c >= a.d) continue;
+            float k[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) k[e] = a.alpha;
+            if (a.post) {
+                float w[N];
+                Piece<E, N>::load(a.w_post + c, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e) k[e] *= w[e] * n;
+            }
+            if (task >= 0) {
+                float w[N];
+                Piece<E, N>::load(a.gate + size_t(task) * a.d + c, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e) k[e] *= w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[i][e] = rounded<E>(fmaf(k[e], bv[i][e], v[i][e]));
+            Piece<E, N>::store(a.r_out + base + c, v[i]);
+        }
+    }
+    if (!a.w_pre) return;
+    sums[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sums[0] = fmaf(v[i][e], v[i][e], sums[0]);
+    team_sum<NT, 1>(sums, lds[1]);
+    const float m = 1.f / sqrtf(sums[0] / float(a.d) + a.eps);
+    if (t == 0 && a.rstd_pre) a.rstd_pre[row] = m;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int32_t c = (t + i * NT) * N;
+        if (c >= a.d) continue;
+        float w[N];
+        Piece<E, N>::load(a.w_pre + c, w);
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = w[e] * (v[i][e] * m);
+        Piece<E, N>::store(a.x + base + c, w);
+    }
+}
+
+template <typename E> struct NormGradArgs {
+    const E *r_out, *b, *w_post, *gate, *w_pre, *dr_out, *dx;
+    const float *rstd_post, *rstd_pre;
+    E *dr, *db;
+    float *part_gate, *part_post, *part_pre;          // [teams + nseg][d], [teams][d], [teams][d], or NULL
+    int32_t d, rows;                                  // rows: of a team
+    float alpha;
+    bool post;
+};
+
+// A team's rows one after the other.  SUMS: the sums over tokens are wanted.  sum_run = sum g bh of a run of rows of one segment (without
+// gates: of all rows): at its end it goes to the gate's partial sums and, times alpha gate_t, into sum_post.
+template <typename E, int N, int NT, int I, bool SUMS>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT)
+void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
+{
+    constexpr int BT = NT < 256 ? 256 : NT;
+    __shared__ float lds[2][3 * (NT / 64)];
+    const int32_t team = int32_t(blockIdx.x) * (BT / NT) + int32_t(threadIdx.x) / NT, t = threadIdx.x % NT;
+    const int64_t first = int64_t(team) * a.rows;
+    if (first >= pd.T) return;                        // (whole waves, or the whole workgroup)
+    const int32_t row0 = int32_t(first), row1 = int32_t(first + a.rows < pd.T ? first + a.rows : pd.T);
+    constexpr int IS = SUMS ? I : 1;
+    float sum_run[IS][N], sum_post[IS][N], sum_pre[IS][N];
+#pragma unroll
+    for (int i = 0; i < IS; ++i)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum_run[i][e] = sum_post[i][e] = sum_pre[i][e] = 0.f;
+    const bool gated = a.gate != nullptr;             // the rows' tasks matter
+    int32_t seg = gated ? segment_of_row(pd, row0) : 0;
+    int32_t seg_end = gated ? pd.cseg_off[seg + 1] : row1, task = gated ? pd.cseg_task[seg] : -1;
+    auto end_run = [&]() {
+        if constexpr (SUMS) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                const int32_t c = (t + i * NT) * N;
+                if (c >= a.d) continue;
+                float k[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) k[e] = 1.f;
+                if (task >= 0) Piece<E, N>::load(a.gate + size_t(task) * a.d + c, k);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (a.part_gate) a.part_gate[(size_t(team) + seg) * a.d + c + e] = sum_run[i][e];
+                    sum_post[i][e] = fmaf(a.alpha * k[e], sum_run[i][e], sum_post[i][e]);
+                    sum_run[i][e] = 0.f;
+                }
+            }
+        }
+    };
+    const float inv_d = 1.f / float(a.d);
+    for (int32_t row = row0; row < row1; ++row) {
+        if (row >= seg_end) {                         // (no segment is empty)
+            end_run();
+            ++seg;
+            seg_end = pd.cseg_off[seg + 1];
+            task = pd.cseg_task[seg];
+        }
+        const size_t base = size_t(row) * a.d;
+        const float n = a.post ? a.rstd_post[row] : 1.f, m = a.dx ? a.rstd_pre[row] : 0.f;
+        float g[I][N], rh[I][N], bh[I][N], q[I][N], dx[I][N];
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int32_t c = (t + i * NT) * N;
+            const bool in = c < a.d;
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[i][e] = rh[i][e] = bh[i][e] = dx[i][e] = 0.f;
+            if (in && a.dx) {
+                Piece<E, N>::load(a.dx + base + c, dx[i]);
+                Piece<E, N>::load(a.r_out + base + c, rh[i]);
+            }
+            if (in && a.dr_out) Piece<E, N>::load(a.dr_out + base + c, g[i]);
+            if (in && a.b) Piece<E, N>::load(a.b + base + c, bh[i]);
+        }
+        float sums[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int32_t c = (t + i * NT) * N;
+            const bool in = c < a.d;
+            float u[N], w[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) q[i][e] = a.alpha;
+            if (in && a.post) {
+                Piece<E, N>::load(a.w_post + c, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e) q[i][e] *= w[e];
+            }
+            if (in && task >= 0) {
+                Piece<E, N>::load(a.gate + size_t(task) * a.d + c, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e) q[i][e] *= w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) u[e] = 0.f;
+            if (in && a.dx) Piece<E, N>::load(a.w_pre + c, u);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                rh[i][e] *= m;
+                bh[i][e] *= n;
+                u[e] *= dx[i][e];
+                sums[0] = fmaf(u[e], rh[i][e], sums[0]);
+                g[i][e] = fmaf(m, u[e], g[i][e]);     // all of g but the mean's term
+                const float qb = q[i][e] * bh[i][e];
+                sums[1] = fmaf(qb, g[i][e], sums[1]);
+                sums[2] = fmaf(qb, rh[i][e], sums[2]);
+            }
+        }
+        team_sum<NT, 3>(sums, lds[row & 1]);
+        const float mean = sums[0] * inv_d, c1 = m * mean, c2 = (sums[1] - c1 * sums[2]) * inv_d;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int32_t c = (t + i * NT) * N;
+            if (c >= a.d) continue;
+            float out[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                g[i][e] = fmaf(-c1, rh[i][e], g[i][e]);
+                if constexpr (SUMS) {
+                    sum_run[i][e] = fmaf(g[i][e], bh[i][e], sum_run[i][e]);
+                    sum_pre[i][e] = fmaf(dx[i][e], rh[i][e], sum_pre[i][e]);
+                }
+                out[e] = q[i][e] * g[i][e];
+                if (a.post) out[e] = n * fmaf(-bh[i][e], c2, out[e]);
+            }
+            Piece<E, N>::store(a.dr + base + c, g[i]);
+            if (a.b) Piece<E, N>::store(a.db + base + c, out);
+        }
+    }
+    if constexpr (SUMS) {
+        end_run();
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int32_t c = (t + i * NT) * N;
+            if (c >= a.d) continue;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                if (a.part_post) a.part_post[size_t(team) * a.d + c + e] = sum_post[i][e];
+                if (a.part_pre) a.part_pre[size_t(team) * a.d + c + e] = sum_pre[i][e];
+            }
+        }
+    }
+}
+
+// Adds the partial sums up, in order: y = 0 and 1: the gains', over the teams; y = 2 + t: task t's gate's, over the runs of its segments
+// (segment k's runs are the teams from the one with its first row to the one with its last).  64 columns by 16 lanes of slots.
+template <typename E>
+__global__ __launch_bounds__(1024)
+void block_norm_sum_kernel(PlanDev pd, const float* __restrict__ part_gate, const float* __restrict__ part_post, const float* __restrict__ part_pre,
+                           int32_t d, int32_t teams, int32_t rows, float alpha, const E* __restrict__ w_post, float* __restrict__ dgate,
+                           float* __restrict__ dw_post, float* __restrict__ dw_pre, int accumulate)
+{
+    __shared__ float lds[16][64];
+    const int32_t col = int32_t(blockIdx.x) * 64 + (threadIdx.x & 63), lane = threadIdx.x >> 6;
+    const int32_t what = blockIdx.y;
+    float* out = what == 0 ? dw_post : what == 1 ? dw_pre : dgate;
+    if (!out) return;                                 // (uniform)
+    float s = 0.f;
+    bool any = true;
+    if (what < 2) {
+        const float* p = what == 0 ? part_post : part_pre;
+        if (col < d)
+            for (int32_t k = lane; k < teams; k += 16) s += p[size_t(k) * d + col];
+    } else {
+        any = false;
+        for (int32_t k = 0; k < pd.nseg; ++k) {
+            if (pd.cseg_task[k] != what - 2) continue;
+            any = true;
+            const int32_t w0 = pd.cseg_off[k] / rows, w1 = (pd.cseg_off[k + 1] - 1) / rows;
+            if (col < d)
+                for (int32_t w = w0 + lane; w <= w1; w += 16) s += part_gate[(size_t(w) + k) * d + col];
+        }
+        out += size_t(what - 2) * d;
+    }
+    lds[lane][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (lane != 0 || col >= d) return;
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += lds[k][threadIdx.x];
+    if (what >= 2) s *= w_post ? alpha * Elem<E>::load(w_post, size_t(col)) : alpha;
+    if (accumulate) {
+        if (any) out[col] += s;
+    } else {
+        out[col] = s;
+    }
+}
+
+// How rows are dealt to threads: a wave holds a row of up to two packets a lane; wider ones take workgroups.
+struct Deal {
+    int32_t nt, i, n;        // threads of a team, pieces of n elements per thread
+};
+Deal deal(int dtype, int32_t d)
+{
+    const int32_t per = dtype == LOBRA_F32 ? 4 : 8, n = d % per == 0 ? per : 1;
+    const int32_t pieces = (d + n - 1) / n;
+    if (n == 1) {
+        if (pieces <= 256) return {64, 4, 1};
+        if (pieces <= 2048) return {512, 4, 1};
+        if (pieces <= 4096) return {1024, 4, 1};
+        return {1024, 16, 1};
+    }
+    if (pieces <= 64) return {64, 1, n};
+    if (pieces <= 128) return {64, 2, n};
+    if (pieces <= 256) return {256, 1, n};
+    if (pieces <= 512) return {512, 1, n};
+    if (pieces <= 1024) return {1024, 1, n};
+    if (pieces <= 2048) return {1024, 2, n};
+    return {1024, 4, n};
+}
+
+// Teams of the backward kernel and their rows: some 16 waves per compute unit, and at least eight rows a team, whose sums are written
+// once (T / rows fp32 rows per sum next to T rows of six bf16 ones).
+int32_t team_rows(const Deal& dl, int64_t T)
+{
+    const int64_t teams = 4096 / (dl.nt / 64), rows = (T + teams - 1) / teams;
+    return int32_t(rows < 8 ? 8 : rows);
+}
+
+template <typename E, int N, int NT, int I> struct Launch {
+    static void fwd(const PlanDev& pd, const NormArgs<E>& a, hipStream_t st)
+    {
+        constexpr int BT = NT < 256 ? 256 : NT;
+        block_norm_fwd_kernel<E, N, NT, I><<<dim3(uint32_t((int64_t(pd.T) + BT / NT - 1) / (BT / NT))), BT, 0, st>>>(pd, a);
+    }
+    static void bwd(const PlanDev& pd, const NormGradArgs<E>& a, bool sums, int32_t teams, hipStream_t st)
+    {
+        constexpr int BT = NT < 256 ? 256 : NT;
+        const dim3 grid(uint32_t((teams + BT / NT - 1) / (BT / NT)));
+        if (sums) block_norm_bwd_kernel<E, N, NT, I, true><<<grid, BT, 0, st>>>(pd, a);
+        else block_norm_bwd_kernel<E, N, NT, I, false><<<grid, BT, 0, st>>>(pd, a);
+    }
+};
+
+// f(Launch<...>) of the deal
+template <typename E, typename F> void with_deal(const Deal& dl, F&& f)
+{
+    constexpr int N = Packet<E>::N;
+    if (dl.n == 1) {
+        if constexpr (N == 4) {                       // (bf16 widths are multiples of 8)
+            if (dl.nt == 64) f(Launch<E, 1, 64, 4>{});
+            else if (dl.nt == 512) f(Launch<E, 1, 512, 4>{});
+            else if (dl.i == 4) f(Launch<E, 1, 1024, 4>{});
+            else f(Launch<E, 1, 1024, 16>{});
+        }
+    } else if (dl.nt == 64) {
+        if (dl.i == 1) f(Launch<E, N, 64, 1>{});
+        else f(Launch<E, N, 64, 2>{});
+    } else if (dl.nt == 256) f(Launch<E, N, 256, 1>{});
+    else if (dl.nt == 512) f(Launch<E, N, 512, 1>{});
+    else if (dl.i == 1) f(Launch<E, N, 1024, 1>{});
+    else if (dl.i == 2) f(Launch<E, N, 1024, 2>{});
+    else if constexpr (N == 4) f(Launch<E, N, 1024, 4>{});
+}
+
+template <typename E>
+hipError_t fwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r, const void* b, void* r_out, void* x, float* rstd_post,
+               float* rstd_pre, hipStream_t st)
+{
+    NormArgs<E> a;
+    a.r = static_cast<const E*>(r);
+    a.b = bn.block ? static_cast<const E*>(b) : nullptr;
+    a.w_post = static_cast<const E*>(bn.w_post);
+    a.gate = bn.block ? static_cast<const E*>(bn.gate) : nullptr;
+    a.w_pre = static_cast<const E*>(bn.w_pre);
+    a.r_out = static_cast<E*>(r_out);
+    a.x = static_cast<E*>(x);
+    a.rstd_post = rstd_post;
+    a.rstd_pre = rstd_pre;
+    a.d = pd.d_in;
+    a.eps = bn.eps;
+    a.alpha = bn.alpha;
+    a.post = bn.post;
+    with_deal<E>(deal(dtype, pd.d_in), [&](auto l) { l.fwd(pd, a, st); });
+    return hipGetLastError();
+}
+
+template <typename E>
+hipError_t bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r_out, const void* b, const float* rstd_post, const float* rstd_pre,
+               const void* dr_out, const void* dx, void* dr, void* db, float* dgate, float* dw_post, float* dw_pre, bool accumulate, float* part,
+               hipStream_t st)
+{
+    const Deal dl = deal(dtype, pd.d_in);
+    const int32_t rows = team_rows(dl, pd.T), teams = int32_t((int64_t(pd.T) + rows - 1) / rows);
+    NormGradArgs<E> a;
+    a.r_out = static_cast<const E*>(r_out);
+    a.b = bn.block ? static_cast<const E*>(b) : nullptr;
+    a.w_post = static_cast<const E*>(bn.w_post);
+    a.gate = bn.block ? static_cast<const E*>(bn.gate) : nullptr;
+    a.w_pre = static_cast<const E*>(bn.w_pre);
+    a.dr_out = static_cast<const E*>(dr_out);
+    a.dx = static_cast<const E*>(dx);
+    a.rstd_post = rstd_post;
+    a.rstd_pre = rstd_pre;
+    a.dr = static_cast<E*>(dr);
+    a.db = static_cast<E*>(db);
+    const bool sums = dgate || dw_post || dw_pre;
+    const size_t row = size_t(pd.d_in);
+    a.part_gate = dgate ? part : nullptr;
+    a.part_post = dw_post ? part + size_t(teams + pd.nseg) * row : nullptr;
+    a.part_pre = dw_pre ? part + size_t(2 * size_t(teams) + pd.nseg) * row : nullptr;
+    a.d = pd.d_in;
+    a.rows = rows;
+    a.alpha = bn.alpha;
+    a.post = bn.post;
+    if (pd.T > 0) with_deal<E>(dl, [&](auto l) { l.bwd(pd, a, sums, teams, st); });
+    if (sums)
+        block_norm_sum_kernel<E><<<dim3(uint32_t((pd.d_in + 63) / 64), uint32_t(dgate ? 2 + pd.n_tasks : 2)), 1024, 0, st>>>(
+            pd, a.part_gate, a.part_post, a.part_pre, pd.d_in, teams, rows, bn.alpha, bn.post ? a.w_post : nullptr, dgate, dw_post, dw_pre,
+            accumulate ? 1 : 0);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t block_norm_part_bytes(int64_t T, int32_t d, int32_t nseg, int dtype)
+{
+    const int64_t rows = team_rows(deal(dtype, d), T), teams = (T + rows - 1) / rows;
+    return (size_t(3 * teams) + size_t(nseg)) * size_t(d) * sizeof(float);
+}
+
+hipError_t block_norm_fwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r, const void* b, void* r_out, void* x,
+                          float* rstd_post, float* rstd_pre, hipStream_t st)
+{
+    return dtype == LOBRA_F32 ? fwd<float>(pd, dtype, bn, r, b, r_out, x, rstd_post, rstd_pre, st)
+                              : fwd<uint16_t>(pd, dtype, bn, r, b, r_out, x, rstd_post, rstd_pre, st);
+}
+
+hipError_t block_norm_bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r_out, const void* b, const float* rstd_post,
+                          const float* rstd_pre, const void* dr_out, const void* dx, void* dr, void* db, float* dgate, float* dw_post,
+                          float* dw_pre, bool accumulate, float* part, hipStream_t st)
+{
+    return dtype == LOBRA_F32
+        ? bwd<float>(pd, dtype, bn, r_out, b, rstd_post, rstd_pre, dr_out, dx, dr, db, dgate, dw_post, dw_pre, accumulate, part, st)
+        : bwd<uint16_t>(pd, dtype, bn, r_out, b, rstd_post, rstd_pre, dr_out, dx, dr, db, dgate, dw_post, dw_pre, accumulate, part, st);
+}
+
+}  // namespace lobra

@@ -1,0 +1,85 @@
+// The gated feed-forward block's activation: h = a(g) u, and backward dg = dh u a'(g), du = dh a(g), of [g | u] [T][2 f].
+//     silu: a = g q, a' = q (1 + g (1 - q)) with q = 1 / (1 + exp(-g))
+//     gelu: a = g (1 + th) / 2, a' = (1 + th) / 2 + g (1 - th^2) / 2 c (1 + 3 k g^2), th = tanh(c (g + k g^3))
+// f is a multiple of 8, so that rows of all three tensors keep 16-byte packets.  Bound: memory.
+#include "activation.h"
+#include "kernels.h"
+#include "row_common.h"
+
+namespace lobra {
+
+using namespace rows;
+
+namespace {
+
+constexpr int NT = 256;
+
+// Packet k of T fp (fp packets to a row): a thread takes every stride-th, whose row and column follow without a division
+// (stride = srow fp + scol).
+template <typename E, int ACT, bool BACK>
+__global__ __launch_bounds__(NT)
+void gated_kernel(int64_t packets, int32_t fp, int64_t srow, int32_t scol, const E* gu, const E* __restrict__ dh, E* out)
+{
+    constexpr int N = Packet<E>::N;
+    const size_t f = size_t(fp) * N;
+    int64_t k = int64_t(blockIdx.x) * NT + threadIdx.x;
+    int64_t row = k / fp;
+    int32_t col = int32_t(k - row * fp);
+    for (; k < packets; k += int64_t(gridDim.x) * NT) {
+        const size_t at = size_t(row) * (2 * f) + size_t(col) * N, ah = size_t(k) * N;
+        float g[N], u[N], d[N];
+        Packet<E>::widen(*reinterpret_cast<const u32x4*>(gu + at), g);
+        Packet<E>::widen(*reinterpret_cast<const u32x4*>(gu + at + f), u);
+        if (BACK) {
+            Packet<E>::widen(*reinterpret_cast<const u32x4*>(dh + ah), d);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                float da;
+                const float a = activate<ACT>(g[e], da);
+                g[e] = d[e] * u[e] * da;
+                u[e] = d[e] * a;
+            }
+            *reinterpret_cast<u32x4*>(out + at) = Packet<E>::narrow(g);
+            *reinterpret_cast<u32x4*>(out + at + f) = Packet<E>::narrow(u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[e] = activate<ACT>(g[e]) * u[e];
+            *reinterpret_cast<u32x4*>(out + ah) = Packet<E>::narrow(g);
+        }
+        row += srow;
+        col += scol;
+        if (col >= fp) {
+            col -= fp;
+            ++row;
+        }
+    }
+}
+
+template <typename E, bool BACK>
+hipError_t launch(int act, int64_t T, int32_t f, const void* gu, const void* dh, void* out, hipStream_t st)
+{
+    const int32_t fp = f / Packet<E>::N;
+    const int64_t packets = T * fp, most = 256 * 16, blocks = (packets + NT - 1) / NT;
+    const dim3 grid(uint32_t(blocks < most ? blocks : most));
+    const int64_t stride = int64_t(grid.x) * NT, srow = stride / fp;
+    const int32_t scol = int32_t(stride - srow * fp);
+    const E *a = static_cast<const E*>(gu), *b = static_cast<const E*>(dh);
+    E* o = static_cast<E*>(out);
+    if (act == LOBRA_ACT_SILU) gated_kernel<E, LOBRA_ACT_SILU, BACK><<<grid, NT, 0, st>>>(packets, fp, srow, scol, a, b, o);
+    else gated_kernel<E, LOBRA_ACT_GELU_TANH, BACK><<<grid, NT, 0, st>>>(packets, fp, srow, scol, a, b, o);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t gated_activate(int dtype, int act, int64_t T, int32_t f, const void* gu, void* h, hipStream_t st)
+{
+    return dtype == LOBRA_F32 ? launch<float, false>(act, T, f, gu, nullptr, h, st) : launch<uint16_t, false>(act, T, f, gu, nullptr, h, st);
+}
+
+hipError_t gated_derive(int dtype, int act, int64_t T, int32_t f, const void* gu, const void* dh, void* dgu, hipStream_t st)
+{
+    return dtype == LOBRA_F32 ? launch<float, true>(act, T, f, gu, dh, dgu, st) : launch<uint16_t, true>(act, T, f, gu, dh, dgu, st);
+}
+
+}  // namespace lobra

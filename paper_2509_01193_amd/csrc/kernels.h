@@ -125,6 +125,51 @@ hipError_t adam_step(const PlanDev& pd, int dtype, float beta1, float beta2, flo
                      const float* lr, const int32_t* step, const float* grad_scale,
                      const AdamTensor& ta, const AdamTensor& tb, hipStream_t st);
 
+// ---- the rest of a training step around the linears ------------------------------------------------------------------------
+// Log probabilities and their gradient (logprob.hip): lobra_token_logprob_fwd / _bwd with checked arguments (T > 0, ld >= V).
+struct LogprobShape {
+    int32_t dtype, V, top_k;
+    int64_t T, ld;
+};
+struct LogprobOut {
+    float *logp, *lse, *lse_rest, *entropy, *top_logp;
+    int32_t* top_id;
+};
+struct LogprobGrad {
+    const float *lse, *lse_rest, *entropy, *dlogp, *dentropy;
+};
+hipError_t logprob_fwd(const LogprobShape& s, const void* logits, const int32_t* target, const LogprobOut& out, hipStream_t st);
+hipError_t logprob_bwd(const LogprobShape& s, const void* logits, const int32_t* target, const LogprobGrad& in, void* dlogits, hipStream_t st);
+
+// Gradient norms and clipping (grad_clip.hip) over a set's pieces, which are grouped by task: those of task t are
+// task_piece[t] .. task_piece[t + 1] - 1.  partial [pieces] fp64.
+struct GradPiece {
+    const float* grad;
+    float* out;              // or NULL
+    int32_t n, task;
+};
+hipError_t grad_clip(const GradPiece* pieces, const int32_t* task_piece, int32_t n_pieces, int32_t n_tasks, bool any_out, const float* max_norm,
+                     const float* grad_scale, const int32_t* step, float* norm, float* clip_scale, int32_t* step_out, bool joint,
+                     double* partial, float* scale, hipStream_t st);
+
+// The norms around a residual block (block_norm.hip); arguments as lobra_mlora_block_norm_fwd / _bwd, checked.
+struct BlockNorm {
+    float eps, alpha;
+    const void *w_post, *gate, *w_pre;
+    bool post, block;        // the block's output is normed; there is a block's output
+};
+hipError_t block_norm_fwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r, const void* b, void* r_out, void* x,
+                          float* rstd_post, float* rstd_pre, hipStream_t st);
+// part: block_norm_part_bytes
+size_t block_norm_part_bytes(int64_t T, int32_t d, int32_t nseg, int dtype);
+hipError_t block_norm_bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r_out, const void* b, const float* rstd_post,
+                          const float* rstd_pre, const void* dr_out, const void* dx, void* dr, void* db, float* dgate, float* dw_post,
+                          float* dw_pre, bool accumulate, float* part, hipStream_t st);
+
+// h = a(g) u of [g | u] [T][2 f], and [dg | du] from dh (gated.hip).
+hipError_t gated_activate(int dtype, int act, int64_t T, int32_t f, const void* gu, void* h, hipStream_t st);
+hipError_t gated_derive(int dtype, int act, int64_t T, int32_t f, const void* gu, const void* dh, void* dgu, hipStream_t st);
+
 hipError_t token_task_map(const PlanDev& pd, int32_t* out_task, int64_t* out_count, hipStream_t st);
 
 }  // namespace lobra
