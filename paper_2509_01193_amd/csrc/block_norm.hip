@@ -20,13 +20,23 @@ using namespace rows;
 
 namespace {
 
-// N consecutive elements of E: a 16-byte packet, or a single element where rows keep no such alignment.
+// N consecutive elements of E: a 16-byte packet, or a single element where rows keep no such alignment.  Raw: as they are in memory.
 template <typename E, int N> struct Piece {
-    static __device__ __forceinline__ void load(const E* p, float (&v)[N]) { Packet<E>::widen(*reinterpret_cast<const u32x4*>(p), v); }
+    typedef u32x4 Raw;
+    static __device__ __forceinline__ Raw fetch(const E* p) { return *reinterpret_cast<const u32x4*>(p); }
+    static __device__ __forceinline__ void widen(Raw r, float (&v)[N]) { Packet<E>::widen(r, v); }
+    static __device__ __forceinline__ float widen(Raw r, int i) { return Packet<E>::element(r, i); }
+    static __device__ __forceinline__ Raw zero() { return u32x4{0u, 0u, 0u, 0u}; }
+    static __device__ __forceinline__ void load(const E* p, float (&v)[N]) { widen(fetch(p), v); }
     static __device__ __forceinline__ void store(E* p, const float (&v)[N]) { *reinterpret_cast<u32x4*>(p) = Packet<E>::narrow(v); }
 };
 template <typename E> struct Piece<E, 1> {
-    static __device__ __forceinline__ void load(const E* p, float (&v)[1]) { v[0] = Elem<E>::load(p, 0); }
+    typedef E Raw;
+    static __device__ __forceinline__ Raw fetch(const E* p) { return *p; }
+    static __device__ __forceinline__ void widen(Raw r, float (&v)[1]) { v[0] = Elem<E>::load(&r, 0); }
+    static __device__ __forceinline__ float widen(Raw r, int) { return Elem<E>::load(&r, 0); }
+    static __device__ __forceinline__ Raw zero() { return E(0); }
+    static __device__ __forceinline__ void load(const E* p, float (&v)[1]) { widen(fetch(p), v); }
     static __device__ __forceinline__ void store(E* p, const float (&v)[1]) { Elem<E>::store(p, 0, v[0]); }
 };
 // v as the element type holds it
@@ -45,12 +55,9 @@ template <int NT, int K> __device__ __forceinline__ void team_sum(float (&v)[K],
 #pragma unroll
             for (int k = 0; k < K; ++k) lds[w * K + k] = v[k];
         __syncthreads();
+        const int o = threadIdx.x & 15;               // (up to 16 waves: a wave's sum per lane of a row of 16)
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            v[k] = 0.f;
-#pragma unroll
-            for (int o = 0; o < NT / 64; ++o) v[k] += lds[o * K + k];
-        }
+        for (int k = 0; k < K; ++k) v[k] = row_sum(o < NT / 64 ? lds[o * K + k] : 0.f);
     }
 }
 
@@ -73,7 +80,7 @@ void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a)
 {
     constexpr int BT = NT < 256 ? 256 : NT;
     __shared__ float lds[2][NT / 64];
-    const int32_t row = int32_t(blockIdx.x) * (BT / NT) + int32_t(threadIdx.x) / NT, t = threadIdx.x % NT;
+    const int32_t row = xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x)) * (BT / NT) + int32_t(threadIdx.x) / NT, t = threadIdx.x % NT;
     if (row >= pd.T) return;                          // (whole waves; with NT > 64 a workgroup has one row)
     const size_t base = size_t(row) * a.d;
     float v[I][N], bv[I][N];
@@ -160,12 +167,12 @@ template <typename E> struct NormGradArgs {
 // A team's rows one after the other.  SUMS: the sums over tokens are wanted.  sum_run = sum g bh of a run of rows of one segment (without
 // gates: of all rows): at its end it goes to the gate's partial sums and, times alpha gate_t, into sum_post.
 template <typename E, int N, int NT, int I, bool SUMS>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT)
+__global__ __launch_bounds__(NT < 256 ? 256 : NT, I * N <= 8 ? 4 : 1)
 void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
 {
     constexpr int BT = NT < 256 ? 256 : NT;
     __shared__ float lds[2][3 * (NT / 64)];
-    const int32_t team = int32_t(blockIdx.x) * (BT / NT) + int32_t(threadIdx.x) / NT, t = threadIdx.x % NT;
+    const int32_t team = xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x)) * (BT / NT) + int32_t(threadIdx.x) / NT, t = threadIdx.x % NT;
     const int64_t first = int64_t(team) * a.rows;
     if (first >= pd.T) return;                        // (whole waves, or the whole workgroup)
     const int32_t row0 = int32_t(first), row1 = int32_t(first + a.rows < pd.T ? first + a.rows : pd.T);
@@ -178,6 +185,9 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
     const bool gated = a.gate != nullptr;             // the rows' tasks matter
     int32_t seg = gated ? segment_of_row(pd, row0) : 0;
     int32_t seg_end = gated ? pd.cseg_off[seg + 1] : row1, task = gated ? pd.cseg_task[seg] : -1;
+    // gains and the task's gate stay in registers as they are in memory, and a row is fetched while the one before is worked on
+    typedef Piece<E, N> P;
+    typename P::Raw w_post[I], w_pre[I], w_gate[I];
     auto end_run = [&]() {
         if constexpr (SUMS) {
 #pragma unroll
@@ -185,11 +195,10 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
                 const int32_t c = (t + i * NT) * N;
                 if (c >= a.d) continue;
                 float k[N];
-#pragma unroll
-                for (int e = 0; e < N; ++e) k[e] = 1.f;
-                if (task >= 0) Piece<E, N>::load(a.gate + size_t(task) * a.d + c, k);
+                Piece<E, N>::widen(w_gate[i], k);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
+                    if (task < 0) k[e] = 1.f;
                     if (a.part_gate) a.part_gate[(size_t(team) + seg) * a.d + c + e] = sum_run[i][e];
                     sum_post[i][e] = fmaf(a.alpha * k[e], sum_run[i][e], sum_post[i][e]);
                     sum_run[i][e] = 0.f;
@@ -197,6 +206,57 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
             }
         }
     };
+    struct Row {
+        typename P::Raw dx[I], r[I], dr[I], b[I];
+        float n, m;
+    };
+    auto fetch_gate = [&]() {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int32_t c = (t + i * NT) * N;
+            w_gate[i] = c < a.d && task >= 0 ? P::fetch(a.gate + size_t(task) * a.d + c) : P::zero();
+        }
+    };
+    auto fetch_row = [&](Row& f, int32_t row) {
+        const size_t base = size_t(row) * a.d;
+        f.n = a.post ? a.rstd_post[row] : 1.f;
+        f.m = a.dx ? a.rstd_pre[row] : 0.f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int32_t c = (t + i * NT) * N;
+            const bool in = c < a.d;
+            f.dx[i] = in && a.dx ? P::fetch(a.dx + base + c) : P::zero();
+            f.r[i] = in && a.dx ? P::fetch(a.r_out + base + c) : P::zero();
+            f.dr[i] = in && a.dr_out ? P::fetch(a.dr_out + base + c) : P::zero();
+            f.b[i] = in && a.b ? P::fetch(a.b + base + c) : P::zero();
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int32_t c = (t + i * NT) * N;
+        w_post[i] = c < a.d && a.post ? P::fetch(a.w_post + c) : P::zero();
+        w_pre[i] = c < a.d && a.dx ? P::fetch(a.w_pre + c) : P::zero();
+    }
+    fetch_gate();
+    // an element's terms, from how they are in memory: g without the term of its mean
+    struct Terms {
+        float dx, rh, bh, q, u, g;
+    };
+    auto expand = [&](const Row& f, int i, int e) __attribute__((always_inline)) {
+        Terms k;
+        k.dx = P::widen(f.dx[i], e);
+        k.rh = f.m * P::widen(f.r[i], e);
+        k.bh = f.n * P::widen(f.b[i], e);
+        k.u = P::widen(w_pre[i], e) * k.dx;
+        k.g = fmaf(f.m, k.u, P::widen(f.dr[i], e));
+        k.q = a.alpha;
+        if (a.post) k.q *= P::widen(w_post[i], e);
+        if (task >= 0) k.q *= P::widen(w_gate[i], e);
+        return k;
+    };
+    constexpr bool AHEAD = I * int(sizeof(typename P::Raw)) <= 16;       // (the next row does not fit next to larger ones)
+    Row cur, next;
+    fetch_row(cur, row0);
     const float inv_d = 1.f / float(a.d);
     for (int32_t row = row0; row < row1; ++row) {
         if (row >= seg_end) {                         // (no segment is empty)
@@ -204,76 +264,50 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
             ++seg;
             seg_end = pd.cseg_off[seg + 1];
             task = pd.cseg_task[seg];
+            fetch_gate();
         }
-        const size_t base = size_t(row) * a.d;
-        const float n = a.post ? a.rstd_post[row] : 1.f, m = a.dx ? a.rstd_pre[row] : 0.f;
-        float g[I][N], rh[I][N], bh[I][N], q[I][N], dx[I][N];
-#pragma unroll
-        for (int i = 0; i < I; ++i) {
-            const int32_t c = (t + i * NT) * N;
-            const bool in = c < a.d;
-#pragma unroll
-            for (int e = 0; e < N; ++e) g[i][e] = rh[i][e] = bh[i][e] = dx[i][e] = 0.f;
-            if (in && a.dx) {
-                Piece<E, N>::load(a.dx + base + c, dx[i]);
-                Piece<E, N>::load(a.r_out + base + c, rh[i]);
-            }
-            if (in && a.dr_out) Piece<E, N>::load(a.dr_out + base + c, g[i]);
-            if (in && a.b) Piece<E, N>::load(a.b + base + c, bh[i]);
-        }
+        if (AHEAD && row + 1 < row1) fetch_row(next, row + 1);
         float sums[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int32_t c = (t + i * NT) * N;
-            const bool in = c < a.d;
-            float u[N], w[N];
-#pragma unroll
-            for (int e = 0; e < N; ++e) q[i][e] = a.alpha;
-            if (in && a.post) {
-                Piece<E, N>::load(a.w_post + c, w);
-#pragma unroll
-                for (int e = 0; e < N; ++e) q[i][e] *= w[e];
-            }
-            if (in && task >= 0) {
-                Piece<E, N>::load(a.gate + size_t(task) * a.d + c, w);
-#pragma unroll
-                for (int e = 0; e < N; ++e) q[i][e] *= w[e];
-            }
-#pragma unroll
-            for (int e = 0; e < N; ++e) u[e] = 0.f;
-            if (in && a.dx) Piece<E, N>::load(a.w_pre + c, u);
+            asm volatile("" : "+v"(w_post[i]), "+v"(w_pre[i]), "+v"(w_gate[i]));        // (they are not widened in front of the loop)
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                rh[i][e] *= m;
-                bh[i][e] *= n;
-                u[e] *= dx[i][e];
-                sums[0] = fmaf(u[e], rh[i][e], sums[0]);
-                g[i][e] = fmaf(m, u[e], g[i][e]);     // all of g but the mean's term
-                const float qb = q[i][e] * bh[i][e];
-                sums[1] = fmaf(qb, g[i][e], sums[1]);
-                sums[2] = fmaf(qb, rh[i][e], sums[2]);
+                const Terms k = expand(cur, i, e);
+                const float qb = k.q * k.bh;
+                sums[0] = fmaf(k.u, k.rh, sums[0]);
+                sums[1] = fmaf(qb, k.g, sums[1]);
+                sums[2] = fmaf(qb, k.rh, sums[2]);
             }
         }
         team_sum<NT, 3>(sums, lds[row & 1]);
-        const float mean = sums[0] * inv_d, c1 = m * mean, c2 = (sums[1] - c1 * sums[2]) * inv_d;
+        const float mean = sums[0] * inv_d, c1 = cur.m * mean, c2 = (sums[1] - c1 * sums[2]) * inv_d;
+        const size_t base = size_t(row) * a.d;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int32_t c = (t + i * NT) * N;
-            if (c >= a.d) continue;
-            float out[N];
+            // (opaque to the optimiser: the terms are worked out once more instead of waiting in 48 registers for the sums, which would
+            //  halve the waves of a compute unit)
+            asm volatile("" : "+v"(cur.dx[i]), "+v"(cur.r[i]), "+v"(cur.dr[i]), "+v"(cur.b[i]), "+v"(w_post[i]), "+v"(w_pre[i]), "+v"(w_gate[i]));
+            float g[N], out[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                g[i][e] = fmaf(-c1, rh[i][e], g[i][e]);
+                const Terms k = expand(cur, i, e);
+                g[e] = fmaf(-c1, k.rh, k.g);
                 if constexpr (SUMS) {
-                    sum_run[i][e] = fmaf(g[i][e], bh[i][e], sum_run[i][e]);
-                    sum_pre[i][e] = fmaf(dx[i][e], rh[i][e], sum_pre[i][e]);
+                    sum_run[i][e] = fmaf(g[e], k.bh, sum_run[i][e]);
+                    sum_pre[i][e] = fmaf(k.dx, k.rh, sum_pre[i][e]);
                 }
-                out[e] = q[i][e] * g[i][e];
-                if (a.post) out[e] = n * fmaf(-bh[i][e], c2, out[e]);
+                out[e] = k.q * g[e];
+                if (a.post) out[e] = cur.n * fmaf(-k.bh, c2, out[e]);
             }
-            Piece<E, N>::store(a.dr + base + c, g[i]);
-            if (a.b) Piece<E, N>::store(a.db + base + c, out);
+            if (c < a.d) {
+                P::store(a.dr + base + c, g);
+                if (a.b) P::store(a.db + base + c, out);
+            }
         }
+        if (AHEAD) cur = next;
+        else if (row + 1 < row1) fetch_row(cur, row + 1);
     }
     if constexpr (SUMS) {
         end_run();

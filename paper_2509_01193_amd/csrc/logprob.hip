@@ -39,6 +39,7 @@ template <bool ENT> __device__ __forceinline__ void rescale(Stat& a, float m)
     a.m = m;
 }
 
+// (the more elements at a time, the less often m grows: nearly every time some lane's does)
 template <bool ENT, int N> __device__ __forceinline__ void take(Stat& a, const float (&z)[N])
 {
     float c = z[0];
@@ -56,6 +57,55 @@ template <bool ENT, int N> __device__ __forceinline__ void take(Stat& a, const f
 }
 
 template <typename E> __device__ __forceinline__ float element(const E* p, int32_t i) { return Elem<E>::load(p, size_t(i)); }
+
+// A packet of -inf, which adds nothing.
+template <typename E> __device__ __forceinline__ u32x4 nothing()
+{
+    const uint32_t w = sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;
+    return u32x4{w, w, w, w};
+}
+
+// The statistics of the elements that this thread looks at: batches of U packets, the next one on its way while one is worked on, the
+// last one filled up with -inf.  (One by one, what is left behind the whole batches - up to a quarter of a row - would wait for memory U
+// times more.)
+template <typename E, int NT, bool ENT> __device__ __forceinline__ Stat row_stat(const E* row, const RowShape& sh)
+{
+    constexpr int N = Packet<E>::N, U = 4;
+    Stat a{-INFINITY, 0.f, 0.f};
+    const u32x4* p = reinterpret_cast<const u32x4*>(row + sh.head);
+    const int32_t t = threadIdx.x;
+    auto fetch = [&](u32x4 (&q)[U], int32_t first) {
+        if (first + U * NT <= sh.packets) {           // (uniform)
+#pragma unroll
+            for (int c = 0; c < U; ++c) q[c] = p[first + c * NT + t];
+        } else {
+#pragma unroll
+            for (int c = 0; c < U; ++c) q[c] = first + c * NT + t < sh.packets ? p[first + c * NT + t] : nothing<E>();
+        }
+    };
+    u32x4 q[U], next[U];
+    if (sh.packets > 0) fetch(q, 0);
+    // the elements in front of the first packet and behind the last one: fewer than 2 N, a thread each
+    const bool has_edge = t < sh.head + sh.tail;
+    E edge = E(0);
+    if (has_edge) edge = row[t < sh.head ? t : t + sh.packets * N];
+    for (int32_t first = 0; first < sh.packets; first += U * NT) {
+        if (first + U * NT < sh.packets) fetch(next, first + U * NT);
+        float z[U * N];
+#pragma unroll
+        for (int c = 0; c < U; ++c)
+#pragma unroll
+            for (int e = 0; e < N; ++e) z[c * N + e] = Packet<E>::element(q[c], e);
+        take<ENT>(a, z);
+#pragma unroll
+        for (int c = 0; c < U; ++c) q[c] = next[c];
+    }
+    if (has_edge) {
+        const float z[1] = {Elem<E>::load(&edge, 0)};
+        take<ENT>(a, z);
+    }
+    return a;
+}
 
 // f(first index, values) over the elements of the row that this thread looks at, in ascending order of index within the whole packets
 template <typename E, int NT, typename F> __device__ __forceinline__ void each(const E* row, const RowShape& sh, F&& f)
@@ -102,10 +152,11 @@ __device__ __forceinline__ float key_value(uint64_t key)
 __device__ __forceinline__ int32_t key_index(uint64_t key) { return int32_t(~uint32_t(key)); }
 
 // The top_k largest of a row, all of whose threads know m and ln S.
-// 64 groups of threads have a maximum each; the top_k-th largest of these, tau, has at least top_k logits at or above it, and only
-// threads that have seen one of those look at their part of the row again (it is in the caches) and put what is not below tau on a
-// list, whose members find their place by counting who is larger.  Rows with more candidates than the list holds (thousands of equal
-// logits) take the largest top_k times over.
+// 64 groups of threads have a maximum each; the top_k-th largest of these, tau, has at least top_k logits at or above it, and what is
+// not below tau was seen by a few threads only.  All threads together look at these threads' packets again (they are in the caches) and
+// put what is not below tau on a list, whose members find their place by counting who is larger.  (Each thread looking at its own packets
+// again keeps its wave busy with nearly the whole row: 4096 x 128000, 8 alternatives, 250 us instead of 188.)  Rows with more
+// candidates than the list holds (thousands of equal logits) take the largest top_k times over.
 template <typename E, int NT>
 __device__ void alternatives(const E* row, const RowShape& sh, int32_t V, float mine, float m, float ln_s, int32_t k, float* top_logp,
                              int32_t* top_id)
@@ -113,23 +164,24 @@ __device__ void alternatives(const E* row, const RowShape& sh, int32_t V, float 
     __shared__ uint64_t list[kCandidates];
     __shared__ float group_max[64];
     __shared__ float tau_s;
-    __shared__ int32_t count;
+    __shared__ int32_t count, seers;
+    __shared__ int32_t seer[NT];
     constexpr int G = NT / 64;
     const int32_t tid = threadIdx.x, lane = tid & 63;
     float g = mine;
 #pragma unroll
     for (int x = 1; x < G; x <<= 1) g = fmaxf(g, __shfl_xor(g, x));
     if (tid % G == 0) group_max[tid / G] = g;
-    if (tid == 0) count = 0;
+    if (tid == 0) count = seers = 0;
     __syncthreads();
     if (tid < 64) {
-        const float own = group_max[lane];
-        int32_t rank = 0;
-        for (int o = 0; o < 64; ++o) {
-            const float other = group_max[o];
-            rank += (other > own || (other == own && o < lane)) ? 1 : 0;
+        // (a short loop: code that runs once is fetched about as slowly as it is long)
+        float v = group_max[lane], m = 0.f;
+        for (int32_t r = 0; r < k; ++r) {
+            m = wave_max(v);
+            v = lane == __builtin_ctzll(__ballot(v == m)) ? -INFINITY : v;
         }
-        if (rank == k - 1) tau_s = own;
+        if (lane == 0) tau_s = m;
     }
     __syncthreads();
     const float tau = tau_s;
@@ -138,15 +190,35 @@ __device__ void alternatives(const E* row, const RowShape& sh, int32_t V, float 
         if (top_logp) top_logp[place] = m == -INFINITY ? -INFINITY : (v - m) - ln_s;
         if (top_id) top_id[place] = key_index(key);
     };
-    if (mine >= tau && mine > -INFINITY)
-        each<E, NT>(row, sh, [&](int32_t at, const auto& z) {
+    if (mine >= tau && mine > -INFINITY) seer[atomicAdd(&seers, 1)] = tid;
+    __syncthreads();
+    auto consider = [&](float z, int32_t at) {
+        if (z >= tau && z > -INFINITY) {
+            const int32_t n = atomicAdd(&count, 1);
+            if (n < kCandidates) list[n] = order_key(z, at);
+        }
+    };
+    {
+        constexpr int N = Packet<E>::N;
+        const u32x4* p = reinterpret_cast<const u32x4*>(row + sh.head);
+        const int32_t of = seers, total = of * ((sh.packets + NT - 1) / NT);
+        for (int32_t j = tid; j < total; j += NT) {
+            const int32_t step = j / of, i = step * NT + seer[j - step * of];
+            if (i >= sh.packets) continue;
+            const u32x4 q = p[i];
+            uint32_t hits = 0;
 #pragma unroll
-            for (int i = 0; i < int(sizeof(z) / sizeof(float)); ++i)
-                if (z[i] >= tau && z[i] > -INFINITY) {
-                    const int32_t n = atomicAdd(&count, 1);
-                    if (n < kCandidates) list[n] = order_key(z[i], at + i);
-                }
-        });
+            for (int e = 0; e < N; ++e) hits |= Packet<E>::element(q, e) >= tau ? 1u << e : 0u;
+            for (; hits; hits &= hits - 1) {
+                const int32_t at = sh.head + i * N + __builtin_ctz(hits);
+                consider(element(row, at), at);
+            }
+        }
+        if (tid < sh.head + sh.tail) {
+            const int32_t at = tid < sh.head ? tid : tid + sh.packets * N;
+            consider(element(row, at), at);
+        }
+    }
     __syncthreads();
     const int32_t n = count;
     int32_t filled = min(n, k);
@@ -154,6 +226,7 @@ __device__ void alternatives(const E* row, const RowShape& sh, int32_t V, float 
         for (int32_t c = tid; c < n; c += NT) {
             const uint64_t key = list[c];
             int32_t rank = 0;
+#pragma unroll 4
             for (int32_t o = 0; o < n; ++o) rank += list[o] > key ? 1 : 0;
             if (rank < k) write(rank, key);
         }
@@ -204,15 +277,14 @@ __global__ __launch_bounds__(NT)
 void logprob_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, const int32_t* __restrict__ target, LogprobOut out, int32_t top_k)
 {
     __shared__ Stat part[NT / 64];
-    const size_t r = blockIdx.x;
+    const size_t r = size_t(xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x)));
     const E* row = logits + r * size_t(ld);
     const RowShape sh = row_shape(row, V);
     const int32_t tid = threadIdx.x;
     const int32_t tgt = target ? target[r] : -1;
     const bool has = tgt >= 0 && tgt < V;
+    Stat a = row_stat<E, NT, ENT>(row, sh);
     const float zt = has ? element(row, tgt) : 0.f;
-    Stat a{-INFINITY, 0.f, 0.f};
-    each<E, NT>(row, sh, [&](int32_t, const auto& z) { take<ENT>(a, z); });
     const float mine = a.m;
     rescale<ENT>(a, wave_max(a.m));
     a.s = wave_sum(a.s);
@@ -250,7 +322,7 @@ __global__ __launch_bounds__(NT)
 void logprob_bwd_kernel(const E* logits, int64_t ld, int32_t V, const int32_t* __restrict__ target, LogprobGrad in, E* dlogits)
 {
     constexpr int N = Packet<E>::N;
-    const size_t r = blockIdx.x;
+    const size_t r = size_t(xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x)));
     const E* row = logits + r * size_t(ld);
     E* out = dlogits + r * size_t(ld);
     const RowShape sh = row_shape(row, V);            // (logits and dlogits are aligned alike: both bases to 16 bytes)
@@ -296,14 +368,20 @@ void launch_fwd(const LogprobShape& s, const E* logits, const int32_t* target, c
 
 template <typename E> hipError_t fwd(const LogprobShape& s, const E* logits, const int32_t* target, const LogprobOut& out, hipStream_t st)
 {
-    // few rows: as many threads to a row as there are
-    const bool wide = s.T <= 512 && s.V >= 8192;
+    // four to eight packets a thread: more threads than that wait for each other at a row's end longer than they read, fewer have too little
+    // on the way (forward alone, us, with 64 / 128 / 256 / 512 threads: 16000 x 1000 10 / 15 / 25 / 47, x 4000 25 / 24 / 32 / 62, 8000 x
+    // 16000 50 / 48 / 45 / 45, 4096 x 128000 with 8 alternatives 315 / 261 / 214 / 195, 1 x 32000 with 20 28 / 16 / 11 / 9.5)
+    const int32_t packets = s.V / Packet<E>::N;
     if (out.entropy) {
-        if (wide) launch_fwd<E, 1024, true>(s, logits, target, out, st);
-        else launch_fwd<E, 256, true>(s, logits, target, out, st);
+        if (packets <= 256) launch_fwd<E, 64, true>(s, logits, target, out, st);
+        else if (packets <= 512) launch_fwd<E, 128, true>(s, logits, target, out, st);
+        else if (packets <= 2048) launch_fwd<E, 256, true>(s, logits, target, out, st);
+        else launch_fwd<E, 512, true>(s, logits, target, out, st);
     } else {
-        if (wide) launch_fwd<E, 1024, false>(s, logits, target, out, st);
-        else launch_fwd<E, 256, false>(s, logits, target, out, st);
+        if (packets <= 256) launch_fwd<E, 64, false>(s, logits, target, out, st);
+        else if (packets <= 512) launch_fwd<E, 128, false>(s, logits, target, out, st);
+        else if (packets <= 2048) launch_fwd<E, 256, false>(s, logits, target, out, st);
+        else launch_fwd<E, 512, false>(s, logits, target, out, st);
     }
     return hipGetLastError();
 }

@@ -17,6 +17,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 template <typename E> struct Packet;
 template <> struct Packet<float> {
     static constexpr int N = 4;
+    static __device__ __forceinline__ float element(u32x4 p, int i) { return __uint_as_float(p[i]); }
     static __device__ __forceinline__ void widen(u32x4 p, float (&v)[N])
     {
 #pragma unroll
@@ -32,6 +33,7 @@ template <> struct Packet<float> {
 };
 template <> struct Packet<uint16_t> {
     static constexpr int N = 8;
+    static __device__ __forceinline__ float element(u32x4 p, int i) { return __uint_as_float(i & 1 ? p[i >> 1] & 0xffff0000u : p[i >> 1] << 16); }
     static __device__ __forceinline__ void widen(u32x4 p, float (&v)[N])
     {
 #pragma unroll
@@ -49,18 +51,39 @@ template <> struct Packet<uint16_t> {
     }
 };
 
+// Joins of a value over the 64 lanes of a wave, the result in all of them: along the rows of 16 lanes, then row 0 into 1 and 2 into 3,
+// then 1 into 2 and 3.  Data-parallel moves take a few cycles each, where a shuffle goes through the LDS unit.  Every lane has to be
+// active.  `none`: what joins without effect.
+template <int CTRL, int ROWS> __device__ __forceinline__ float lanes_moved(float v, float none)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+template <typename F> __device__ __forceinline__ float wave_join(float v, float none, F&& f)
+{
+    v = f(v, lanes_moved<0x111, 0xf>(v, none));      // row_shr 1, 2, 4, 8
+    v = f(v, lanes_moved<0x112, 0xf>(v, none));
+    v = f(v, lanes_moved<0x114, 0xf>(v, none));
+    v = f(v, lanes_moved<0x118, 0xf>(v, none));
+    v = f(v, lanes_moved<0x142, 0xa>(v, none));      // row_bcast 15: lane 15 of a row to the next one
+    v = f(v, lanes_moved<0x143, 0xc>(v, none));      // row_bcast 31
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+// The sum of the first 16 lanes, in all lanes.
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += lanes_moved<0x111, 0xf>(v, 0.f);
+    v += lanes_moved<0x112, 0xf>(v, 0.f);
+    v += lanes_moved<0x114, 0xf>(v, 0.f);
+    v += lanes_moved<0x118, 0xf>(v, 0.f);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 15));
+}
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-    return v;
+    return wave_join(v, 0.f, [](float a, float b) { return a + b; });
 }
-
 __device__ __forceinline__ float wave_max(float v)
 {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-    return v;
+    return wave_join(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // A row of n elements that may start anywhere: `head` elements up to the first 16-byte boundary, `packets` whole packets, `tail`
