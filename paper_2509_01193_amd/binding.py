@@ -190,12 +190,10 @@ def validate(desc: Desc) -> int:
 
 
 def _ptr(t):
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return ctypes.c_void_p(t)
+    if t is None or isinstance(t, int):
+        return t
     assert t.is_contiguous(), "tensors must be contiguous"
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream(stream):
@@ -406,13 +404,14 @@ def make_logprob_desc(dtype, T, V, ld=0, top_k=0) -> LogprobDesc:
 def _rows_ptr(t, desc: LogprobDesc):
     """A [T, V] tensor of the descriptor's type whose rows are ld elements apart (a slice of wider rows, for one)."""
     if t is None or isinstance(t, int):
-        return _ptr(t)
-    import torch
-    assert t.dtype == (torch.float32 if desc.dtype == F32 else torch.bfloat16), "logits of another type than the descriptor's"
-    assert tuple(t.shape) == (desc.T, desc.V), "logits of another shape than the descriptor's"
-    assert desc.T <= 1 or t.stride(0) == (desc.ld or desc.V), "rows of logits are not ld elements apart"
-    assert desc.V <= 1 or t.stride(1) == 1, "rows of logits must be contiguous"
-    return ctypes.c_void_p(t.data_ptr())
+        return t
+    T, V = t.shape
+    ld, one = t.stride()
+    assert t.element_size() == (4 if desc.dtype == F32 else 2) and t.is_floating_point(), "logits of another type than the descriptor's"
+    assert T == desc.T and V == desc.V, "logits of another shape than the descriptor's"
+    assert T <= 1 or ld == (desc.ld or V), "rows of logits are not ld elements apart"
+    assert V <= 1 or one == 1, "rows of logits must be contiguous"
+    return t.data_ptr()
 
 
 def lobra_token_logprob_fwd(desc: LogprobDesc, logits, target, logp=None, lse=None, lse_rest=None, entropy=None, top_logp=None, top_id=None,

@@ -33,6 +33,10 @@ size_t gated_scratch(const Plan& p)
     return align256(size_t(p.desc.T) * size_t(p.desc.d_out) * (p.desc.dtype == LOBRA_F32 ? 4 : 2));
 }
 
+// Few tokens (decoding) have kernels of their own, which keep no projected activations.
+bool gated_is_skinny(const Plan& p) { return p.mfma && p.desc.T > 0 && p.desc.T <= kSkinnyTokens; }
+size_t gated_skinny_bytes(const Plan& p) { return gated_skinny_ws_bytes(p.desc.T, p.desc.d_in, p.dg, p.tb.empty() ? 0 : p.r_max); }
+
 // ---- norms ----------------------------------------------------------------------------------------------------------------
 
 lobra_status block_norm_check(const Plan& p, const lobra_block_norm_config* cfg)
@@ -147,6 +151,7 @@ lobra_status lobra_mlora_gated_workspace_bytes(const lobra_mlora_plan* plan, int
     if (!fwd_bytes) return LOBRA_ERR_NULL;
     if (plan->n_proj != 2) return LOBRA_ERR_SHAPE;
     *fwd_bytes = (save_gu ? 0 : gated_scratch(*plan)) + plan->fwd_ws_bytes;
+    if (gated_is_skinny(*plan)) *fwd_bytes = std::max(*fwd_bytes, gated_skinny_bytes(*plan));
     return LOBRA_OK;
 }
 
@@ -160,12 +165,23 @@ lobra_status lobra_mlora_gated_fwd(const lobra_mlora_plan* plan, int32_t act, co
     if (p.desc.T == 0) return LOBRA_OK;
     if (!h) return LOBRA_ERR_NULL;
     if (!aligned16(h) || !aligned16(gu) || !aligned16(ws)) return LOBRA_ERR_ALIGN;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const bool adapters = !p.tb.empty();
+    if (gated_is_skinny(p) && !h_save) {
+        if (!x || !W || (adapters && (!A || !B || !s))) return LOBRA_ERR_NULL;
+        if (!aligned16(x) || !aligned16(W) || !aligned16(A) || !aligned16(B)) return LOBRA_ERR_ALIGN;
+        if (!ws || ws_bytes < gated_skinny_bytes(p)) return LOBRA_ERR_WORKSPACE;
+        PlanDev pd = device_view(p);
+        if (!adapters) pd.r_max = 0;
+        LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK_GEMM, gated_skinny_product(pd, x, W, A, s, ws, adapters, st));
+        LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_skinny_finish(pd, act, B, ws, adapters, gu, h, st));
+        return LOBRA_OK;
+    }
     const size_t own = gu ? 0 : gated_scratch(p);
     if (own > 0 && (!ws || ws_bytes < own)) return LOBRA_ERR_WORKSPACE;
     void* const y = gu ? gu : ws;
     char* const rest = ws ? static_cast<char*>(ws) + own : nullptr;
     if ((rs = lobra_mlora_plan_fwd(plan, x, W, A, B, s, y, h_save, rest, ws_bytes - own, hip_stream)) != LOBRA_OK) return rs;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
     LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_activate(p.desc.dtype, act, p.desc.T, p.dg, y, h, st));
     return LOBRA_OK;
 }

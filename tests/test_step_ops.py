@@ -62,11 +62,13 @@ def ref_logprob(z, target, k):
     logp = torch.where(has, torch.where(none, torch.full_like(at, -math.inf), (at - m0) - torch.log(s)), torch.zeros_like(at))
     top_id = torch.full((T, k), -1, dtype=torch.int64)
     top_lp = torch.full((T, k), -math.inf, dtype=torch.float64)
-    for i in range(T):
-        order = sorted((j for j in range(V) if not math.isnan(z[i, j])), key=lambda j: (-float(z[i, j]), j))[:k] if k else []
-        for q, j in enumerate(order):
-            top_id[i, q] = j
-            top_lp[i, q] = -math.inf if none[i] else (z[i, j] - m0[i]) - torch.log(s[i])
+    if k:
+        number = ~torch.isnan(z)
+        order = torch.sort(torch.where(number, z, -math.inf), dim=1, descending=True, stable=True).indices
+        for i in range(T):
+            ids = [j for j in order[i, :k + int((~number[i]).sum())].tolist() if number[i, j]][:k]
+            top_id[i, :len(ids)] = torch.tensor(ids, dtype=torch.int64)
+            top_lp[i, :len(ids)] = -math.inf if none[i] else (z[i, ids] - m0[i]) - torch.log(s[i])
     return dict(lse=lse, logp=logp, ent=ent, p=p, top_id=top_id, top_lp=top_lp, has=has, none=none)
 
 
@@ -628,6 +630,9 @@ def ref_gated_back(v, f, ranks, of, dy):
 GATED = [
     # dtype, T, d, f, ranks, batch, activation
     ("f32", 1, 33, 8, [8], "one", 0), ("f32", 150, 100, 72, [8, 16], "mixed", 1), ("f32", 700, 96, 200, [8, 8, 8], "mixed", 0),
+    ("bf16", 16, 264, 72, [8, 8], "tokens", 0), ("bf16", 17, 1000, 8, [24], "tokens", 1), ("bf16", 33, 8, 136, [8], "mixed", 0),
+    ("bf16", 64, 4096, 64, [16, 64, 8], "tokens", 1), ("bf16", 64, 136, 8200, [8], "bare", 0), ("bf16", 5, 2056, 520, [64, 8], "tokens", 0),
+    ("bf16", 65, 512, 192, [16], "mixed", 0),
     ("bf16", 1, 64, 64, [8], "one", 0), ("bf16", 40, 512, 1376, [16, 8], "tokens", 1), ("bf16", 300, 256, 128, [16], "mixed", 0),
     ("bf16", 300, 264, 136, [8, 16], "mixed", 1), ("bf16", 600, 1024, 640, [16, 32, 8], "mixed", 0), ("bf16", 300, 256, 512, [8], "bare", 0),
     ("bf16", 2100, 512, 1160, [64, 8], "mixed", 0), ("bf16", 4500, 256, 1024, [8, 24, 16], "mixed", 1), ("bf16", 3000, 640, 2048, [40], "one", 0),
