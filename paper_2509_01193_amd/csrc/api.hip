@@ -13,22 +13,6 @@ using namespace lobra;
 
 namespace {
 
-// Argument checks of a forward call on plan p (everything except the plan itself): host only.
-lobra_status fwd_check(const Plan& p, const void* x, const void* W, const void* A, const void* B, const float* s,
-                       const void* y, const void* h_save, const void* ws, size_t ws_bytes)
-{
-    const bool adapters = !p.tb.empty();
-    if (!x || !W || !y) return LOBRA_ERR_NULL;
-    if (adapters && (!A || !B || !s)) return LOBRA_ERR_NULL;
-    if (!aligned16(x) || !aligned16(W) || !aligned16(y) || !aligned16(A) || !aligned16(B) ||
-        !aligned16(h_save) || !aligned16(ws))
-        return LOBRA_ERR_ALIGN;
-    // the workspace holds, without h_save, the projected activations, and in front of them, if there is room, a split base product's sums
-    const size_t need = h_save ? 0 : p.p_layout.total;
-    if (adapters && need > 0 && (!ws || ws_bytes < need)) return LOBRA_ERR_WORKSPACE;
-    return LOBRA_OK;
-}
-
 // Scratch of lobra_mlora_fwd_static_ws: device memory that is part of the library's code object, so that
 // a call needs no allocation by anybody.  Every GPU the library runs on holds its own copy at its own
 // address; the name below is only a handle for hipGetSymbolAddress, never a pointer to pass to a kernel.
@@ -264,7 +248,7 @@ lobra_status plan_fwd(const lobra_mlora_plan* plan, const void* x, const void* W
     if (rs != LOBRA_OK) return rs;
     const Plan& p = *plan;
     if (p.desc.T == 0) return LOBRA_OK;
-    rs = fwd_check(p, x, W, A, B, s, y, h_save, ws, ws_bytes);
+    rs = plan_fwd_check(p, x, W, A, B, s, y, h_save, ws, ws_bytes);
     if (rs != LOBRA_OK) return rs;
     const bool adapters = !p.tb.empty();
     const bool room = ws && ws_bytes >= (h_save ? p.fwd_part : p.fwd_ws_bytes);       // for a split product's sums
@@ -581,7 +565,7 @@ lobra_status lobra_mlora_fwd(const lobra_mlora_desc* desc, const void* x, const 
     if (p->desc.T == 0) st = LOBRA_OK;
     else if (!ws || ws_bytes < img + (h_save ? 0 : p->p_layout.total)) st = LOBRA_ERR_WORKSPACE;
     else if (!aligned16(ws)) st = LOBRA_ERR_ALIGN;
-    else if ((st = fwd_check(*p, x, W, A, B, s, y, h_save, rest, ws_bytes - img)) == LOBRA_OK &&
+    else if ((st = plan_fwd_check(*p, x, W, A, B, s, y, h_save, rest, ws_bytes - img)) == LOBRA_OK &&
              (st = upload_oneshot(p, ws, stream)) == LOBRA_OK) {
         st = lobra_mlora_plan_fwd(p, x, W, A, B, s, y, h_save, rest, ws_bytes - img, hip_stream);
         const lobra_status rel = release_after(stream, p);

@@ -82,6 +82,22 @@ inline lobra_status runnable(const lobra_mlora_plan* plan)
             LOBRA_HIP(hipEventRecord(static_cast<hipEvent_t>(tp_.trace_events[2 * ti_ + 1]), stream)); \
     } while (0)
 
+// Argument checks of a forward call on plan p (everything except the plan itself): host only.
+inline lobra_status plan_fwd_check(const Plan& p, const void* x, const void* W, const void* A, const void* B, const float* s,
+                                   const void* y, const void* h_save, const void* ws, size_t ws_bytes)
+{
+    const bool adapters = !p.tb.empty();
+    if (!x || !W || !y) return LOBRA_ERR_NULL;
+    if (adapters && (!A || !B || !s)) return LOBRA_ERR_NULL;
+    if (!aligned16(x) || !aligned16(W) || !aligned16(y) || !aligned16(A) || !aligned16(B) ||
+        !aligned16(h_save) || !aligned16(ws))
+        return LOBRA_ERR_ALIGN;
+    // the workspace holds, without h_save, the projected activations, and in front of them, if there is room, a split base product's sums
+    const size_t need = h_save ? 0 : p.p_layout.total;
+    if (adapters && need > 0 && (!ws || ws_bytes < need)) return LOBRA_ERR_WORKSPACE;
+    return LOBRA_OK;
+}
+
 // Argument checks of a backward call on plan p (everything except the plan itself): host only.
 inline lobra_status plan_bwd_check(const Plan& p, const void* x, const void* W, const void* A, const void* B, const float* s,
                                    const void* dy, const void* h_saved, const void* dx, const float* dA, const float* dB,

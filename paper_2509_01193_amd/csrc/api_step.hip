@@ -150,7 +150,7 @@ lobra_status lobra_mlora_gated_workspace_bytes(const lobra_mlora_plan* plan, int
     if (!plan) return LOBRA_ERR_PLAN;
     if (!fwd_bytes) return LOBRA_ERR_NULL;
     if (plan->n_proj != 2) return LOBRA_ERR_SHAPE;
-    *fwd_bytes = (save_gu ? 0 : gated_scratch(*plan)) + plan->fwd_ws_bytes;
+    *fwd_bytes = (save_gu || plan->gated_persistent ? 0 : gated_scratch(*plan)) + plan->fwd_ws_bytes;
     if (gated_is_skinny(*plan)) *fwd_bytes = std::max(*fwd_bytes, gated_skinny_bytes(*plan));
     return LOBRA_OK;
 }
@@ -175,6 +175,16 @@ lobra_status lobra_mlora_gated_fwd(const lobra_mlora_plan* plan, int32_t act, co
         if (!adapters) pd.r_max = 0;
         LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK_GEMM, gated_skinny_product(pd, x, W, A, s, ws, adapters, st));
         LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_skinny_finish(pd, act, B, ws, adapters, gu, h, st));
+        return LOBRA_OK;
+    }
+    if (p.gated_persistent) {
+        if ((rs = plan_fwd_check(p, x, W, A, B, s, h, h_save, ws, ws_bytes)) != LOBRA_OK) return rs;
+        const PlanDev pd = device_view(p);
+        char* const hb = static_cast<char*>(h_save ? h_save : ws);
+        if (adapters)
+            LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK,
+                         shrink_mfma(pd, x, A, s, hb + p.p_layout.p_tok, hb + p.p_layout.p_blk, pd.d_in, pd.d_in, 1, 0, st));
+        LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gemm_persistent_gated(pd, act, x, W, adapters ? hb + p.p_layout.p_tok : nullptr, B, gu, h, st));
         return LOBRA_OK;
     }
     const size_t own = gu ? 0 : gated_scratch(p);

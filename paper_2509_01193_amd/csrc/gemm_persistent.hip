@@ -53,13 +53,26 @@
                              // accumulators; 0 / 2: timing variants (hardly any stores / plain stores)
 #endif
 
-// This file is compiled twice: as it is for K that is a multiple of 128, and by gemm_persistent_ktail.hip for any other K,
+// This file is compiled three times: as it is for K that is a multiple of 128, by gemm_persistent_ktail.hip for any other K,
 // as kernels of another name (a flag of one template would do, but the two together cost the first one its last free
-// registers).
+// registers), and by gemm_persistent_gated.hip for the forward product of a gated feed-forward block.
+// GATED: W's columns are gate (N of them) and up (N), and a column tile is 128 of the one and the matching 128 of the other: of a
+// wave's 128 columns the first 64 are gate's, the other 64 the same columns of up, so that a lane holds g and u of an output in the same
+// place of two accumulators and stores h = a(g) u, from fp32 (and [g | u] where backward is to come: SAVE).  An up projection's step has 16
+// ranks of the gate's window of a segment and the same 16 of the up's, each multiplied with its own half of the columns.
+// 16384 x 4096 x 2 x 11008, us: 2142, with [g | u] 2290; the product and an activation behind it 2187 + 192.  (Of a tile's some 100 us the
+// activation takes 1.5, the stores of [g | u] 6: the next tile's second barrier waits for them.  Plain stores instead of non-temporal ones
+// 2225 and 2407.)
 #ifndef LOBRA_GP_KTAIL
 #define LOBRA_GP_KTAIL 0
 #define LOBRA_GP_KERNEL gemm_persistent_kernel
 #define LOBRA_GP_HOST gemm_persistent
+#endif
+#ifndef LOBRA_GP_GATED
+#define LOBRA_GP_GATED 0
+#endif
+#if LOBRA_GP_GATED
+#include "activation.h"
 #endif
 
 namespace lobra {
@@ -101,16 +114,28 @@ constexpr int acc_reg(int mb, int nb) { return 4 * (NB * mb + nb); }   // first 
 
 }  // namespace
 
+#if LOBRA_GP_GATED
+template <int ACT, bool SAVE>
+#else
 template <bool W_KN>
+#endif
 __global__ __launch_bounds__(64 * NW)
 void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t* __restrict__ W,
                      const uint16_t* __restrict__ P, const uint16_t* __restrict__ M,
                      uint16_t* __restrict__ C, int32_t K, int32_t N, int32_t ldw, int32_t ldc,
                      int32_t nproj, int32_t proj, int32_t tiles_m, int32_t tiles_n, int32_t GM, int32_t cpx,
                      int32_t TPW, const int32_t* __restrict__ tile_seg, const int32_t* __restrict__ cseg_off,
-                     const int32_t* __restrict__ cseg_task, const int32_t* __restrict__ rank_off)
+                     const int32_t* __restrict__ cseg_task, const int32_t* __restrict__ rank_off
+#if LOBRA_GP_GATED
+                     , uint16_t* __restrict__ gated_h
+#endif
+)
 {
-    constexpr bool KTAIL = LOBRA_GP_KTAIL;
+    constexpr bool KTAIL = LOBRA_GP_KTAIL, GATED = LOBRA_GP_GATED;
+#if LOBRA_GP_GATED
+    constexpr bool W_KN = true;
+#endif
+    constexpr int CN = GATED ? BN / 2 : BN;          // columns (of N) of an output tile
     // KTAIL: K is not a multiple of 128 (any multiple of 8 from kPersistentMinKTail on).  The last pair of K tiles is then partly,
     // its second tile perhaps wholly, beyond K: their copies repeat the last valid chunk, and both operands' fragments
     // are cleared in registers in front of the K steps that reach beyond K.  A kernel of its own, so that whole K tiles
@@ -161,7 +186,7 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
         // fits (the launcher guarantees T >= BM, N >= BN): it computes some elements of its neighbour once
         // more, bit for bit the same, and no tile needs clamped addresses or masked stores.
         row0 = min((first_m + in % gsz) * BM, T - BM);
-        col0 = min((in / gsz) * BN, N - BN);
+        col0 = min((in / gsz) * CN, N - CN);
     };
 
     // Accumulator (mb, nb) of this wave is a[acc_reg(mb, nb) : + 3] (see gemm_common.h); its register v holds
@@ -185,7 +210,9 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
         if (W_KN) {
             const int krow = 2 * blk + (lane >> 5);
             const int chn = (lane & 31) ^ kn_swz2(krow);
-            wvo[c] = (uint32_t(krow) * uint32_t(ldw) + 8u * chn) * 2u;
+            // (GATED: chunks 0 .. 7 and 16 .. 23 are columns 0 .. 63 and 64 .. 127 of gate, the others those of up)
+            if (GATED) wvo[c] = (uint32_t(krow) * uint32_t(ldw) + uint32_t(chn >> 3 & 1) * uint32_t(N) + 64u * (chn >> 4) + 8u * (chn & 7)) * 2u;
+            else wvo[c] = (uint32_t(krow) * uint32_t(ldw) + 8u * chn) * 2u;
         } else {
             // LDS row `row` of the W tile feeds result row (row & 15) of block (row & 127) >> 4 of wave
             // row >> 7: it holds the column that block_col deals to it
@@ -406,6 +433,13 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
     auto next_step = [&](Walk& w, int32_t row_end) __attribute__((always_inline)) {
         if (w.r == 0) return false;
         const int32_t left = w.r - w.k;
+        if constexpr (GATED) {                       // (w.m, w.pc: the gate's window; the up's follows it)
+            w.a = Half{w.lo, w.hi, w.m + w.k, min(left, 16), w.pc + w.k};
+            w.b = Half{w.lo, w.hi, w.a.m + w.r, w.a.n, w.a.pc + w.r};
+            w.k += 16;
+            if (w.k >= w.r) next_segment(w, row_end);
+            return true;
+        }
         w.a = Half{w.lo, w.hi, w.m + w.k, min(left, 16), w.pc + w.k};
         w.b = Half{w.lo, w.hi, w.a.m, 0, w.a.pc};
         if (left > 16) {
@@ -429,12 +463,14 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
     auto first_step = [&](Walk& w, int32_t row0, int32_t col0) __attribute__((always_inline)) {
         w.e = 0;
         w.sg = rec[4 * kGemmTileSegs];
-        w.pj = proj >= 0 ? proj : rfl(col0 / pd.dg);
+        w.pj = GATED ? 0 : proj >= 0 ? proj : rfl(col0 / pd.dg);
         w.mcol0 = proj >= 0 ? 0 : w.pj * pd.dg;
         w.mpitch = proj >= 0 ? N : pd.dg;
         window(w, rec[0], rec[1], rec[2], rec[3]);
         return next_step(w, min(row0 + BM, T));
     };
+    // first column of chunk n of a row of M in the adapter region, from the tile's (GATED: the same ones for gate and up)
+    auto mcol = [](uint32_t n) __attribute__((always_inline)) { return GATED ? 64u * (n >> 4) + 8u * (n & 7) : 8u * n; };
     // copies a step's operands for the tile at (row0, col0): 2 RCOPIES copies per wave
     auto copy_step = [&](const Walk& w, int32_t row0, int32_t col0) __attribute__((always_inline)) {
         // (opaque to the optimiser: the per-lane offsets are worked out here instead of living in loop-invariant registers
@@ -447,7 +483,7 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
             const int32_t m = c < RCOPIES / 2 ? w.a.m : w.b.m, n = c < RCOPIES / 2 ? w.a.n : w.b.n;
             dma16(lds0 + MSLICE_OFF + (wave_u + NW * c) * 1024,
                   reinterpret_cast<const unsigned char*>(M + size_t(m) * w.mpitch + (col0 - w.mcol0)),
-                  (uint32_t(min(krow & 15, max(n - 1, 0))) * uint32_t(w.mpitch) + 8u * ((ln & 31) ^ kn_swz2(krow))) * 2u);
+                  (uint32_t(min(krow & 15, max(n - 1, 0))) * uint32_t(w.mpitch) + mcol(uint32_t((ln & 31) ^ kn_swz2(krow)))) * 2u);
         }
         const int ch = ln & 3, k = 8 * (ch & 1);
         const int32_t pcol = ch < 2 ? w.a.pc + (k < w.a.n ? k : 0) : w.b.pc + (k < w.b.n ? k : 0);
@@ -516,12 +552,14 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
                 u32x4 km;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) km[w] = (2 * w < nv ? 0xffffu : 0u) | (2 * w + 1 < nv ? 0xffff0000u : 0u);
+                // GATED: gate's columns, the first half of the blocks, meet the ranks of half 0 alone, up's those of half 1
+                const u32x4 kmg = kg < 2 ? km : zero4, kmu = kg < 2 ? zero4 : km;
                 bf16x8 m[NB];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     union { bf16x8 b; u32x4 u; } cv;
                     cv.b = mf[nb];
-                    cv.u &= km;
+                    cv.u &= !GATED ? km : nb < NB / 2 ? kmg : kmu;
                     m[nb] = cv.b;
                 }
                 // The MFMAs are asm statements, which the compiler's hazard pass does not look into: an MFMA must not read a
@@ -533,6 +571,14 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
                     constexpr int mb = decltype(mb_c)::value;
                     const int32_t rb = srow0 + mb * 16, row = rb + j;
                     if (hi <= rb || lo >= rb + 16) return;           // wave-uniform
+                    if constexpr (GATED) {
+                        const bool in = row >= lo && row < hi;
+                        bf16x8 pg = as_bf16x8(in ? (pv[mb] & kmg) : zero4), pu = as_bf16x8(in ? (pv[mb] & kmu) : zero4);
+                        asm volatile("s_nop 1" : "+v"(pg), "+v"(pu));
+                        static_for<0, NB / 2>([&](auto nb_c) { mfma_acc<acc_reg(mb, decltype(nb_c)::value)>(m[decltype(nb_c)::value], pg); });
+                        static_for<NB / 2, NB>([&](auto nb_c) { mfma_acc<acc_reg(mb, decltype(nb_c)::value)>(m[decltype(nb_c)::value], pu); });
+                        return;
+                    }
                     bf16x8 pf = as_bf16x8((row >= lo && row < hi) ? (pv[mb] & km) : zero4);
                     asm volatile("s_nop 1" : "+v"(pf));
                     static_for<0, NB>([&](auto nb_c) { mfma_acc<acc_reg(mb, decltype(nb_c)::value)>(m[decltype(nb_c)::value], pf); });
@@ -582,6 +628,40 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
         //      carried out in order, so the reads of a block need no wait for its writes.
         //      (Nobody reads the adapter region any more: the last step's reads are behind a barrier.)
         unsigned char* cs = lds + MSLICE_OFF + wave * 8192;
+#if LOBRA_GP_GATED
+        // (GATED: three 64 x 64 blocks per 64 rows, or one: g, u, and h = a(g) u of accumulators that lie four blocks apart)
+        static_for<0, 6>([&](auto b_c) {
+            constexpr int hm = decltype(b_c)::value / 3, what = decltype(b_c)::value % 3;
+            if constexpr (!SAVE && what < 2) return;
+            static_for<0, 4>([&](auto m_c) {
+                constexpr int mb = 4 * hm + decltype(m_c)::value;
+                static_for<0, 2>([&](auto p_c) {
+                    constexpr int p = decltype(p_c)::value;
+                    bf16x8 o;
+                    static_for<0, 8>([&](auto q_c) {
+                        constexpr int q = decltype(q_c)::value;
+                        if constexpr (what < 2) {
+                            o[q] = (__bf16)acc_read<acc_reg(mb, 2 * p + 4 * what) + q>();
+                        } else {
+                            const float g = acc_read<acc_reg(mb, 2 * p) + q>(), u = acc_read<acc_reg(mb, 2 * p + 4) + q>();
+                            o[q] = (__bf16)(activate<ACT>(g) * u);
+                        }
+                    });
+                    o = pair_order(o);
+                    const int r = 16 * (mb % 4) + j, c = 4 * p + kg;
+                    *reinterpret_cast<bf16x8*>(cs + r * 128 + ((c ^ swz_row(r)) << 4)) = o;
+                });
+            });
+            static_for<0, 8>([&](auto i_c) {
+                const int r = 8 * decltype(i_c)::value + (lane >> 3), pos = lane & 7;
+                const bf16x8 o = *reinterpret_cast<const bf16x8*>(cs + r * 128 + (pos << 4));
+                const size_t row = size_t(wrow0 + 64 * hm + r);
+                const int32_t col = col0 + wn * 64 + 8 * (pos ^ swz_row(r));
+                uint16_t* dst = what < 2 ? C + row * ldc + what * N + col : gated_h + row * N + col;
+                __builtin_nontemporal_store(o, reinterpret_cast<bf16x8*>(dst));
+            });
+        });
+#else
         static_for<0, 4>([&](auto b_c) {
             constexpr int hm = decltype(b_c)::value / 2, hn = decltype(b_c)::value % 2;
             static_for<0, 4>([&](auto m_c) {
@@ -612,6 +692,7 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
 #endif
             });
         });
+#endif
 #endif
         // (the accumulators are not cleared here: the first K step of the next tile starts from zero)
     };
@@ -647,7 +728,11 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
     // (The workgroup's very first tile has no stores behind its copies: the prologue waits for them itself.)
     auto tile_barrier_after_stores = []() __attribute__((always_inline)) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#if LOBRA_GP_GATED
+        wait_vmcnt<SAVE ? 48 : 16>();
+#else
         wait_vmcnt<LOBRA_GP_STORES_IN_FLIGHT>();
+#endif
         __builtin_amdgcn_s_barrier();
     };
     // KTAIL: in front of K step q (0 .. 3) of a pair of K tiles, the fragments' lanes whose 8 k lie beyond K are
@@ -713,10 +798,16 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
 }
 
 namespace {
+#if LOBRA_GP_GATED
+template <int ACT, bool SAVE>
+#define LOBRA_GP_ARGS ACT, SAVE
+#else
 template <bool W_KN>
+#define LOBRA_GP_ARGS W_KN
+#endif
 hipError_t launch_persistent(const PlanDev& pd, const void* Z, const void* W, const void* P, const void* M, void* C,
                              int32_t K, int32_t N, int32_t ldw, int32_t ldc, int32_t nproj, int32_t proj,
-                             int32_t tiles_m, int32_t tiles_n, int32_t gm, hipStream_t st)
+                             int32_t tiles_m, int32_t tiles_n, int32_t gm, hipStream_t st, [[maybe_unused]] void* gated_h = nullptr)
 {
     // once per device: the kernel needs more dynamic LDS than the default limit; one workgroup per compute unit
     static std::atomic<int32_t> cus[64];
@@ -726,7 +817,7 @@ hipError_t launch_persistent(const PlanDev& pd, const void* Z, const void* W, co
     if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
     int32_t ncu = cus[dev].load(std::memory_order_acquire);
     if (ncu == 0) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&LOBRA_GP_KERNEL<W_KN>),
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&LOBRA_GP_KERNEL<LOBRA_GP_ARGS>),
                                 hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
         if (e != hipSuccess) return e;
         int n = 0;
@@ -741,13 +832,28 @@ hipError_t launch_persistent(const PlanDev& pd, const void* Z, const void* W, co
     const int64_t xmax = (ntiles + 7) / 8;                                    // tiles of the fullest XCD
     const int64_t rounds = (xmax + int64_t(cpx) * tpw - 1) / (int64_t(cpx) * tpw);
     const int64_t wgs = ntiles <= 8 * int64_t(cpx) ? ntiles : 8 * rounds * cpx;   // few tiles: one workgroup each
-    LOBRA_GP_KERNEL<W_KN><<<dim3(uint32_t(wgs)), 64 * NW, LDS_BYTES, st>>>(
+    LOBRA_GP_KERNEL<LOBRA_GP_ARGS><<<dim3(uint32_t(wgs)), 64 * NW, LDS_BYTES, st>>>(
         pd, (const uint16_t*)Z, (const uint16_t*)W, (const uint16_t*)P, (const uint16_t*)M, (uint16_t*)C,
-        K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, gm, cpx, tpw, pd.gemm_tile_seg, pd.cseg_off, pd.cseg_task, pd.rank_off);
+        K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, gm, cpx, tpw, pd.gemm_tile_seg, pd.cseg_off, pd.cseg_task, pd.rank_off
+#if LOBRA_GP_GATED
+        , (uint16_t*)gated_h
+#endif
+    );
     return hipGetLastError();
 }
 }  // namespace
 
+#if LOBRA_GP_GATED
+hipError_t LOBRA_GP_HOST(const PlanDev& pd, int act, const void* x, const void* W, const void* P, const void* B, void* gu, void* h, hipStream_t st)
+{
+    const int32_t K = pd.d_in, f = pd.dg, tiles_m = (pd.T + BM - 1) / BM, tiles_n = (f + BN / 2 - 1) / (BN / 2), gm = K > 4096 ? 4 : 6;
+    if (pd.T < BM || f < BN / 2 || K % (2 * BK) != 0) return hipErrorInvalidValue;      // (what choose_gated_persistent asks for)
+#define LOBRA_GATED(...) launch_persistent<__VA_ARGS__>(pd, x, W, P, B, gu, K, f, 2 * f, 2 * f, 2, 0, tiles_m, tiles_n, gm, st, h)
+    if (act == LOBRA_ACT_SILU) return gu ? LOBRA_GATED(LOBRA_ACT_SILU, true) : LOBRA_GATED(LOBRA_ACT_SILU, false);
+    return gu ? LOBRA_GATED(LOBRA_ACT_GELU_TANH, true) : LOBRA_GATED(LOBRA_ACT_GELU_TANH, false);
+#undef LOBRA_GATED
+}
+#else
 hipError_t LOBRA_GP_HOST(const PlanDev& pd, bool transW, const void* Z, const void* W, const void* P,
                            const void* M, void* C, int32_t K, int32_t N, int32_t ldw, int32_t ldc, int32_t nproj,
                            int32_t proj, int32_t tiles_m, int32_t tiles_n, int32_t gm, hipStream_t st)
@@ -759,5 +865,6 @@ hipError_t LOBRA_GP_HOST(const PlanDev& pd, bool transW, const void* Z, const vo
     if (transW) return launch_persistent<false>(pd, Z, W, P, M, C, K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, gm, st);
     return launch_persistent<true>(pd, Z, W, P, M, C, K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, gm, st);
 }
+#endif
 
 }  // namespace lobra

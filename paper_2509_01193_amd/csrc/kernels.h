@@ -174,6 +174,10 @@ constexpr int64_t kSkinnyTokens = 64;
 size_t gated_skinny_ws_bytes(int64_t T, int32_t K, int32_t f, int32_t r_max);
 hipError_t gated_skinny_product(const PlanDev& pd, const void* x, const void* W, const void* A, const float* s, void* ws, bool adapters, hipStream_t st);
 hipError_t gated_skinny_finish(const PlanDev& pd, int act, const void* B, const void* ws, bool adapters, void* gu, void* h, hipStream_t st);
+// The product with the activation in its epilogue (gemm_persistent.hip), of a plan that says so (gated_persistent).  P: the token-major
+// projections, or NULL; gu or NULL.
+hipError_t gemm_persistent_gated(const PlanDev& pd, int act, const void* x, const void* W, const void* P, const void* B, void* gu, void* h,
+                                 hipStream_t st);
 hipError_t gated_derive(int dtype, int act, int64_t T, int32_t f, const void* gu, const void* dh, void* dgu, hipStream_t st);
 
 hipError_t token_task_map(const PlanDev& pd, int32_t* out_task, int64_t* out_count, hipStream_t st);

@@ -401,6 +401,7 @@ lobra_status build_host_plan(const lobra_mlora_desc* d, uint32_t flags, Plan* p)
                 choose_gemm(T, d->d_in, d->d_out, p->dg, ns, rk, 0).cost <=
                     float(p->n_proj) * (choose_gemm(T, d->d_in, p->dg, 0, ns, rk, 0).cost + 3.f))
                 p->fwd_group = p->dg;
+            p->gated_persistent = p->n_proj == 2 && choose_gated_persistent(T, d->d_in, p->dg, p->fwd_group, ns, rk);
             p->beside_fwd = p->beside_bwd = GemmChoice{};
             if (p->n_proj == 1) {
                 int32_t halves = 1;
@@ -472,6 +473,17 @@ GemmChoice choose_gemm(int64_t T, int32_t K, int32_t N, int32_t group, int32_t n
         }
     }
     return best;
+}
+
+bool choose_gated_persistent(int64_t T, int32_t K, int32_t f, int32_t group, int32_t nseg, int32_t rank)
+{
+    const GemmTile& t = kGemmTiles[kPersistentTile];
+    if (T < t.tm || f < t.tn / 2 || K % (2 * kGemmKTile) != 0) return false;
+    const float segments = std::max(0.f, float(nseg) * kGemmTileRows / float(T) - 1.f);
+    const int64_t tiles = (T + t.tm - 1) / t.tm * ((f + t.tn / 2 - 1) / (t.tn / 2));
+    const float inside = rounds_cost(t, tiles, K / kGemmKTile, t.fixed + kGatedFixed + kSegmentCost.persistent * segments) + t.once;
+    const float apart = group > 0 ? choose_gemm(T, K, 2 * f, f, nseg, rank, 0).cost : 2.f * (choose_gemm(T, K, f, 0, nseg, rank, 0).cost + 3.f);
+    return inside <= apart + 3.f + float(T) * float(f) * 6.f / 5.6e6f;
 }
 
 GemmChoice choose_beside(int64_t T, int32_t K, int32_t N, int32_t nseg, int32_t rank, int64_t ntb, int32_t halves)

@@ -146,6 +146,14 @@ GemmChoice choose_gemm(int64_t T, int32_t K, int32_t N, int32_t group, int32_t n
 inline float beside_gain(int32_t K) { return K < 3414 ? 3.5f + 0.45f * float(K) / 1024.f : 5.f; }
 constexpr int64_t kMaxBesideItems = 256, kMaxBesideRankRows = int64_t(32) << 20;
 GemmChoice choose_beside(int64_t T, int32_t K, int32_t N, int32_t nseg, int32_t rank, int64_t ntb, int32_t halves);
+// A gated feed-forward block's forward pass (n_proj = 2, f = N / 2 columns of each): whether the persistent kernel's form with the activation
+// in the epilogue (T >= 256, f >= 128, whole K tiles of 128) is no worse than the product as group says (as Plan::fwd_group) and a launch that
+// activates it (5.6 TB/s).  kGatedFixed: what the epilogue costs a tile beside `fixed`.  Measured, us, product and activation / in one, without
+// saving [g | u]: 300 x 4096 x 2 x 8192 62 / 85, 400 x 1024 x 8192 31 / 34, 1000 x 1024 x 4096 32 / 33, 4000 x 1024 x 1024 33 / 36, 700 x 2048 x
+// 8192 62 / 54, 900 x 4096 x 5504 115 / 87, 3000 x 2048 x 2048 63 / 57, 12000 x 4096 x 600 182 / 125, 16000 x 512 x 2000 151 / 87, 16384 x 4096 x
+// 11008 2379 / 2142 (saving it 2290).
+constexpr float kGatedFixed = 3.f;
+bool choose_gated_persistent(int64_t T, int32_t K, int32_t f, int32_t group, int32_t nseg, int32_t rank);
 // The scratch that these choices would like to have (0: none).
 size_t gemm_part_bytes(int64_t T, int32_t K, int32_t N, int32_t group, int32_t nseg, int32_t rank, const GemmChoice& beside);
 
@@ -203,6 +211,7 @@ struct Plan {
     // (fwd_group: fused projections' forward products run as one launch whose tiles do not straddle multiples of this
     // many columns; 0: one launch per projection)
     int32_t fwd_group = 0;
+    bool gated_persistent = false;      // n_proj = 2: choose_gated_persistent
     GemmChoice beside_fwd, beside_bwd;  // the projection in the launch of its product, given scratch for it (tile -1: not)
     size_t bwd_off_spart = 0, fwd_part = 0, bwd_part = 0, bwd_need = 0;
     // dB fused into the sliced projection of dy (one pass over dy for s_t B_t dy_i and for dB): a workgroup

@@ -637,6 +637,8 @@ GATED = [
     ("bf16", 300, 264, 136, [8, 16], "mixed", 1), ("bf16", 600, 1024, 640, [16, 32, 8], "mixed", 0), ("bf16", 300, 256, 512, [8], "bare", 0),
     ("bf16", 2100, 512, 1160, [64, 8], "mixed", 0), ("bf16", 4500, 256, 1024, [8, 24, 16], "mixed", 1), ("bf16", 3000, 640, 2048, [40], "one", 0),
     ("bf16", 2049, 1024, 4096, [16] * 5, "mixed", 1),
+    ("bf16", 16000, 128, 128, [8, 16], "mixed", 0), ("bf16", 9000, 256, 264, [64, 8, 24], "mixed", 0), ("bf16", 5000, 256, 1160, [8], "bare", 1),
+    ("bf16", 6000, 128, 1000, [16] * 9, "tokens", 0),
 ]
 
 
@@ -695,6 +697,40 @@ def test_gated(dtype, T, d, f, ranks, batch, act):
     bd.lobra_mlora_gated_bwd(plan, act, *w, gu, dv["dh"], hs, gu, dx, dA, dB, bd.FLAG_NO_DX, wsb)
     torch.cuda.synchronize()
     assert torch.equal(gu, keep)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [40, 200, 4500])
+def test_gated_adapter_of_no_finite_value_stays_with_its_task(T):
+    """Tasks side by side in a tile: NaN and inf in one's adapters (both projections) reach its own tokens alone - and, as in the layer's own
+    products, whose matrix instructions take 16 rows at a time, at most rows that share a block of 16 with those.  The few-token kernels share
+    nothing."""
+    d, f, ranks = 256, 1024, [8, 16, 24]
+    off, task = batch_of("mixed", T, 3)
+    of = torch.from_numpy(np.repeat(np.asarray(task), np.diff(np.asarray(off))))
+    v = gated_inputs("bf16", T, d, f, ranks, T)
+    for row in (16, 20, 31, 32, 47):                  # task 1: stacked rows 16 .. 47, gate's then up's
+        v["B"][row, ::3] = math.nan
+        v["A"][row, ::5] = math.inf
+    plan = bd.Plan("bf16", T, d, 2 * f, [0, 16, 48, 96], off, task, n_proj=2)
+    y = ref_gated_projections({**v, "A": torch.nan_to_num(v["A"], posinf=0.0), "B": torch.nan_to_num(v["B"])}, f, ranks, of)
+    h_ref = act64(0, y[:, :f])[0] * y[:, f:]
+    w = [v[k].to(DEV) for k in ("x", "W", "A", "B", "s")]
+    gu, h = torch.empty(T, 2 * f, dtype=torch.bfloat16, device=DEV), torch.empty(T, f, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(bd.lobra_mlora_gated_workspace_bytes(plan, True), dtype=torch.uint8, device=DEV)
+    bd.lobra_mlora_gated_fwd(plan, 0, *w, gu, h, None, ws)
+    torch.cuda.synchronize()
+    others = of != 1
+    got = h.double().cpu()
+    assert bool(torch.isnan(got[of == 1]).any())
+    if T > 64:
+        blocks = torch.zeros((T + 31) // 16 * 16, dtype=torch.bool)
+        blocks[:T] = of == 1
+        # (the last row of tiles may begin anywhere: blocks of 16 from any row)
+        others &= torch.tensor([not bool(blocks[max(0, i - 15):i + 16].any()) for i in range(T)])
+        assert int(others.sum()) > 20
+    assert bool(torch.isfinite(got[others]).all())
+    assert float((got - h_ref)[others].abs().max() / h_ref[others].abs().max()) <= 2.0 ** -7
 
 
 @pytest.mark.gpu
