@@ -24,20 +24,31 @@ namespace {
 template <typename E, int N> struct Piece {
     typedef u32x4 Raw;
     static __device__ __forceinline__ Raw fetch(const E* p) { return *reinterpret_cast<const u32x4*>(p); }
+    template <bool ONCE> static __device__ __forceinline__ Raw fetch_row(const E* p)
+    {
+        return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)) : fetch(p);
+    }
     static __device__ __forceinline__ void widen(Raw r, float (&v)[N]) { Packet<E>::widen(r, v); }
     static __device__ __forceinline__ float widen(Raw r, int i) { return Packet<E>::element(r, i); }
     static __device__ __forceinline__ Raw zero() { return u32x4{0u, 0u, 0u, 0u}; }
     static __device__ __forceinline__ void load(const E* p, float (&v)[N]) { widen(fetch(p), v); }
     static __device__ __forceinline__ void store(E* p, const float (&v)[N]) { *reinterpret_cast<u32x4*>(p) = Packet<E>::narrow(v); }
+    template <bool ONCE> static __device__ __forceinline__ void store_row(E* p, const float (&v)[N])
+    {
+        if (ONCE) __builtin_nontemporal_store(Packet<E>::narrow(v), reinterpret_cast<u32x4*>(p));
+        else store(p, v);
+    }
 };
 template <typename E> struct Piece<E, 1> {
     typedef E Raw;
     static __device__ __forceinline__ Raw fetch(const E* p) { return *p; }
+    template <bool ONCE> static __device__ __forceinline__ Raw fetch_row(const E* p) { return fetch(p); }
     static __device__ __forceinline__ void widen(Raw r, float (&v)[1]) { v[0] = Elem<E>::load(&r, 0); }
     static __device__ __forceinline__ float widen(Raw r, int) { return Elem<E>::load(&r, 0); }
     static __device__ __forceinline__ Raw zero() { return E(0); }
     static __device__ __forceinline__ void load(const E* p, float (&v)[1]) { widen(fetch(p), v); }
     static __device__ __forceinline__ void store(E* p, const float (&v)[1]) { Elem<E>::store(p, 0, v[0]); }
+    template <bool ONCE> static __device__ __forceinline__ void store_row(E* p, const float (&v)[1]) { store(p, v); }
 };
 // v as the element type holds it
 template <typename E> __device__ __forceinline__ float rounded(float v);
@@ -166,7 +177,8 @@ template <typename E> struct NormGradArgs {
 
 // A team's rows one after the other.  SUMS: the sums over tokens are wanted.  sum_run = sum g bh of a run of rows of one segment (without
 // gates: of all rows): at its end it goes to the gate's partial sums and, times alpha gate_t, into sum_post.
-template <typename E, int N, int NT, int I, bool SUMS>
+// ONCE: the rows are more than the caches hold and are read and written past them.
+template <typename E, int N, int NT, int I, bool SUMS, bool ONCE>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT, I * N <= 8 ? 4 : 1)
 void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
 {
@@ -225,10 +237,10 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
         for (int i = 0; i < I; ++i) {
             const int32_t c = (t + i * NT) * N;
             const bool in = c < a.d;
-            f.dx[i] = in && a.dx ? P::fetch(a.dx + base + c) : P::zero();
-            f.r[i] = in && a.dx ? P::fetch(a.r_out + base + c) : P::zero();
-            f.dr[i] = in && a.dr_out ? P::fetch(a.dr_out + base + c) : P::zero();
-            f.b[i] = in && a.b ? P::fetch(a.b + base + c) : P::zero();
+            f.dx[i] = in && a.dx ? P::template fetch_row<ONCE>(a.dx + base + c) : P::zero();
+            f.r[i] = in && a.dx ? P::template fetch_row<ONCE>(a.r_out + base + c) : P::zero();
+            f.dr[i] = in && a.dr_out ? P::template fetch_row<ONCE>(a.dr_out + base + c) : P::zero();
+            f.b[i] = in && a.b ? P::template fetch_row<ONCE>(a.b + base + c) : P::zero();
         }
     };
 #pragma unroll
@@ -302,8 +314,8 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
                 if (a.post) out[e] = cur.n * fmaf(-k.bh, c2, out[e]);
             }
             if (c < a.d) {
-                P::store(a.dr + base + c, g);
-                if (a.b) P::store(a.db + base + c, out);
+                P::template store_row<ONCE>(a.dr + base + c, g);
+                if (a.b) P::template store_row<ONCE>(a.db + base + c, out);
             }
         }
         if (AHEAD) cur = next;
@@ -325,7 +337,9 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
 }
 
 // Adds the partial sums up, in order: y = 0 and 1: the gains', over the teams; y = 2 + t: task t's gate's, over the runs of its segments
-// (segment k's runs are the teams from the one with its first row to the one with its last).  64 columns by 16 lanes of slots.
+// (segment k's runs are the teams from the one with its first row to the one with its last, their slots one behind the other).  64
+// columns by 16 lanes, of which four take different segments.  (Segment after segment by all lanes, each segment's reads waited for before
+// the next one's task is known, 41 segments took 13 us instead of 8.)
 template <typename E>
 __global__ __launch_bounds__(1024)
 void block_norm_sum_kernel(PlanDev pd, const float* __restrict__ part_gate, const float* __restrict__ part_post, const float* __restrict__ part_pre,
@@ -333,6 +347,8 @@ void block_norm_sum_kernel(PlanDev pd, const float* __restrict__ part_gate, cons
                            float* __restrict__ dw_post, float* __restrict__ dw_pre, int accumulate)
 {
     __shared__ float lds[16][64];
+    __shared__ int2 runs[1024];                       // first slot and slots of the task's segments among 1024
+    __shared__ int32_t found[16];
     const int32_t col = int32_t(blockIdx.x) * 64 + (threadIdx.x & 63), lane = threadIdx.x >> 6;
     const int32_t what = blockIdx.y;
     float* out = what == 0 ? dw_post : what == 1 ? dw_pre : dgate;
@@ -342,15 +358,36 @@ void block_norm_sum_kernel(PlanDev pd, const float* __restrict__ part_gate, cons
     if (what < 2) {
         const float* p = what == 0 ? part_post : part_pre;
         if (col < d)
+#pragma unroll 8
             for (int32_t k = lane; k < teams; k += 16) s += p[size_t(k) * d + col];
     } else {
         any = false;
-        for (int32_t k = 0; k < pd.nseg; ++k) {
-            if (pd.cseg_task[k] != what - 2) continue;
-            any = true;
-            const int32_t w0 = pd.cseg_off[k] / rows, w1 = (pd.cseg_off[k + 1] - 1) / rows;
+        for (int32_t base = 0; base < pd.nseg; base += 1024) {
+            const int32_t k = base + int32_t(threadIdx.x);
+            const bool mine = k < pd.nseg && pd.cseg_task[k] == what - 2;
+            const uint64_t mask = __ballot(mine);
+            if ((threadIdx.x & 63) == 0) found[lane] = __popcll(mask);
+            __syncthreads();
+            int32_t at = 0, n = 0;
+#pragma unroll
+            for (int w = 0; w < 16; ++w) {
+                at += w < lane ? found[w] : 0;
+                n += found[w];
+            }
+            if (mine) {
+                const int32_t w0 = pd.cseg_off[k] / rows, w1 = (pd.cseg_off[k + 1] - 1) / rows;
+                runs[at + __popcll(mask & ((uint64_t(1) << (threadIdx.x & 63)) - 1))] = int2{w0 + k, w1 - w0 + 1};
+            }
+            __syncthreads();
+            any = any || n > 0;
             if (col < d)
-                for (int32_t w = w0 + lane; w <= w1; w += 16) s += part_gate[(size_t(w) + k) * d + col];
+                for (int32_t q = lane & 3; q < n; q += 4) {
+                    const int2 run = runs[q];
+                    const float* p = part_gate + size_t(run.x) * d + col;
+#pragma unroll 4
+                    for (int32_t w = lane >> 2; w < run.y; w += 4) s += p[size_t(w) * d];
+                }
+            __syncthreads();
         }
         out += size_t(what - 2) * d;
     }
@@ -409,8 +446,16 @@ template <typename E, int N, int NT, int I> struct Launch {
     {
         constexpr int BT = NT < 256 ? 256 : NT;
         const dim3 grid(uint32_t((teams + BT / NT - 1) / (BT / NT)));
-        if (sums) block_norm_bwd_kernel<E, N, NT, I, true><<<grid, BT, 0, st>>>(pd, a);
-        else block_norm_bwd_kernel<E, N, NT, I, false><<<grid, BT, 0, st>>>(pd, a);
+        // six tensors beyond the 256 MB infinity cache (us, plain / past the caches: 16384 x 4096 bf16, 805 MB, with the forward pass in front of it 313 / 275; 2999 x 1025 fp32,
+        // 74 MB, 26 / 33)
+        const bool once = N > 1 && size_t(pd.T) * size_t(a.d) * sizeof(E) * 6 > (size_t(256) << 20);
+        if (sums) {
+            if (once) block_norm_bwd_kernel<E, N, NT, I, true, N != 1><<<grid, BT, 0, st>>>(pd, a);
+            else block_norm_bwd_kernel<E, N, NT, I, true, false><<<grid, BT, 0, st>>>(pd, a);
+        } else {
+            if (once) block_norm_bwd_kernel<E, N, NT, I, false, N != 1><<<grid, BT, 0, st>>>(pd, a);
+            else block_norm_bwd_kernel<E, N, NT, I, false, false><<<grid, BT, 0, st>>>(pd, a);
+        }
     }
 };
 
