@@ -67,7 +67,7 @@ struct lobra_grad_set {
     std::vector<unsigned char> blob;         // what the device has: the pieces, then task_piece [n_tasks + 1]
     size_t o_task_piece = 0;
     int32_t n_pieces = 0, n_tasks = 0;
-    bool any_out = false;
+    bool any_out = false, once = false;      // once: more than the 256 MB infinity cache holds
     int device = -1;
     void* dev = nullptr;
     bool owns = false;
@@ -105,6 +105,7 @@ lobra_status make_set(const lobra_grad_tensor* tensors, int32_t n_tensors, int32
     if (total / per + int64_t(n_tensors) * n_tasks >= int64_t(1) << 23) return LOBRA_ERR_SHAPE;     // (a launch holds less than 2^32 threads)
     lobra_grad_set* s = new (std::nothrow) lobra_grad_set();
     if (!s) return LOBRA_ERR_NOMEM;
+    s->once = size_t(total) * sizeof(float) > (size_t(256) << 20);
     try {
         std::vector<GradPiece> pieces;
         std::vector<int32_t> task_piece(size_t(n_tasks) + 1, 0);
@@ -398,7 +399,7 @@ lobra_status lobra_grad_clip(const lobra_grad_set* set, const float* max_norm, c
     double* partial = static_cast<double*>(ws);
     float* scale = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(size_t(set->n_pieces) * sizeof(double)));
     LOBRA_HIP(grad_clip(reinterpret_cast<const GradPiece*>(d), reinterpret_cast<const int32_t*>(d + set->o_task_piece), set->n_pieces, set->n_tasks,
-                        set->any_out, max_norm, grad_scale, step, norm, clip_scale, step_out, (flags & LOBRA_FLAG_JOINT_NORM) != 0, partial, scale,
+                        set->any_out, set->once, max_norm, grad_scale, step, norm, clip_scale, step_out, (flags & LOBRA_FLAG_JOINT_NORM) != 0, partial, scale,
                         static_cast<hipStream_t>(hip_stream)));
     return LOBRA_OK;
 }

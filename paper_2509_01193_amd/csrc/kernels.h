@@ -142,13 +142,13 @@ hipError_t logprob_fwd(const LogprobShape& s, const void* logits, const int32_t*
 hipError_t logprob_bwd(const LogprobShape& s, const void* logits, const int32_t* target, const LogprobGrad& in, void* dlogits, hipStream_t st);
 
 // Gradient norms and clipping (grad_clip.hip) over a set's pieces, which are grouped by task: those of task t are
-// task_piece[t] .. task_piece[t + 1] - 1.  partial [pieces] fp64.
+// task_piece[t] .. task_piece[t + 1] - 1.  partial [pieces] fp64.  once: they are more than the caches hold.
 struct GradPiece {
     const float* grad;
     float* out;              // or NULL
     int32_t n, task;
 };
-hipError_t grad_clip(const GradPiece* pieces, const int32_t* task_piece, int32_t n_pieces, int32_t n_tasks, bool any_out, const float* max_norm,
+hipError_t grad_clip(const GradPiece* pieces, const int32_t* task_piece, int32_t n_pieces, int32_t n_tasks, bool any_out, bool once, const float* max_norm,
                      const float* grad_scale, const int32_t* step, float* norm, float* clip_scale, int32_t* step_out, bool joint,
                      double* partial, float* scale, hipStream_t st);
 
