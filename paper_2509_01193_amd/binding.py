@@ -435,13 +435,16 @@ def lobra_token_logprob_bwd(desc: LogprobDesc, logits, target, lse, lse_rest, en
 
 def make_grad_tensors(tensors):
     """(array of GradTensor, keepalive) of [(grad, out or None, rank_off)]: fp32 tensors [R, D]."""
-    arr, keep = (GradTensor * max(len(tensors), 1))(), []
+    arr, keep, tables = (GradTensor * max(len(tensors), 1))(), [], {}
     for i, (g, out, rank_off) in enumerate(tensors):
-        ro = _i32(rank_off)
-        keep += [g, out, ro]
-        arr[i].grad, arr[i].out, arr[i].D = _ptr(g), _ptr(out), int(g.shape[1])
-        arr[i].rank_off = ro.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
-        assert tuple(g.shape) == (int(ro[-1]), g.shape[1]) and (out is None or out.shape == g.shape), "a gradient of another shape than its ranks'"
+        ro = tuple(rank_off)            # one table for all layers of the same ranks
+        if ro not in tables:
+            tables[ro] = (ctypes.c_int32 * len(ro))(*map(int, ro))
+        keep += [g, out]
+        a = arr[i]
+        a.grad, a.out, a.D, a.rank_off = _ptr(g), _ptr(out), g.shape[1], tables[ro]
+        assert g.shape[0] == ro[-1] and len(g.shape) == 2 and (out is None or out.shape == g.shape), "a gradient of another shape than its ranks'"
+    keep += tables.values()
     return arr, keep
 
 

@@ -99,7 +99,7 @@ lobra_status make_set(const lobra_grad_tensor* tensors, int32_t n_tensors, int32
         if (n >= int64_t(1) << 40) return LOBRA_ERR_SHAPE;
         if (n > 0 && !g.grad) return LOBRA_ERR_NULL;
         if (!aligned16(g.grad) || !aligned16(g.out)) return LOBRA_ERR_ALIGN;
-        total += n;
+        if ((total += n) >= int64_t(1) << 56) return LOBRA_ERR_SHAPE;
     }
     const int64_t per = piece_elements(total);
     if (total / per + int64_t(n_tensors) * n_tasks >= int64_t(1) << 23) return LOBRA_ERR_SHAPE;     // (a launch holds less than 2^32 threads)
