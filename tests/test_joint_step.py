@@ -1,0 +1,102 @@
+"""The joint step of paper_2509_01193_amd/joint_step.py: all its calls together against the same step in 64 bits on the CPU.
+
+Tolerance: every call holds fp32 results to 1e-5 of the largest; a gradient has some 20 calls behind it (forward and backward of two blocks
+and the head), so 2e-4 of its tensor's largest."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(step, tokens, target, seg_off, seg_task, dlogp):
+    """logp [T] and the gradients of sum(dlogp logp), by autograd in 64 bits."""
+    T, n, d, f = step.T, step.n_tasks, step.d, step.f
+    up = lambda t: t.detach().double().cpu()
+    task = torch.full((T,), -1)
+    for i, t in enumerate(seg_task):
+        task[seg_off[i]:seg_off[i + 1]] = t
+    leaves = []
+
+    def norm(v):
+        return v / torch.sqrt((v * v).mean(dim=1, keepdim=True) + 1e-5)
+
+    def adapted(x, W, A, B, off, parts):
+        y = x @ W
+        out = []
+        for t in range(n):
+            a, b = A[off[t]:off[t + 1]].chunk(parts), B[off[t]:off[t + 1]].chunk(parts)
+            out.append(torch.cat([(x @ ai.T) @ bi for ai, bi in zip(a, b)], dim=1) * (2.0 * (task == t).double()[:, None]))
+        return y + sum(out)
+
+    r = up(step.embedding)[tokens.cpu()]
+    for blk in step.blocks:
+        p = {k: up(blk[k]).requires_grad_() for k in ("A_gu", "B_gu", "A_down", "B_down", "gate")}
+        leaves.append(p)
+        gu = adapted(norm(r), up(blk["W_gu"]), p["A_gu"], p["B_gu"], step.rank_off2, 2)
+        b = adapted(torch.nn.functional.silu(gu[:, :f]) * gu[:, f:], up(blk["W_down"]), p["A_down"], p["B_down"], step.rank_off, 1)
+        gate = torch.cat([p["gate"], torch.ones(1, d, dtype=torch.float64)])[task]     # (-1: the row of ones)
+        r = r + gate * norm(b)
+    logits = norm(r) @ up(step.head)
+    tgt = target.cpu().long()
+    has = (tgt >= 0) & (tgt < step.vocab)
+    logp = torch.log_softmax(logits, dim=1).gather(1, tgt.clamp(0, step.vocab - 1)[:, None])[:, 0] * has
+    (logp * dlogp.double().cpu()).sum().backward()
+    return logp.detach(), leaves
+
+
+def close(got, ref, what, tol=2e-4):
+    err, top = float((got.double().cpu() - ref).abs().max()), float(ref.abs().max())
+    assert math.isfinite(err) and err <= tol * top, "%s: %g of %g" % (what, err, top)
+
+
+def test_gradients_of_the_whole_step_and_serving():
+    from paper_2509_01193_amd.joint_step import JointStep
+    seg_off, seg_task = [0, 17, 30, 31, 45], [1, 0, -1, 1]
+    step = JointStep("f32", 64, 96, 104, 2, [8, 16], seg_off, seg_task)
+    gen = torch.Generator().manual_seed(3)
+    for blk in step.blocks:
+        for k in ("B_gu", "B_down"):
+            blk["master_" + k].copy_(torch.randn(blk[k].shape, generator=gen) * 0.1)
+            blk[k].copy_(blk["master_" + k])
+        blk["gate32"].copy_(torch.randn(blk["gate"].shape, generator=gen))
+        blk["gate"].copy_(blk["gate32"])
+    tokens = torch.randint(104, (45,), generator=gen).cuda()
+    target = torch.randint(104, (45,), generator=gen).int()
+    target[5], target[40] = -100, 104
+    target = target.cuda()
+    dlogp = torch.randn(45, generator=gen).cuda()
+    logp, leaves = reference(step, tokens, target, seg_off, seg_task, dlogp)
+    got = step.forward(tokens, target).clone()
+    step.backward(target, dlogp)
+    torch.cuda.synchronize()
+    close(got, logp, "logp")
+    for i, (blk, p) in enumerate(zip(step.blocks, leaves)):
+        for k, v in p.items():
+            close(blk["d" + k], v.grad, "block %d, d%s" % (i, k))
+    # the tasks' gradient norms, and a step that is no longer than the limit allows
+    step.max_norm.copy_(torch.tensor([1e-3, 1e9]))
+    step.update()
+    for t in range(2):
+        sq = sum(float((p[k].grad[o[t]:o[t + 1]] ** 2).sum()) for p in leaves
+                 for k, o in (("A_gu", step.rank_off2), ("B_gu", step.rank_off2), ("A_down", step.rank_off), ("B_down", step.rank_off), ("gate", [0, 1, 2])))
+        assert abs(float(step.norm[t]) - math.sqrt(sq)) <= 2e-4 * math.sqrt(sq)
+        want = 1e-3 / math.sqrt(sq) if t == 0 else 1.0
+        assert abs(float(step.clip_scale[t]) - want) <= 4e-4 * want
+    # the same tokens of the updated adapters, as a batch and one at a time
+    again = step.forward(tokens, target).clone()
+    top = torch.empty(2, 1, device="cuda"), torch.empty(2, 1, dtype=torch.int32, device="cuda")
+    step.batch([0, 1, 2], [0, 1], train=False)
+    one = step.forward(tokens[[20, 2]], target[[20, 2]], top)
+    close(one, again[[20, 2]].double().cpu(), "one token at a time")
+    assert torch.equal(top[1][:, 0].long(), step.logits.argmax(dim=1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_example_learns(dtype, capsys):
+    from paper_2509_01193_amd import joint_step
+    losses = joint_step.main(["--dtype", dtype, "--steps", "15", "--width", "256", "--ffn", "512", "--tokens", "300", "--new-tokens", "2"])
+    assert len(losses) == 15 and all(math.isfinite(v) for row in losses for v in row)
+    assert all(last < first for first, last in zip(losses[0], losses[-1]))
