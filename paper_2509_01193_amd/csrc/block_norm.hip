@@ -6,8 +6,7 @@
 //     dgate_t = alpha w_post sum_t g bh   dw_post = alpha sum gate_t g bh   dw_pre = sum dx rh
 // The two means of backward are one reduction: with s1 = sum u rh, s2 = sum q bh (dr' + m u), s3 = sum q bh rh, mean(u rh) = s1 / d and
 // mean(q g bh) = (s2 - m s1 / d s3) / d.
-// A row lives in the registers of a team of threads - a wave, or a workgroup - from its read to its write; rows wider than a workgroup
-// holds are read again instead.  Backward's teams take neighbouring rows and keep the sums over tokens in registers from row to row; they
+// A row lives in the registers of a team of threads - a wave, or a workgroup of up to 1024 - from its read to its write.  Backward's teams take neighbouring rows and keep the sums over tokens in registers from row to row; they
 // write them out where their rows end, the gate's also where a segment ends (slot: team + segment, which no two runs share), and a second
 // launch adds them in order.
 // Bound: memory, 4 T d elements forward and 6 T d backward.
@@ -84,15 +83,16 @@ template <typename E> struct NormArgs {
 // task of a row, -1: none
 __device__ __forceinline__ int32_t row_task(const PlanDev& pd, int32_t row) { return pd.cseg_task[segment_of_row(pd, row)]; }
 
-// I pieces of N elements per thread hold a row of up to NT I N; BT / NT teams per workgroup, a row each.
+// I pieces of N elements per thread hold a row of up to NT I N; BT / NT teams per workgroup, a row each, from row0 on.
 template <typename E, int N, int NT, int I>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT)
-void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a)
+void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a, int32_t row0)
 {
     constexpr int BT = NT < 256 ? 256 : NT;
     __shared__ float lds[2][NT / 64];
-    const int32_t row = xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x)) * (BT / NT) + int32_t(threadIdx.x) / NT, t = threadIdx.x % NT;
-    if (row >= pd.T) return;                          // (whole waves; with NT > 64 a workgroup has one row)
+    const int64_t at = row0 + int64_t(xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x))) * (BT / NT) + int32_t(threadIdx.x) / NT;
+    if (at >= pd.T) return;                           // (whole waves; with NT > 64 a workgroup has one row)
+    const int32_t row = int32_t(at), t = threadIdx.x % NT;
     const size_t base = size_t(row) * a.d;
     float v[I][N], bv[I][N];
     float sums[1];
@@ -336,7 +336,7 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
     }
 }
 
-// Adds the partial sums up, in order: y = 0 and 1: the gains', over the teams; y = 2 + t: task t's gate's, over the runs of its segments
+// Adds the partial sums up, in order: first + y = 0 and 1: the gains', over the teams; first + y = 2 + t: task t's gate's, over the runs of its segments
 // (segment k's runs are the teams from the one with its first row to the one with its last, their slots one behind the other).  64
 // columns by 16 lanes, of which four take different segments.  (Segment after segment by all lanes, each segment's reads waited for before
 // the next one's task is known, 41 segments took 13 us instead of 8.)
@@ -344,13 +344,13 @@ template <typename E>
 __global__ __launch_bounds__(1024)
 void block_norm_sum_kernel(PlanDev pd, const float* __restrict__ part_gate, const float* __restrict__ part_post, const float* __restrict__ part_pre,
                            int32_t d, int32_t teams, int32_t rows, float alpha, const E* __restrict__ w_post, float* __restrict__ dgate,
-                           float* __restrict__ dw_post, float* __restrict__ dw_pre, int accumulate)
+                           float* __restrict__ dw_post, float* __restrict__ dw_pre, int accumulate, int32_t first)
 {
     __shared__ float lds[16][64];
     __shared__ int2 runs[1024];                       // first slot and slots of the task's segments among 1024
     __shared__ int32_t found[16];
     const int32_t col = int32_t(blockIdx.x) * 64 + (threadIdx.x & 63), lane = threadIdx.x >> 6;
-    const int32_t what = blockIdx.y;
+    const int32_t what = first + int32_t(blockIdx.y);
     float* out = what == 0 ? dw_post : what == 1 ? dw_pre : dgate;
     if (!out) return;                                 // (uniform)
     float s = 0.f;
@@ -440,14 +440,18 @@ template <typename E, int N, int NT, int I> struct Launch {
     static void fwd(const PlanDev& pd, const NormArgs<E>& a, hipStream_t st)
     {
         constexpr int BT = NT < 256 ? 256 : NT;
-        block_norm_fwd_kernel<E, N, NT, I><<<dim3(uint32_t((int64_t(pd.T) + BT / NT - 1) / (BT / NT))), BT, 0, st>>>(pd, a);
+        constexpr int64_t most = int64_t(1) << 21;    // rows of a launch, which holds less than 2^32 threads
+        for (int64_t row0 = 0; row0 < pd.T; row0 += most) {
+            const int64_t rows = pd.T - row0 < most ? pd.T - row0 : most;
+            block_norm_fwd_kernel<E, N, NT, I><<<dim3(uint32_t((rows + BT / NT - 1) / (BT / NT))), BT, 0, st>>>(pd, a, int32_t(row0));
+        }
     }
     static void bwd(const PlanDev& pd, const NormGradArgs<E>& a, bool sums, int32_t teams, hipStream_t st)
     {
         constexpr int BT = NT < 256 ? 256 : NT;
         const dim3 grid(uint32_t((teams + BT / NT - 1) / (BT / NT)));
-        // six tensors beyond the 256 MB infinity cache (us, plain / past the caches: 16384 x 4096 bf16, 805 MB, with the forward pass in front of it 313 / 275; 2999 x 1025 fp32,
-        // 74 MB, 26 / 33)
+        // six tensors beyond the 256 MB infinity cache (us, plain / past the caches: 16384 x 4096 bf16, 805 MB, with the forward pass in
+        // front of it 313 / 275; 2999 x 1025 fp32, 74 MB, 26 / 33)
         const bool once = N > 1 && size_t(pd.T) * size_t(a.d) * sizeof(E) * 6 > (size_t(256) << 20);
         if (sums) {
             if (once) block_norm_bwd_kernel<E, N, NT, I, true, N != 1><<<grid, BT, 0, st>>>(pd, a);
@@ -531,10 +535,11 @@ hipError_t bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r_
     a.alpha = bn.alpha;
     a.post = bn.post;
     if (pd.T > 0) with_deal<E>(dl, [&](auto l) { l.bwd(pd, a, sums, teams, st); });
-    if (sums)
-        block_norm_sum_kernel<E><<<dim3(uint32_t((pd.d_in + 63) / 64), uint32_t(dgate ? 2 + pd.n_tasks : 2)), 1024, 0, st>>>(
+    const int32_t outs = !sums ? 0 : dgate ? 2 + pd.n_tasks : 2, most = 1 << 15;         // (a grid's y is below 2^16)
+    for (int32_t first = 0; first < outs; first += most)
+        block_norm_sum_kernel<E><<<dim3(uint32_t((pd.d_in + 63) / 64), uint32_t(outs - first < most ? outs - first : most)), 1024, 0, st>>>(
             pd, a.part_gate, a.part_post, a.part_pre, pd.d_in, teams, rows, bn.alpha, bn.post ? a.w_post : nullptr, dgate, dw_post, dw_pre,
-            accumulate ? 1 : 0);
+            accumulate ? 1 : 0, first);
     return hipGetLastError();
 }
 

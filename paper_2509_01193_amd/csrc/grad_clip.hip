@@ -63,34 +63,30 @@ void grad_squares_kernel(const GradPiece* __restrict__ pieces, double* __restric
 // Workgroup t: task t's sum, norm and factor.  joint: one workgroup, the sum of all (clip_scale may be grad_scale, which nobody
 // else reads any more by then).
 __global__ __launch_bounds__(NT)
-void grad_factor_kernel(const double* __restrict__ partial, const int32_t* __restrict__ task_piece, int32_t n_tasks, const float* __restrict__ max_norm,
-                        const float* grad_scale, const int32_t* step, float* __restrict__ norm, float* clip_scale, int32_t* step_out, int joint,
-                        float* __restrict__ scale)
+void grad_factor_kernel(const GradPiece* __restrict__ pieces, const double* __restrict__ partial, const int32_t* __restrict__ task_piece, int32_t n_tasks,
+                        const float* __restrict__ max_norm, const float* grad_scale, const int32_t* step, float* __restrict__ norm, float* clip_scale,
+                        int32_t* step_out, int joint, float* __restrict__ scale)
 {
     __shared__ double lds[NT / 64];
-    auto task_square = [&](int32_t k) {
-        double s = 0.;
-        for (int32_t i = task_piece[k] + int32_t(threadIdx.x); i < task_piece[k + 1]; i += NT) s += partial[i];
-        const double f = grad_scale ? double(grad_scale[k]) : 1.;
-        return f * f * block_sum(s, lds);
-    };
-    double square = 0.;
-    if (joint) {
-        for (int32_t k = 0; k < n_tasks; ++k) square += task_square(k);
-    } else {
-        square = task_square(blockIdx.x);
-        if (threadIdx.x != 0) return;
+    auto factor = [&](int32_t k) { return grad_scale ? double(grad_scale[k]) : 1.; };
+    const int32_t own = joint ? 0 : int32_t(blockIdx.x), end = task_piece[joint ? n_tasks : own + 1];
+    double s = 0.;
+    for (int32_t i = task_piece[own] + int32_t(threadIdx.x); i < end; i += NT) {
+        const double f = joint ? factor(pieces[i].task) : 1.;
+        s = fma(f * f, partial[i], s);
     }
+    const double f = joint ? 1. : factor(own), square = f * f * block_sum(s, lds);
+    if (!joint && threadIdx.x != 0) return;
     const double n = sqrt(square);
     const bool finite = n <= double(3.402823466e38f);       // (a norm that fp32 does not hold is none)
     for (int32_t t = joint ? int32_t(threadIdx.x) : int32_t(blockIdx.x); t < n_tasks; t += joint ? NT : n_tasks) {
         const float gs = grad_scale ? grad_scale[t] : 1.f, most = max_norm ? max_norm[t] : -1.f;
-        float f = gs;
-        if (most >= 0.f && n > double(most)) f = float(double(gs) * (double(most) / n));
-        if (!finite) f = 0.f;
-        scale[t] = f;
+        float c = gs;
+        if (most >= 0.f && n > double(most)) c = float(double(gs) * (double(most) / n));
+        if (!finite) c = 0.f;
+        scale[t] = c;
         if (norm) norm[t] = float(n);
-        if (clip_scale) clip_scale[t] = f;
+        if (clip_scale) clip_scale[t] = c;
         if (step_out) step_out[t] = finite ? step[t] : 0;
     }
 }
@@ -141,7 +137,7 @@ hipError_t grad_clip(const GradPiece* pieces, const int32_t* task_piece, int32_t
                      double* partial, float* scale, hipStream_t st)
 {
     if (n_pieces > 0) (once ? grad_squares_kernel<true> : grad_squares_kernel<false>)<<<dim3(uint32_t(n_pieces)), NT, 0, st>>>(pieces, partial);
-    grad_factor_kernel<<<dim3(joint ? 1u : uint32_t(n_tasks)), NT, 0, st>>>(partial, task_piece, n_tasks, max_norm, grad_scale, step, norm, clip_scale, step_out,
+    grad_factor_kernel<<<dim3(joint ? 1u : uint32_t(n_tasks)), NT, 0, st>>>(pieces, partial, task_piece, n_tasks, max_norm, grad_scale, step, norm, clip_scale, step_out,
                                                               joint ? 1 : 0, scale);
     if (any_out && n_pieces > 0) grad_scale_kernel<<<dim3(uint32_t(n_pieces)), NT, 0, st>>>(pieces, scale);
     return hipGetLastError();
