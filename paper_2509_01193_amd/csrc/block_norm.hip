@@ -7,9 +7,11 @@
 // The two means of backward are one reduction: with s1 = sum u rh, s2 = sum q bh (dr' + m u), s3 = sum q bh rh, mean(u rh) = s1 / d and
 // mean(q g bh) = (s2 - m s1 / d s3) / d.
 // A row lives in the registers of a team of threads - a wave, or a workgroup of up to 1024 - from its read to its write.  Backward's teams take neighbouring rows and keep the sums over tokens in registers from row to row; they
-// write them out where their rows end, the gate's also where a segment ends (slot: team + segment, which no two runs share), and a second
-// launch adds them in order.
+// write them out where their rows end, the gate's also where a segment ends (slot: team + segment, which no two runs share; the slots'
+// tasks stand beside them), and a second launch adds them in order.
 // Bound: memory, 4 T d elements forward and 6 T d backward.
+#include <algorithm>
+
 #include "kernels.h"
 #include "row_common.h"
 
@@ -170,6 +172,7 @@ template <typename E> struct NormGradArgs {
     const float *rstd_post, *rstd_pre;
     E *dr, *db;
     float *part_gate, *part_post, *part_pre;          // [teams + nseg][d], [teams][d], [teams][d], or NULL
+    int32_t* slot_task;                               // [teams + nseg]: whose a slot of part_gate is
     int32_t d, rows;                                  // rows: of a team
     float alpha;
     bool post;
@@ -197,11 +200,14 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
     const bool gated = a.gate != nullptr;             // the rows' tasks matter
     int32_t seg = gated ? segment_of_row(pd, row0) : 0;
     int32_t seg_end = gated ? pd.cseg_off[seg + 1] : row1, task = gated ? pd.cseg_task[seg] : -1;
+    // (a segment that begins with a team's first row leaves a slot between its run and the one before)
+    if (SUMS && a.part_gate && t == 0 && team > 0 && pd.cseg_off[seg] == row0) a.slot_task[team + seg - 1] = -1;
     // gains and the task's gate stay in registers as they are in memory, and a row is fetched while the one before is worked on
     typedef Piece<E, N> P;
     typename P::Raw w_post[I], w_pre[I], w_gate[I];
     auto end_run = [&]() {
         if constexpr (SUMS) {
+            if (a.part_gate && t == 0) a.slot_task[team + seg] = task;
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int32_t c = (t + i * NT) * N;
@@ -336,20 +342,20 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
     }
 }
 
-// Adds the partial sums up, in order: first + y = 0 and 1: the gains', over the teams; first + y = 2 + t: task t's gate's, over the runs of its segments
-// (segment k's runs are the teams from the one with its first row to the one with its last, their slots one behind the other).  64
-// columns by 16 lanes, of which four take different segments.  (Segment after segment by all lanes, each segment's reads waited for before
-// the next one's task is known, 41 segments took 13 us instead of 8.)
-template <typename E>
+// Adds the partial sums up, in order: first + y = 0 and 1: the gains', over the teams; first + y = 2 + t: task t's gate's, over its slots,
+// which are gathered 1024 slots at a time.  COLS columns by 1024 / COLS lanes.
+template <typename E, int COLS>
 __global__ __launch_bounds__(1024)
-void block_norm_sum_kernel(PlanDev pd, const float* __restrict__ part_gate, const float* __restrict__ part_post, const float* __restrict__ part_pre,
-                           int32_t d, int32_t teams, int32_t rows, float alpha, const E* __restrict__ w_post, float* __restrict__ dgate,
-                           float* __restrict__ dw_post, float* __restrict__ dw_pre, int accumulate, int32_t first)
+void block_norm_sum_kernel(const float* __restrict__ part_gate, const float* __restrict__ part_post, const float* __restrict__ part_pre,
+                           const int32_t* __restrict__ slot_task, int32_t d, int32_t teams, int32_t slots, float alpha, const E* __restrict__ w_post,
+                           float* __restrict__ dgate, float* __restrict__ dw_post, float* __restrict__ dw_pre, int accumulate, int32_t first)
 {
-    __shared__ float lds[16][64];
-    __shared__ int2 runs[1024];                       // first slot and slots of the task's segments among 1024
+    constexpr int LANES = 1024 / COLS;
+    __shared__ float lds[16][COLS];
+    __shared__ int32_t own[1024];                     // the task's slots among 1024
     __shared__ int32_t found[16];
-    const int32_t col = int32_t(blockIdx.x) * 64 + (threadIdx.x & 63), lane = threadIdx.x >> 6;
+    const int32_t tid = threadIdx.x, wave = tid >> 6;
+    const int32_t col = int32_t(blockIdx.x) * COLS + tid % COLS, lane = tid / COLS;
     const int32_t what = first + int32_t(blockIdx.y);
     float* out = what == 0 ? dw_post : what == 1 ? dw_pre : dgate;
     if (!out) return;                                 // (uniform)
@@ -359,44 +365,38 @@ void block_norm_sum_kernel(PlanDev pd, const float* __restrict__ part_gate, cons
         const float* p = what == 0 ? part_post : part_pre;
         if (col < d)
 #pragma unroll 8
-            for (int32_t k = lane; k < teams; k += 16) s += p[size_t(k) * d + col];
+            for (int32_t k = lane; k < teams; k += LANES) s += p[size_t(k) * d + col];
     } else {
         any = false;
-        for (int32_t base = 0; base < pd.nseg; base += 1024) {
-            const int32_t k = base + int32_t(threadIdx.x);
-            const bool mine = k < pd.nseg && pd.cseg_task[k] == what - 2;
+        for (int32_t base = 0; base < slots; base += 1024) {
+            const bool mine = base + tid < slots && slot_task[base + tid] == what - 2;
             const uint64_t mask = __ballot(mine);
-            if ((threadIdx.x & 63) == 0) found[lane] = __popcll(mask);
+            if ((tid & 63) == 0) found[wave] = __popcll(mask);
             __syncthreads();
             int32_t at = 0, n = 0;
 #pragma unroll
             for (int w = 0; w < 16; ++w) {
-                at += w < lane ? found[w] : 0;
+                at += w < wave ? found[w] : 0;
                 n += found[w];
             }
-            if (mine) {
-                const int32_t w0 = pd.cseg_off[k] / rows, w1 = (pd.cseg_off[k + 1] - 1) / rows;
-                runs[at + __popcll(mask & ((uint64_t(1) << (threadIdx.x & 63)) - 1))] = int2{w0 + k, w1 - w0 + 1};
-            }
+            if (mine) own[at + __popcll(mask & ((uint64_t(1) << (tid & 63)) - 1))] = base + tid;
             __syncthreads();
             any = any || n > 0;
             if (col < d)
-                for (int32_t q = lane & 3; q < n; q += 4) {
-                    const int2 run = runs[q];
-                    const float* p = part_gate + size_t(run.x) * d + col;
-#pragma unroll 4
-                    for (int32_t w = lane >> 2; w < run.y; w += 4) s += p[size_t(w) * d];
-                }
+#pragma unroll 8
+                for (int32_t q = lane; q < n; q += LANES) s += part_gate[size_t(own[q]) * d + col];
             __syncthreads();
         }
         out += size_t(what - 2) * d;
     }
-    lds[lane][threadIdx.x & 63] = s;
+#pragma unroll
+    for (int m = COLS; m < 64; m <<= 1) s += __shfl_xor(s, m);
+    if ((tid & 63) < COLS) lds[wave][tid % COLS] = s;
     __syncthreads();
-    if (lane != 0 || col >= d) return;
+    if (tid >= COLS || col >= d) return;
     s = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += lds[k][threadIdx.x];
+    for (int w = 0; w < 16; ++w) s += lds[w][tid];
     if (what >= 2) s *= w_post ? alpha * Elem<E>::load(w_post, size_t(col)) : alpha;
     if (accumulate) {
         if (any) out[col] += s;
@@ -428,12 +428,19 @@ Deal deal(int dtype, int32_t d)
     return {1024, 4, n};
 }
 
-// Teams of the backward kernel and their rows: some 16 waves per compute unit, and at least eight rows a team, whose sums are written
-// once (T / rows fp32 rows per sum next to T rows of six bf16 ones).
-int32_t team_rows(const Deal& dl, int64_t T)
+// Columns of a workgroup of the sum: a line's 64, or 16 of narrow rows, which would make too few workgroups of 64 (us of both launches, 64 /
+// 16: 12527 x 128 27 / 25, 9181 x 64 25 / 22, 8000 x 1024 37 / 37, 261 x 1920 22 / 25, 4000 x 4096 58 / 65).
+constexpr int32_t kNarrow = 1024;
+
+// Rows of a team of the backward kernel: what makes some 16 waves per compute unit.  With sums over tokens, which a team writes once (T /
+// rows fp32 rows per sum next to T rows of six bf16 ones) and the second launch reads, at least eight where that leaves 256 teams, fewer
+// where it does not: a team's rows are a chain (us with at least 8 / 4 / 2 / 1: 261 x 1920 22 / 17 / 15 / 16, 1000 x 4096 35 / 31 / 37 /
+// 37, 2000 x 4096 40 / 45 / 45 / 45; without sums 13 / 8 / 5 / 4, 19 / 14 / 12 / 12, 23 / 21 / 21 / 21).
+int32_t team_rows(const Deal& dl, int64_t T, bool sums)
 {
     const int64_t teams = 4096 / (dl.nt / 64), rows = (T + teams - 1) / teams;
-    return int32_t(rows < 8 ? 8 : rows);
+    const int64_t least = sums ? std::min<int64_t>(8, (T + 255) / 256) : 1;
+    return int32_t(std::max<int64_t>(std::max<int64_t>(rows, least), 1));
 }
 
 template <typename E, int N, int NT, int I> struct Launch {
@@ -512,7 +519,8 @@ hipError_t bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r_
                hipStream_t st)
 {
     const Deal dl = deal(dtype, pd.d_in);
-    const int32_t rows = team_rows(dl, pd.T), teams = int32_t((int64_t(pd.T) + rows - 1) / rows);
+    const bool sums = dgate || dw_post || dw_pre;
+    const int32_t rows = team_rows(dl, pd.T, sums), teams = int32_t((int64_t(pd.T) + rows - 1) / rows);
     NormGradArgs<E> a;
     a.r_out = static_cast<const E*>(r_out);
     a.b = bn.block ? static_cast<const E*>(b) : nullptr;
@@ -525,21 +533,24 @@ hipError_t bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r_
     a.rstd_pre = rstd_pre;
     a.dr = static_cast<E*>(dr);
     a.db = static_cast<E*>(db);
-    const bool sums = dgate || dw_post || dw_pre;
     const size_t row = size_t(pd.d_in);
     a.part_gate = dgate ? part : nullptr;
     a.part_post = dw_post ? part + size_t(teams + pd.nseg) * row : nullptr;
     a.part_pre = dw_pre ? part + size_t(2 * size_t(teams) + pd.nseg) * row : nullptr;
+    a.slot_task = reinterpret_cast<int32_t*>(part + (size_t(3) * size_t(teams) + size_t(pd.nseg)) * row);
     a.d = pd.d_in;
     a.rows = rows;
     a.alpha = bn.alpha;
     a.post = bn.post;
     if (pd.T > 0) with_deal<E>(dl, [&](auto l) { l.bwd(pd, a, sums, teams, st); });
     const int32_t outs = !sums ? 0 : dgate ? 2 + pd.n_tasks : 2, most = 1 << 15;         // (a grid's y is below 2^16)
+    const bool narrow = pd.d_in <= kNarrow;
+    const int32_t cols = narrow ? 16 : 64;
     for (int32_t first = 0; first < outs; first += most)
-        block_norm_sum_kernel<E><<<dim3(uint32_t((pd.d_in + 63) / 64), uint32_t(outs - first < most ? outs - first : most)), 1024, 0, st>>>(
-            pd, a.part_gate, a.part_post, a.part_pre, pd.d_in, teams, rows, bn.alpha, bn.post ? a.w_post : nullptr, dgate, dw_post, dw_pre,
-            accumulate ? 1 : 0, first);
+        (narrow ? block_norm_sum_kernel<E, 16> : block_norm_sum_kernel<E, 64>)
+            <<<dim3(uint32_t((pd.d_in + cols - 1) / cols), uint32_t(outs - first < most ? outs - first : most)), 1024, 0, st>>>(
+                a.part_gate, a.part_post, a.part_pre, a.slot_task, pd.d_in, teams, teams + pd.nseg - 1, bn.alpha, bn.post ? a.w_post : nullptr,
+                dgate, dw_post, dw_pre, accumulate ? 1 : 0, first);
     return hipGetLastError();
 }
 
@@ -547,8 +558,8 @@ hipError_t bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r_
 
 size_t block_norm_part_bytes(int64_t T, int32_t d, int32_t nseg, int dtype)
 {
-    const int64_t rows = team_rows(deal(dtype, d), T), teams = (T + rows - 1) / rows;
-    return (size_t(3 * teams) + size_t(nseg)) * size_t(d) * sizeof(float);
+    const int64_t rows = team_rows(deal(dtype, d), T, true), teams = (T + rows - 1) / rows;
+    return (size_t(3 * teams) + size_t(nseg)) * size_t(d) * sizeof(float) + size_t(teams + nseg) * sizeof(int32_t);
 }
 
 hipError_t block_norm_fwd(const PlanDev& pd, int dtype, const BlockNorm& bn, const void* r, const void* b, void* r_out, void* x,

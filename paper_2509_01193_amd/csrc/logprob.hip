@@ -175,13 +175,15 @@ __device__ void alternatives(const E* row, const RowShape& sh, int32_t V, float 
     if (tid == 0) count = seers = 0;
     __syncthreads();
     if (tid < 64) {
-        // (a short loop: code that runs once is fetched about as slowly as it is long)
-        float v = group_max[lane], m = 0.f;
-        for (int32_t r = 0; r < k; ++r) {
-            m = wave_max(v);
-            v = lane == __builtin_ctzll(__ballot(v == m)) ? -INFINITY : v;
+        // whoever has k - 1 others in front of it (a short loop: code that runs once is fetched about as slowly as it is long)
+        const float v = group_max[lane];
+        int32_t in_front = 0;
+#pragma unroll 8
+        for (int32_t o = 0; o < 64; ++o) {
+            const float other = group_max[o];
+            in_front += other > v || (other == v && o < lane) ? 1 : 0;
         }
-        if (lane == 0) tau_s = m;
+        if (in_front == k - 1) tau_s = v;
     }
     __syncthreads();
     const float tau = tau_s;
