@@ -21,35 +21,47 @@ using namespace rows;
 
 namespace {
 
-// N consecutive elements of E: a 16-byte packet, or a single element where rows keep no such alignment.  Raw: as they are in memory.
-template <typename E, int N> struct Piece {
-    typedef u32x4 Raw;
-    static __device__ __forceinline__ Raw fetch(const E* p) { return *reinterpret_cast<const u32x4*>(p); }
-    template <bool ONCE> static __device__ __forceinline__ Raw fetch_row(const E* p)
+typedef u32x4 AnyPacket __attribute__((aligned(4)));       // (global memory is read and written in 16 bytes from any multiple of 4)
+
+// A 16-byte packet of a row of d elements, of which `left` are left from the packet's first one on.  RAGGED: rows whose width is no multiple of a
+// packet (fp32): packets begin at any element, and the row's last one is read and written element by element.
+template <typename E, bool RAGGED> struct Piece {
+    static constexpr int N = Packet<E>::N;
+    template <bool ONCE> static __device__ __forceinline__ u32x4 fetch_row(const E* p, int32_t left)
     {
-        return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)) : fetch(p);
+        if (RAGGED && left < N) {
+            u32x4 q = zero();
+#pragma unroll
+            for (int e = 0; e < N - 1; ++e)
+                if (e < left) q[e] = __float_as_uint(Elem<E>::load(p, size_t(e)));
+            return q;
+        }
+        if constexpr (RAGGED) return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const AnyPacket*>(p)) : *reinterpret_cast<const AnyPacket*>(p);
+        else return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)) : *reinterpret_cast<const u32x4*>(p);
     }
-    static __device__ __forceinline__ void widen(Raw r, float (&v)[N]) { Packet<E>::widen(r, v); }
-    static __device__ __forceinline__ float widen(Raw r, int i) { return Packet<E>::element(r, i); }
-    static __device__ __forceinline__ Raw zero() { return u32x4{0u, 0u, 0u, 0u}; }
-    static __device__ __forceinline__ void load(const E* p, float (&v)[N]) { widen(fetch(p), v); }
-    static __device__ __forceinline__ void store(E* p, const float (&v)[N]) { *reinterpret_cast<u32x4*>(p) = Packet<E>::narrow(v); }
-    template <bool ONCE> static __device__ __forceinline__ void store_row(E* p, const float (&v)[N])
+    static __device__ __forceinline__ u32x4 fetch(const E* p, int32_t left) { return fetch_row<false>(p, left); }
+    static __device__ __forceinline__ void widen(u32x4 r, float (&v)[N]) { Packet<E>::widen(r, v); }
+    static __device__ __forceinline__ float widen(u32x4 r, int i) { return Packet<E>::element(r, i); }
+    static __device__ __forceinline__ u32x4 zero() { return u32x4{0u, 0u, 0u, 0u}; }
+    static __device__ __forceinline__ void load(const E* p, float (&v)[N], int32_t left) { widen(fetch(p, left), v); }
+    template <bool ONCE> static __device__ __forceinline__ void store_row(E* p, const float (&v)[N], int32_t left)
     {
-        if (ONCE) __builtin_nontemporal_store(Packet<E>::narrow(v), reinterpret_cast<u32x4*>(p));
-        else store(p, v);
+        if (RAGGED && left < N) {
+#pragma unroll
+            for (int e = 0; e < N - 1; ++e)
+                if (e < left) Elem<E>::store(p, size_t(e), v[e]);
+            return;
+        }
+        const u32x4 q = Packet<E>::narrow(v);
+        if constexpr (RAGGED) {
+            if (ONCE) __builtin_nontemporal_store(q, reinterpret_cast<AnyPacket*>(p));
+            else *reinterpret_cast<AnyPacket*>(p) = q;
+        } else {
+            if (ONCE) __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(p));
+            else *reinterpret_cast<u32x4*>(p) = q;
+        }
     }
-};
-template <typename E> struct Piece<E, 1> {
-    typedef E Raw;
-    static __device__ __forceinline__ Raw fetch(const E* p) { return *p; }
-    template <bool ONCE> static __device__ __forceinline__ Raw fetch_row(const E* p) { return fetch(p); }
-    static __device__ __forceinline__ void widen(Raw r, float (&v)[1]) { v[0] = Elem<E>::load(&r, 0); }
-    static __device__ __forceinline__ float widen(Raw r, int) { return Elem<E>::load(&r, 0); }
-    static __device__ __forceinline__ Raw zero() { return E(0); }
-    static __device__ __forceinline__ void load(const E* p, float (&v)[1]) { widen(fetch(p), v); }
-    static __device__ __forceinline__ void store(E* p, const float (&v)[1]) { Elem<E>::store(p, 0, v[0]); }
-    template <bool ONCE> static __device__ __forceinline__ void store_row(E* p, const float (&v)[1]) { store(p, v); }
+    static __device__ __forceinline__ void store(E* p, const float (&v)[N], int32_t left) { store_row<false>(p, v, left); }
 };
 // v as the element type holds it
 template <typename E> __device__ __forceinline__ float rounded(float v);
@@ -85,12 +97,13 @@ template <typename E> struct NormArgs {
 // task of a row, -1: none
 __device__ __forceinline__ int32_t row_task(const PlanDev& pd, int32_t row) { return pd.cseg_task[segment_of_row(pd, row)]; }
 
-// I pieces of N elements per thread hold a row of up to NT I N; BT / NT teams per workgroup, a row each, from row0 on.
-template <typename E, int N, int NT, int I>
+// I packets of N elements per thread hold a row of up to NT I N; BT / NT teams per workgroup, a row each, from row0 on.
+template <typename E, bool RAGGED, int NT, int I>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT)
 void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a, int32_t row0)
 {
-    constexpr int BT = NT < 256 ? 256 : NT;
+    typedef Piece<E, RAGGED> P;
+    constexpr int BT = NT < 256 ? 256 : NT, N = P::N;
     __shared__ float lds[2][NT / 64];
     const int64_t at = row0 + int64_t(xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x))) * (BT / NT) + int32_t(threadIdx.x) / NT;
     if (at >= pd.T) return;                           // (whole waves; with NT > 64 a workgroup has one row)
@@ -102,8 +115,8 @@ void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a, int32_t row0)
     for (int i = 0; i < I; ++i) {
         const int32_t c = (t + i * NT) * N;
         if (c < a.d) {
-            Piece<E, N>::load(a.r + base + c, v[i]);
-            if (a.b) Piece<E, N>::load(a.b + base + c, bv[i]);
+            P::load(a.r + base + c, v[i], a.d - c);
+            if (a.b) P::load(a.b + base + c, bv[i], a.d - c);
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e) v[i][e] = bv[i][e] = 0.f;
@@ -131,19 +144,19 @@ void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a, int32_t row0)
             for (int e = 0; e < N; ++e) k[e] = a.alpha;
             if (a.post) {
                 float w[N];
-                Piece<E, N>::load(a.w_post + c, w);
+                P::load(a.w_post + c, w, a.d - c);
 #pragma unroll
                 for (int e = 0; e < N; ++e) k[e] *= w[e] * n;
             }
             if (task >= 0) {
                 float w[N];
-                Piece<E, N>::load(a.gate + size_t(task) * a.d + c, w);
+                P::load(a.gate + size_t(task) * a.d + c, w, a.d - c);
 #pragma unroll
                 for (int e = 0; e < N; ++e) k[e] *= w[e];
             }
 #pragma unroll
             for (int e = 0; e < N; ++e) v[i][e] = rounded<E>(fmaf(k[e], bv[i][e], v[i][e]));
-            Piece<E, N>::store(a.r_out + base + c, v[i]);
+            P::store(a.r_out + base + c, v[i], a.d - c);
         }
     }
     if (!a.w_pre) return;
@@ -160,10 +173,10 @@ void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a, int32_t row0)
         const int32_t c = (t + i * NT) * N;
         if (c >= a.d) continue;
         float w[N];
-        Piece<E, N>::load(a.w_pre + c, w);
+        P::load(a.w_pre + c, w, a.d - c);
 #pragma unroll
         for (int e = 0; e < N; ++e) w[e] = w[e] * (v[i][e] * m);
-        Piece<E, N>::store(a.x + base + c, w);
+        P::store(a.x + base + c, w, a.d - c);
     }
 }
 
@@ -181,11 +194,12 @@ template <typename E> struct NormGradArgs {
 // A team's rows one after the other.  SUMS: the sums over tokens are wanted.  sum_run = sum g bh of a run of rows of one segment (without
 // gates: of all rows): at its end it goes to the gate's partial sums and, times alpha gate_t, into sum_post.
 // ONCE: the rows are more than the caches hold and are read and written past them.
-template <typename E, int N, int NT, int I, bool SUMS, bool ONCE>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT, I * N <= 8 ? 4 : 1)
+template <typename E, bool RAGGED, int NT, int I, bool SUMS, bool ONCE>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT, I == 1 ? 4 : 1)
 void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
 {
-    constexpr int BT = NT < 256 ? 256 : NT;
+    typedef Piece<E, RAGGED> P;
+    constexpr int BT = NT < 256 ? 256 : NT, N = P::N;
     __shared__ float lds[2][3 * (NT / 64)];
     const int32_t team = xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x)) * (BT / NT) + int32_t(threadIdx.x) / NT, t = threadIdx.x % NT;
     const int64_t first = int64_t(team) * a.rows;
@@ -203,8 +217,7 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
     // (a segment that begins with a team's first row leaves a slot between its run and the one before)
     if (SUMS && a.part_gate && t == 0 && team > 0 && pd.cseg_off[seg] == row0) a.slot_task[team + seg - 1] = -1;
     // gains and the task's gate stay in registers as they are in memory, and a row is fetched while the one before is worked on
-    typedef Piece<E, N> P;
-    typename P::Raw w_post[I], w_pre[I], w_gate[I];
+    u32x4 w_post[I], w_pre[I], w_gate[I];
     auto end_run = [&]() {
         if constexpr (SUMS) {
             if (a.part_gate && t == 0) a.slot_task[team + seg] = task;
@@ -213,9 +226,10 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
                 const int32_t c = (t + i * NT) * N;
                 if (c >= a.d) continue;
                 float k[N];
-                Piece<E, N>::widen(w_gate[i], k);
+                P::widen(w_gate[i], k);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
+                    if (RAGGED && c + e >= a.d) break;
                     if (task < 0) k[e] = 1.f;
                     if (a.part_gate) a.part_gate[(size_t(team) + seg) * a.d + c + e] = sum_run[i][e];
                     sum_post[i][e] = fmaf(a.alpha * k[e], sum_run[i][e], sum_post[i][e]);
@@ -225,14 +239,14 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
         }
     };
     struct Row {
-        typename P::Raw dx[I], r[I], dr[I], b[I];
+        u32x4 dx[I], r[I], dr[I], b[I];
         float n, m;
     };
     auto fetch_gate = [&]() {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int32_t c = (t + i * NT) * N;
-            w_gate[i] = c < a.d && task >= 0 ? P::fetch(a.gate + size_t(task) * a.d + c) : P::zero();
+            w_gate[i] = c < a.d && task >= 0 ? P::fetch(a.gate + size_t(task) * a.d + c, a.d - c) : P::zero();
         }
     };
     auto fetch_row = [&](Row& f, int32_t row) {
@@ -243,17 +257,17 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
         for (int i = 0; i < I; ++i) {
             const int32_t c = (t + i * NT) * N;
             const bool in = c < a.d;
-            f.dx[i] = in && a.dx ? P::template fetch_row<ONCE>(a.dx + base + c) : P::zero();
-            f.r[i] = in && a.dx ? P::template fetch_row<ONCE>(a.r_out + base + c) : P::zero();
-            f.dr[i] = in && a.dr_out ? P::template fetch_row<ONCE>(a.dr_out + base + c) : P::zero();
-            f.b[i] = in && a.b ? P::template fetch_row<ONCE>(a.b + base + c) : P::zero();
+            f.dx[i] = in && a.dx ? P::template fetch_row<ONCE>(a.dx + base + c, a.d - c) : P::zero();
+            f.r[i] = in && a.dx ? P::template fetch_row<ONCE>(a.r_out + base + c, a.d - c) : P::zero();
+            f.dr[i] = in && a.dr_out ? P::template fetch_row<ONCE>(a.dr_out + base + c, a.d - c) : P::zero();
+            f.b[i] = in && a.b ? P::template fetch_row<ONCE>(a.b + base + c, a.d - c) : P::zero();
         }
     };
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         const int32_t c = (t + i * NT) * N;
-        w_post[i] = c < a.d && a.post ? P::fetch(a.w_post + c) : P::zero();
-        w_pre[i] = c < a.d && a.dx ? P::fetch(a.w_pre + c) : P::zero();
+        w_post[i] = c < a.d && a.post ? P::fetch(a.w_post + c, a.d - c) : P::zero();
+        w_pre[i] = c < a.d && a.dx ? P::fetch(a.w_pre + c, a.d - c) : P::zero();
     }
     fetch_gate();
     // an element's terms, from how they are in memory: g without the term of its mean
@@ -272,7 +286,7 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
         if (task >= 0) k.q *= P::widen(w_gate[i], e);
         return k;
     };
-    constexpr bool AHEAD = I * int(sizeof(typename P::Raw)) <= 16;       // (the next row does not fit next to larger ones)
+    constexpr bool AHEAD = I == 1;       // (the next row does not fit next to larger ones)
     Row cur, next;
     fetch_row(cur, row0);
     const float inv_d = 1.f / float(a.d);
@@ -320,8 +334,8 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
                 if (a.post) out[e] = cur.n * fmaf(-k.bh, c2, out[e]);
             }
             if (c < a.d) {
-                P::template store_row<ONCE>(a.dr + base + c, g);
-                if (a.b) P::template store_row<ONCE>(a.db + base + c, out);
+                P::template store_row<ONCE>(a.dr + base + c, g, a.d - c);
+                if (a.b) P::template store_row<ONCE>(a.db + base + c, out, a.d - c);
             }
         }
         if (AHEAD) cur = next;
@@ -335,6 +349,7 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
             if (c >= a.d) continue;
 #pragma unroll
             for (int e = 0; e < N; ++e) {
+                if (RAGGED && c + e >= a.d) break;
                 if (a.part_post) a.part_post[size_t(team) * a.d + c + e] = sum_post[i][e];
                 if (a.part_pre) a.part_pre[size_t(team) * a.d + c + e] = sum_pre[i][e];
             }
@@ -407,25 +422,20 @@ void block_norm_sum_kernel(const float* __restrict__ part_gate, const float* __r
 
 // How rows are dealt to threads: a wave holds a row of up to two packets a lane; wider ones take workgroups.
 struct Deal {
-    int32_t nt, i, n;        // threads of a team, pieces of n elements per thread
+    int32_t nt, i;           // threads of a team, packets per thread
+    bool ragged;
 };
 Deal deal(int dtype, int32_t d)
 {
-    const int32_t per = dtype == LOBRA_F32 ? 4 : 8, n = d % per == 0 ? per : 1;
-    const int32_t pieces = (d + n - 1) / n;
-    if (n == 1) {
-        if (pieces <= 256) return {64, 4, 1};
-        if (pieces <= 2048) return {512, 4, 1};
-        if (pieces <= 4096) return {1024, 4, 1};
-        return {1024, 16, 1};
-    }
-    if (pieces <= 64) return {64, 1, n};
-    if (pieces <= 128) return {64, 2, n};
-    if (pieces <= 256) return {256, 1, n};
-    if (pieces <= 512) return {512, 1, n};
-    if (pieces <= 1024) return {1024, 1, n};
-    if (pieces <= 2048) return {1024, 2, n};
-    return {1024, 4, n};
+    const int32_t per = dtype == LOBRA_F32 ? 4 : 8, packets = (d + per - 1) / per;
+    const bool ragged = d % per != 0;                // (bf16 widths are multiples of 8)
+    if (packets <= 64) return {64, 1, ragged};
+    if (packets <= 128) return {64, 2, ragged};
+    if (packets <= 256) return {256, 1, ragged};
+    if (packets <= 512) return {512, 1, ragged};
+    if (packets <= 1024) return {1024, 1, ragged};
+    if (packets <= 2048) return {1024, 2, ragged};
+    return {1024, 4, ragged};
 }
 
 // Columns of a workgroup of the sum: a line's 64, or 16 of narrow rows, which would make too few workgroups of 64 (us of both launches, 64 /
@@ -443,14 +453,14 @@ int32_t team_rows(const Deal& dl, int64_t T, bool sums)
     return int32_t(std::max<int64_t>(std::max<int64_t>(rows, least), 1));
 }
 
-template <typename E, int N, int NT, int I> struct Launch {
+template <typename E, bool RAGGED, int NT, int I> struct Launch {
     static void fwd(const PlanDev& pd, const NormArgs<E>& a, hipStream_t st)
     {
         constexpr int BT = NT < 256 ? 256 : NT;
         constexpr int64_t most = int64_t(1) << 21;    // rows of a launch, which holds less than 2^32 threads
         for (int64_t row0 = 0; row0 < pd.T; row0 += most) {
             const int64_t rows = pd.T - row0 < most ? pd.T - row0 : most;
-            block_norm_fwd_kernel<E, N, NT, I><<<dim3(uint32_t((rows + BT / NT - 1) / (BT / NT))), BT, 0, st>>>(pd, a, int32_t(row0));
+            block_norm_fwd_kernel<E, RAGGED, NT, I><<<dim3(uint32_t((rows + BT / NT - 1) / (BT / NT))), BT, 0, st>>>(pd, a, int32_t(row0));
         }
     }
     static void bwd(const PlanDev& pd, const NormGradArgs<E>& a, bool sums, int32_t teams, hipStream_t st)
@@ -459,36 +469,35 @@ template <typename E, int N, int NT, int I> struct Launch {
         const dim3 grid(uint32_t((teams + BT / NT - 1) / (BT / NT)));
         // six tensors beyond the 256 MB infinity cache (us, plain / past the caches: 16384 x 4096 bf16, 805 MB, with the forward pass in
         // front of it 313 / 275; 2999 x 1025 fp32, 74 MB, 26 / 33)
-        const bool once = N > 1 && size_t(pd.T) * size_t(a.d) * sizeof(E) * 6 > (size_t(256) << 20);
+        const bool once = size_t(pd.T) * size_t(a.d) * sizeof(E) * 6 > (size_t(256) << 20);
         if (sums) {
-            if (once) block_norm_bwd_kernel<E, N, NT, I, true, N != 1><<<grid, BT, 0, st>>>(pd, a);
-            else block_norm_bwd_kernel<E, N, NT, I, true, false><<<grid, BT, 0, st>>>(pd, a);
+            if (once) block_norm_bwd_kernel<E, RAGGED, NT, I, true, true><<<grid, BT, 0, st>>>(pd, a);
+            else block_norm_bwd_kernel<E, RAGGED, NT, I, true, false><<<grid, BT, 0, st>>>(pd, a);
         } else {
-            if (once) block_norm_bwd_kernel<E, N, NT, I, false, N != 1><<<grid, BT, 0, st>>>(pd, a);
-            else block_norm_bwd_kernel<E, N, NT, I, false, false><<<grid, BT, 0, st>>>(pd, a);
+            if (once) block_norm_bwd_kernel<E, RAGGED, NT, I, false, true><<<grid, BT, 0, st>>>(pd, a);
+            else block_norm_bwd_kernel<E, RAGGED, NT, I, false, false><<<grid, BT, 0, st>>>(pd, a);
         }
     }
 };
 
 // f(Launch<...>) of the deal
+template <typename E, bool RAGGED, typename F> void with_team(const Deal& dl, F&& f)
+{
+    if (dl.nt == 64) {
+        if (dl.i == 1) f(Launch<E, RAGGED, 64, 1>{});
+        else f(Launch<E, RAGGED, 64, 2>{});
+    } else if (dl.nt == 256) f(Launch<E, RAGGED, 256, 1>{});
+    else if (dl.nt == 512) f(Launch<E, RAGGED, 512, 1>{});
+    else if (dl.i == 1) f(Launch<E, RAGGED, 1024, 1>{});
+    else if (dl.i == 2) f(Launch<E, RAGGED, 1024, 2>{});
+    else if constexpr (Packet<E>::N == 4) f(Launch<E, RAGGED, 1024, 4>{});
+}
 template <typename E, typename F> void with_deal(const Deal& dl, F&& f)
 {
-    constexpr int N = Packet<E>::N;
-    if (dl.n == 1) {
-        if constexpr (N == 4) {                       // (bf16 widths are multiples of 8)
-            if (dl.nt == 64) f(Launch<E, 1, 64, 4>{});
-            else if (dl.nt == 512) f(Launch<E, 1, 512, 4>{});
-            else if (dl.i == 4) f(Launch<E, 1, 1024, 4>{});
-            else f(Launch<E, 1, 1024, 16>{});
-        }
-    } else if (dl.nt == 64) {
-        if (dl.i == 1) f(Launch<E, N, 64, 1>{});
-        else f(Launch<E, N, 64, 2>{});
-    } else if (dl.nt == 256) f(Launch<E, N, 256, 1>{});
-    else if (dl.nt == 512) f(Launch<E, N, 512, 1>{});
-    else if (dl.i == 1) f(Launch<E, N, 1024, 1>{});
-    else if (dl.i == 2) f(Launch<E, N, 1024, 2>{});
-    else if constexpr (N == 4) f(Launch<E, N, 1024, 4>{});
+    if constexpr (Packet<E>::N == 4) {
+        if (dl.ragged) return with_team<E, true>(dl, f);
+    }
+    with_team<E, false>(dl, f);
 }
 
 template <typename E>
