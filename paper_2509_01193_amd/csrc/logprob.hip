@@ -9,7 +9,10 @@
 // joined over the workgroup at the end.  The row's own maximum is the reference (not a multiple of it in the log2 domain, which would
 // save an instruction): differences of equal logits are 0 at any magnitude, so that rows of the type's lowest value are uniform ones.
 // A workgroup per row; nothing is split over workgroups, since a launch that joins costs more than what a row of 256 KiB takes.
-// Bound: memory; per element some ten VALU slots, four of them the exponential, where the memory's rate leaves 13 to a bf16 element.
+// Bound: memory; per element some ten VALU slots, four of them the exponential, where the memory's rate leaves 13 to a bf16 element.  A row alone
+// is bound by these on its compute unit.  Measured, us: 8190 x 32000 bf16 forward 89 (of 524 MB, 5.9 TB/s; right behind a backward pass, whose
+// gradients are still on their way to memory, 124), backward 206 (of 1048 MB, 5.1 TB/s), over the logits 151; 4096 x 128000 with entropy and 8
+// alternatives 186; 40 x 32000 with 20 of them 9; one row of 32000 5, of 256000 20, with 32 alternatives 8 and 27.
 #include "kernels.h"
 #include "row_common.h"
 
