@@ -1,4 +1,4 @@
-// The gated feed-forward block's forward pass for few tokens (decoding), bf16: the product of up to 64 rows of x with gate and up weights
+// The gated feed-forward block's forward pass for few tokens (decoding), bf16: the product of up to 128 rows of x with gate and up weights
 // as one stream over W, the adapters' down projections in the same launch, and a second launch that adds up, activates and multiplies.
 //     [g | u] = x W + s_t (A_t x) B_t   h = a(g) u
 //
@@ -10,7 +10,9 @@
 // the kernel that does this takes the place of the one that would activate [g | u].
 // The projections H = s_t A_t x are dealt to the same workgroups' waves, four rank rows of a token at a time, while their first K
 // tiles are on their way.  (Workgroups of their own in front of the grid hold up the stream of a compute unit each: 6 us of 44.)
-// Measured (40 tokens, 4096 x 2 x 11008, 8 tasks of rank 16, us): 35.8 and 7.1 (of 180 MB, 5.0 TB/s); W copied as data that is read again 5 more.
+// Measured (4096 x 2 x 11008, 8 tasks of rank 16, us): 40 tokens 36 .. 38 (180 MB, 5.0 TB/s) and 7.5; W copied as data that is read again 5 more.
+// Against the layer's product and an activation behind it (both launches / those): 65 tokens 51 / 67, 128 tokens 63 / 74; 128 tokens of 4096 x 2 x
+// 1376 30 / 41, of 1024 x 2 x 2816 23 / 23.  More tokens leave the ring less than two tiles on their way.
 #include <atomic>
 
 #include "activation.h"
@@ -34,18 +36,20 @@ constexpr int NW = 8;                         // waves
 template <int TB> struct Ring {
     static constexpr int X_BYTES = TB * 16 * KT * 2, STAGE = W_BYTES + X_BYTES;
     static constexpr int D = LDS_MOST / STAGE;
-    static constexpr int NC = 4 + 1;                     // copies per wave and tile: of W, of x (2 TB copies of 8 tokens: the other waves repeat them)
+    static constexpr int XC = (2 * TB + NW - 1) / NW, NC = 4 + XC;         // copies per wave and tile: of x (2 TB copies of 8 tokens: waves left over
+                                                                           // repeat some), and with those of W
 };
 
-// Task of a token, looked up by a whole wave: no more segments than tokens, one per lane.  (A chain of two reads less than segment_of_row,
+// Task of a token, looked up by a whole wave: no more segments than tokens, two per lane.  (A chain of two reads less than segment_of_row,
 // which walks the table.)
-static_assert(kSkinnyTokens <= 64, "a lane per segment");
+static_assert(kSkinnyTokens <= 128, "two segments a lane");
 __device__ __forceinline__ int32_t token_task(const PlanDev& pd, int32_t token)
 {
-    const int lane = threadIdx.x & 63, at = min(lane, pd.nseg - 1);
-    const int32_t end = pd.cseg_off[at + 1], task = pd.cseg_task[at];
-    const int k = __popcll(__ballot(lane < pd.nseg && end <= token));
-    return __builtin_amdgcn_readlane(task, k);
+    const int lane = threadIdx.x & 63;
+    const int32_t a = min(lane, pd.nseg - 1), b = min(64 + lane, pd.nseg - 1);
+    const int32_t enda = pd.cseg_off[a + 1], endb = pd.cseg_off[b + 1], taska = pd.cseg_task[a], taskb = pd.cseg_task[b];
+    const int k = __popcll(__ballot(lane < pd.nseg && enda <= token)) + __popcll(__ballot(64 + lane < pd.nseg && endb <= token));
+    return k < 64 ? __builtin_amdgcn_readlane(taska, k) : __builtin_amdgcn_readlane(taskb, k - 64);
 }
 
 // H[token][row] = s_t (A_t x)[row]: ROWS rank rows of a token at a time, item `wave` of every `waves`, K over a wave's lanes
@@ -115,14 +119,20 @@ void gated_skinny_kernel(PlanDev pd, const uint16_t* __restrict__ x, const uint1
     // Copies of a K tile.  W: copy c holds k rows 2 c and 2 c + 1, 32 chunks of 8 columns each, gate's then up's; chunk n of row k at
     // n ^ kn_swz(k).  x: copy c holds tokens 8 c .. + 7, 8 chunks of 8 k each; chunk n of token i at n ^ swz_row(i).  Rows, columns and
     // tokens that are not there repeat the last one; what they add is cleared or not stored.
-    uint32_t wvo[4], xvo;                            // a whole tile's offsets from its first row and column, and from its first k
+    uint32_t wvo[4], xvo[R::XC];                     // a whole tile's offsets from its first row and column, and from its first k
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
         const int row = 2 * (wave + NW * m) + (lane >> 5), n = (lane & 31) ^ kn_swz(row);
         wvo[m] = (uint32_t(row) * uint32_t(ldw) + uint32_t(8 * (n & 15)) + uint32_t(n >> 4) * uint32_t(f)) * 2u;
     }
-    const int xc = wave % (2 * TB), xi = 8 * xc + (lane >> 3), xn = (lane & 7) ^ swz_row(xi);
-    xvo = (uint32_t(min(xi, T - 1)) * uint32_t(K) + uint32_t(8 * xn)) * 2u;
+    int xc[R::XC], xn[R::XC];
+#pragma unroll
+    for (int m = 0; m < R::XC; ++m) {
+        xc[m] = (wave + NW * m) % (2 * TB);
+        const int xi = 8 * xc[m] + (lane >> 3);
+        xn[m] = (lane & 7) ^ swz_row(xi);
+        xvo[m] = (uint32_t(min(xi, T - 1)) * uint32_t(K) + uint32_t(8 * xn[m])) * 2u;
+    }
     auto copy = [&](const Cursor& u) __attribute__((always_inline)) {
         const int32_t kt = u.kt * KT, c0 = u.tile * COLS;
         const uint32_t stage = lds0 + uint32_t(u.stage) * R::STAGE;
@@ -131,7 +141,8 @@ void gated_skinny_kernel(PlanDev pd, const uint16_t* __restrict__ x, const uint1
         if (kt + KT <= K && c0 + COLS <= f) {        // (uniform)
 #pragma unroll
             for (int m = 0; m < 4; ++m) dma16_once(stage + (wave + NW * m) * 1024, wp, wvo[m]);
-            dma16(stage + W_BYTES + xc * 1024, xp, xvo);
+#pragma unroll
+            for (int m = 0; m < R::XC; ++m) dma16(stage + W_BYTES + xc[m] * 1024, xp, xvo[m]);
             return;
         }
 #pragma unroll
@@ -140,7 +151,8 @@ void gated_skinny_kernel(PlanDev pd, const uint16_t* __restrict__ x, const uint1
             const int32_t col = min(8 * (n & 15), f - 8 - c0) + (n >> 4) * f;
             dma16_once(stage + c * 1024, wp, (uint32_t(min(row, K - 1 - kt)) * uint32_t(ldw) + uint32_t(col)) * 2u);
         }
-        dma16(stage + W_BYTES + xc * 1024, xp, xvo - 2u * uint32_t(8 * xn - min(8 * xn, K - 8 - kt)));
+#pragma unroll
+        for (int m = 0; m < R::XC; ++m) dma16(stage + W_BYTES + xc[m] * 1024, xp, xvo[m] - 2u * uint32_t(8 * xn[m] - min(8 * xn[m], K - 8 - kt)));
     };
 
     // wave w: columns 16 w .. + 15 of gate and of up
@@ -350,7 +362,10 @@ hipError_t gated_skinny_product(const PlanDev& pd, const void* x, const void* W,
     case 1: return launch<1>(pd, c, xp, wp, ap, s, part, H, K, f, st);
     case 2: return launch<2>(pd, c, xp, wp, ap, s, part, H, K, f, st);
     case 3: return launch<3>(pd, c, xp, wp, ap, s, part, H, K, f, st);
-    default: return launch<4>(pd, c, xp, wp, ap, s, part, H, K, f, st);
+    case 4: return launch<4>(pd, c, xp, wp, ap, s, part, H, K, f, st);
+    case 5:
+    case 6: return launch<6>(pd, c, xp, wp, ap, s, part, H, K, f, st);
+    default: return launch<8>(pd, c, xp, wp, ap, s, part, H, K, f, st);
     }
 }
 

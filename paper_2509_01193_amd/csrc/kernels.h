@@ -170,7 +170,7 @@ hipError_t block_norm_bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, con
 hipError_t gated_activate(int dtype, int act, int64_t T, int32_t f, const void* gu, void* h, hipStream_t st);
 // The forward pass for up to kSkinnyTokens tokens, bf16 (gated_skinny.hip): the product's fp32 sums and the projections into ws, then [g | u]
 // (or NULL) and h.
-constexpr int64_t kSkinnyTokens = 64;
+constexpr int64_t kSkinnyTokens = 128;
 size_t gated_skinny_ws_bytes(int64_t T, int32_t K, int32_t f, int32_t r_max);
 hipError_t gated_skinny_product(const PlanDev& pd, const void* x, const void* W, const void* A, const float* s, void* ws, bool adapters, hipStream_t st);
 hipError_t gated_skinny_finish(const PlanDev& pd, int act, const void* B, const void* ws, bool adapters, void* gu, void* h, hipStream_t st);

@@ -5,7 +5,7 @@ units of their largest term."""
 import pytest
 
 from paper_2509_01193_amd import binding as bd
-from test_step_ops import act64, near, ref_block_norm, ref_block_norm_rest, ref_gated_projections
+from test_step_ops import act64, near, ref_block_norm, ref_block_norm_rest, ref_gated_projections, test_gated as check_gated
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -154,3 +154,13 @@ def test_gated_projections_beyond_32_bits(T, f):
         assert float((got.double().cpu() - ref).abs().max() / ref.abs().max()) <= 2e-2, what
     gu[at] = 0
     assert not bool(gu.any())
+
+
+@pytest.mark.parametrize("T,d,f,ranks,batch,act", [
+    (80, 264, 72, [8, 8], "tokens", 0), (97, 1000, 136, [24], "tokens", 1), (112, 64, 264, [8], "mixed", 0), (113, 136, 8200, [8], "bare", 0),
+    (128, 4096, 64, [16, 64, 8], "tokens", 1), (128, 512, 1376, [16] * 9, "tokens", 0), (127, 2056, 520, [64, 8], "mixed", 0),
+    (129, 520, 192, [16], "tokens", 0),
+])
+def test_gated_few_tokens(T, d, f, ranks, batch, act):
+    """(up to 128 tokens are one stream over the weights)"""
+    check_gated("bf16", T, d, f, ranks, batch, act)
