@@ -37,6 +37,9 @@ size_t gated_scratch(const Plan& p)
 bool gated_is_skinny(const Plan& p) { return p.mfma && p.desc.T > 0 && p.desc.T <= kSkinnyTokens; }
 size_t gated_skinny_bytes(const Plan& p) { return gated_skinny_ws_bytes(p.desc.T, p.desc.d_in, p.dg, p.tb.empty() ? 0 : p.r_max); }
 
+// A layer product whose K is split leaves its fp32 sums to the activation, if the workspace has room for those of both projections.
+size_t gated_sums_bytes(const Plan& p) { return p.mfma && p.desc.T > 0 ? p.fwd_part * (p.fwd_group > 0 ? 1 : 2) : 0; }
+
 // ---- norms ----------------------------------------------------------------------------------------------------------------
 
 lobra_status block_norm_check(const Plan& p, const lobra_block_norm_config* cfg)
@@ -153,6 +156,7 @@ lobra_status lobra_mlora_gated_workspace_bytes(const lobra_mlora_plan* plan, int
     if (plan->n_proj != 2) return LOBRA_ERR_SHAPE;
     *fwd_bytes = (save_gu || plan->gated_persistent ? 0 : gated_scratch(*plan)) + plan->fwd_ws_bytes;
     if (gated_is_skinny(*plan)) *fwd_bytes = std::max(*fwd_bytes, gated_skinny_bytes(*plan));
+    if (!plan->gated_persistent && gated_sums_bytes(*plan) > 0) *fwd_bytes = std::max(*fwd_bytes, gated_sums_bytes(*plan) + plan->p_layout.total);
     return LOBRA_OK;
 }
 
@@ -186,6 +190,28 @@ lobra_status lobra_mlora_gated_fwd(const lobra_mlora_plan* plan, int32_t act, co
             LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK,
                          shrink_mfma(pd, x, A, s, hb + p.p_layout.p_tok, hb + p.p_layout.p_blk, pd.d_in, pd.d_in, 1, 0, st));
         LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gemm_persistent_gated(pd, act, x, W, adapters ? hb + p.p_layout.p_tok : nullptr, B, gu, h, st));
+        return LOBRA_OK;
+    }
+    const size_t sums = gated_sums_bytes(p);
+    if (sums > 0 && ws && ws_bytes >= sums + (h_save ? 0 : p.p_layout.total)) {
+        if ((rs = plan_fwd_check(p, x, W, A, B, s, h, h_save, ws, ws_bytes)) != LOBRA_OK) return rs;
+        const PlanDev pd = device_view(p);
+        char* const hb = h_save ? static_cast<char*>(h_save) : static_cast<char*>(ws) + sums;
+        const char* const P = adapters ? hb + p.p_layout.p_tok : nullptr;
+        if (adapters)
+            LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK, shrink_mfma(pd, x, A, s, hb + p.p_layout.p_tok, hb + p.p_layout.p_blk, pd.d_in, pd.d_in, 1, 0, st));
+        const int32_t N = p.fwd_group > 0 ? pd.d_out : pd.dg;
+        const int32_t n = choose_gemm(pd.T, pd.d_in, N, p.fwd_group, adapters ? pd.nseg : 0, pd.r_max / 2, std::min(p.fwd_part, kMaxPartBytes)).splits +
+                          (adapters ? 1 : 0);
+        float *const g = static_cast<float*>(ws), *const u = p.fwd_group > 0 ? g + pd.dg : reinterpret_cast<float*>(static_cast<char*>(ws) + p.fwd_part);
+        if (p.fwd_group > 0)
+            LOBRA_LAUNCH(p, st, LOBRA_K_GEMM, gemm_mfma(pd, false, x, W, P, B, nullptr, pd.d_in, N, pd.d_out, st, pd.d_out, 2, -1, g, p.fwd_part));
+        else
+            for (int32_t j = 0; j < 2; ++j)
+                LOBRA_LAUNCH(p, st, LOBRA_K_GEMM,
+                             gemm_mfma(pd, false, x, static_cast<const char*>(W) + size_t(j) * pd.dg * 2, P, B, nullptr, pd.d_in, N, pd.d_out, st, pd.d_out, 2,
+                                       j, j == 0 ? g : u, p.fwd_part));
+        LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_sums(act, pd.T, pd.dg, g, u, N, int64_t(pd.T) * N, n, gu, h, st));
         return LOBRA_OK;
     }
     const size_t own = gu ? 0 : gated_scratch(p);

@@ -731,7 +731,7 @@ static hipError_t launch_tile(const PlanDev& pd, const void* Z, const void* W, c
         pd, (const uint16_t*)Z, (const uint16_t*)W, (const uint16_t*)P, (const uint16_t*)M, (uint16_t*)C,
         K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, 1024 / TM, splits, part);
     e = hipGetLastError();
-    if (e != hipSuccess || splits == 1) return e;
+    if (e != hipSuccess || splits == 1 || !C) return e;
     const int64_t n = int64_t(pd.T) * N;             // (N is a multiple of 8)
     with_splits<2, kMaxSplits + 1>(per, [&](auto s_c) {
         gemm_add_kernel<decltype(s_c)::value><<<dim3(uint32_t((n + 2047) / 2048)), 256, 0, st>>>(part, (uint16_t*)C, n, N, ldc);
@@ -802,6 +802,7 @@ hipError_t gemm_mfma(const PlanDev& pd, bool transW, const void* Z, const void* 
     if (!gemm_mfma_shape_ok(pd.T, K, N, ldw)) return hipErrorInvalidValue;   // (plan creation has checked already)
     const GemmChoice choice = choose_gemm(pd.T, K, N, proj < 0 ? pd.dg : 0, P ? pd.nseg : 0, pd.r_max / nproj,
                                           part ? std::min(part_bytes, kMaxPartBytes) : 0);
+    if (!C && choice.splits < 2) return hipErrorInvalidValue;
 #define LOBRA_TILE(...)                                                                                          \
     (transW ? launch_tile<false, __VA_ARGS__>(pd, Z, W, P, M, C, K, N, ldw, ldc, nproj, proj, st, choice.splits, part)                 \
             : launch_tile<true, __VA_ARGS__>(pd, Z, W, P, M, C, K, N, ldw, ldc, nproj, proj, st, choice.splits, part))

@@ -72,7 +72,8 @@ hipError_t grad_f32_one(const PlanDev& pd, const GradJob& ja, const GradJob& jb,
 hipError_t gemm_mfma(const PlanDev& pd, bool transW, const void* Z, const void* W, const void* P,
                      const void* M, void* C, int32_t K, int32_t N, int32_t ldw, hipStream_t st,
                      int32_t ldc = 0, int32_t nproj = 1, int32_t proj = 0, float* part = nullptr, size_t part_bytes = 0);
-// part, part_bytes: scratch for the sums of a product whose K is split (choose_gemm; NULL, 0: it is not split).
+// part, part_bytes: scratch for the sums of a product whose K is split (choose_gemm; NULL, 0: it is not split).  C = NULL, of a product that
+// is split: the sums stay there, [splits (+ 1 with P)][T][N].
 // The projection of Z by the down factors D and the product in one launch (and one that adds up): what choose_beside chose for the
 // batch; P_tok and P_blk are what shrink_mfma would have written.
 hipError_t gemm_mfma_beside(const PlanDev& pd, const GemmChoice& choice, bool transW, const void* Z, const void* W, const void* D,
@@ -168,6 +169,9 @@ hipError_t block_norm_bwd(const PlanDev& pd, int dtype, const BlockNorm& bn, con
 
 // h = a(g) u of [g | u] [T][2 f], and [dg | du] from dh (gated.hip).
 hipError_t gated_activate(int dtype, int act, int64_t T, int32_t f, const void* gu, void* h, hipStream_t st);
+// h and (if not NULL) gu from the fp32 sums of a split product: n of g's, `stride` floats apart, rows of ld floats, from g on, u's likewise.
+hipError_t gated_sums(int act, int64_t T, int32_t f, const float* g, const float* u, int64_t ld, int64_t stride, int32_t n, void* gu, void* h,
+                      hipStream_t st);
 // The forward pass for up to kSkinnyTokens tokens, bf16 (gated_skinny.hip): the product's fp32 sums and the projections into ws, then [g | u]
 // (or NULL) and h.
 constexpr int64_t kSkinnyTokens = 128;

@@ -164,3 +164,27 @@ def test_gated_projections_beyond_32_bits(T, f):
 def test_gated_few_tokens(T, d, f, ranks, batch, act):
     """(up to 128 tokens are one stream over the weights)"""
     check_gated("bf16", T, d, f, ranks, batch, act)
+
+
+@pytest.mark.parametrize("T,d,f,ranks,batch,act", [
+    (167, 2176, 1432, [8] * 16, "mixed", 0), (200, 4096, 512, [16, 8], "tokens", 1), (300, 4096, 256, [64, 8], "mixed", 0), (150, 2048, 264, [8], "bare", 0),
+    (500, 1032, 64, [16], "one", 0), (140, 8192, 128, [8], "mixed", 1),
+])
+def test_gated_sums_of_a_split_product(T, d, f, ranks, batch, act):
+    check_gated("bf16", T, d, f, ranks, batch, act)
+
+
+def test_gated_workspace_without_room_for_sums():
+    """What a smaller workspace takes: the product rounds [g | u], as where it is not split."""
+    T, d, f = 200, 4096, 512
+    gen = torch.Generator().manual_seed(1)
+    mk = lambda std, *s: (torch.randn(*s, generator=gen) * std).bfloat16().to(DEV)
+    plan = bd.Plan("bf16", T, d, 2 * f, [0, 16], [0, T], [0], n_proj=2)
+    w = mk(1.0, T, d), mk(1 / 64, d, 2 * f), mk(1 / 64, 16, d), mk(0.3, 16, f), torch.ones(1, device=DEV)
+    hs = torch.empty(plan.h_save_bytes, dtype=torch.uint8, device=DEV)
+    gu, h, h1 = torch.empty(T, 2 * f, dtype=torch.bfloat16, device=DEV), *(torch.empty(T, f, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ws = torch.empty(bd.lobra_mlora_gated_workspace_bytes(plan, True), dtype=torch.uint8, device=DEV)
+    bd.lobra_mlora_gated_fwd(plan, 0, *w, gu, h, hs, ws)
+    bd.lobra_mlora_gated_fwd(plan, 0, *w, gu, h1, hs, ws[:256])
+    torch.cuda.synchronize()
+    assert float((h.double() - h1.double()).abs().max() / h.double().abs().max()) <= 2.0 ** -7
