@@ -318,7 +318,7 @@ LOBRA_API lobra_status lobra_mlora_adam_step(const lobra_mlora_plan *plan, const
  *     dg = dh u a'(g),  du = dh a(g);  dx, dA, dB = the layer's gradients of dy = [dg | du]
  * a = LOBRA_ACT_SILU: g / (1 + exp(-g)); LOBRA_ACT_GELU_TANH: g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2.
  *   gu    : device [T, 2 f], element type of the plan: [g | u], each rounded once, which backward starts from; NULL (serving): not kept
- *   h     : device [T, f], overwritten; from the fp32 projections where a kernel has those (up to 128 tokens without h_save, a split
+ *   h     : device [T, f], overwritten; from the fp32 projections where a kernel has those (up to 128 tokens, 64 in fp32, without h_save, a split
  *           product with room for its sums in ws, long batches), else from [g | u] as rounded to the element type
  *   ws    : lobra_mlora_gated_workspace_bytes (save_gu: whether gu will be given) says what is enough; as in lobra_mlora_plan_fwd a
  *           split product's sums are optional, what they leave has to be there (LOBRA_ERR_WORKSPACE)

@@ -34,8 +34,11 @@ size_t gated_scratch(const Plan& p)
 }
 
 // Few tokens (decoding) have kernels of their own, which keep no projected activations.
-bool gated_is_skinny(const Plan& p) { return p.mfma && p.desc.T > 0 && p.desc.T <= kSkinnyTokens; }
-size_t gated_skinny_bytes(const Plan& p) { return gated_skinny_ws_bytes(p.desc.T, p.desc.d_in, p.dg, p.tb.empty() ? 0 : p.r_max); }
+bool gated_is_skinny(const Plan& p) { return p.desc.T > 0 && p.desc.T <= (p.mfma ? kSkinnyTokens : p.desc.dtype == LOBRA_F32 ? kFewTokens : 0); }
+size_t gated_skinny_bytes(const Plan& p)
+{
+    return (p.mfma ? gated_skinny_ws_bytes : gated_few_ws_bytes)(p.desc.T, p.desc.d_in, p.dg, p.tb.empty() ? 0 : p.r_max);
+}
 
 // A layer product whose K is split leaves its fp32 sums to the activation, if the workspace has room for those of both projections.
 size_t gated_sums_bytes(const Plan& p) { return p.mfma && p.desc.T > 0 ? p.fwd_part * (p.fwd_group > 0 ? 1 : 2) : 0; }
@@ -178,8 +181,14 @@ lobra_status lobra_mlora_gated_fwd(const lobra_mlora_plan* plan, int32_t act, co
         if (!ws || ws_bytes < gated_skinny_bytes(p)) return LOBRA_ERR_WORKSPACE;
         PlanDev pd = device_view(p);
         if (!adapters) pd.r_max = 0;
-        LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK_GEMM, gated_skinny_product(pd, x, W, A, s, ws, adapters, st));
-        LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_skinny_finish(pd, act, B, ws, adapters, gu, h, st));
+        if (p.mfma) {
+            LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK_GEMM, gated_skinny_product(pd, x, W, A, s, ws, adapters, st));
+            LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_skinny_finish(pd, act, B, ws, adapters, gu, h, st));
+        } else {
+            const auto floats = [](const void* q) { return static_cast<const float*>(q); };
+            LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK_GEMM, gated_few_product(pd, floats(x), floats(W), floats(A), s, ws, adapters, st));
+            LOBRA_LAUNCH(p, st, LOBRA_K_GATED, gated_few_finish(pd, act, floats(B), ws, adapters, static_cast<float*>(gu), static_cast<float*>(h), st));
+        }
         return LOBRA_OK;
     }
     if (p.gated_persistent) {

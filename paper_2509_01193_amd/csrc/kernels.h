@@ -178,6 +178,11 @@ constexpr int64_t kSkinnyTokens = 128;
 size_t gated_skinny_ws_bytes(int64_t T, int32_t K, int32_t f, int32_t r_max);
 hipError_t gated_skinny_product(const PlanDev& pd, const void* x, const void* W, const void* A, const float* s, void* ws, bool adapters, hipStream_t st);
 hipError_t gated_skinny_finish(const PlanDev& pd, int act, const void* B, const void* ws, bool adapters, void* gu, void* h, hipStream_t st);
+// The same in fp32, for up to kFewTokens (gated_few_f32.hip).
+constexpr int64_t kFewTokens = 64;
+size_t gated_few_ws_bytes(int64_t T, int32_t K, int32_t f, int32_t r_max);
+hipError_t gated_few_product(const PlanDev& pd, const float* x, const float* W, const float* A, const float* s, void* ws, bool adapters, hipStream_t st);
+hipError_t gated_few_finish(const PlanDev& pd, int act, const float* B, const void* ws, bool adapters, float* gu, float* h, hipStream_t st);
 // The product with the activation in its epilogue (gemm_persistent.hip), of a plan that says so (gated_persistent).  P: the token-major
 // projections, or NULL; gu or NULL.
 hipError_t gemm_persistent_gated(const PlanDev& pd, int act, const void* x, const void* W, const void* P, const void* B, void* gu, void* h,

@@ -188,3 +188,11 @@ def test_gated_workspace_without_room_for_sums():
     bd.lobra_mlora_gated_fwd(plan, 0, *w, gu, h1, hs, ws[:256])
     torch.cuda.synchronize()
     assert float((h.double() - h1.double()).abs().max() / h.double().abs().max()) <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("T,d,f,ranks,batch,act", [
+    (1, 1, 8, [8], "one", 0), (2, 15, 64, [8], "bare", 1), (16, 16, 72, [8, 8], "tokens", 0), (17, 17, 136, [24], "tokens", 1), (33, 63, 8, [8], "mixed", 0),
+    (28, 919, 256, [16] * 8, "tokens", 0), (48, 4097, 64, [64, 8], "tokens", 1), (64, 130, 2056, [8, 16], "mixed", 0), (65, 130, 200, [8], "tokens", 0),
+])
+def test_gated_few_tokens_fp32(T, d, f, ranks, batch, act):
+    check_gated("f32", T, d, f, ranks, batch, act)
