@@ -6,9 +6,9 @@
 //     dgate_t = alpha w_post sum_t g bh   dw_post = alpha sum gate_t g bh   dw_pre = sum dx rh
 // The two means of backward are one reduction: with s1 = sum u rh, s2 = sum q bh (dr' + m u), s3 = sum q bh rh, mean(u rh) = s1 / d and
 // mean(q g bh) = (s2 - m s1 / d s3) / d.
-// A row lives in the registers of a team of threads - a wave, or a workgroup of up to 1024 - from its read to its write.  Backward's teams take neighbouring rows and keep the sums over tokens in registers from row to row; they
-// write them out where their rows end, the gate's also where a segment ends (slot: team + segment, which no two runs share; the slots'
-// tasks stand beside them), and a second launch adds them in order.
+// A row lives in the registers of a team of threads - a wave, or a workgroup of up to 1024 - from its read to its write.  Backward's teams take
+// neighbouring rows and keep the sums over tokens in registers from row to row; they write them out where their rows end, the gate's also where a
+// segment ends (slot: team + segment, which no two runs share; the slots' tasks stand beside them), and a second launch adds them in order.
 // Bound: memory, 4 T d elements forward and 6 T d backward.  Measured, us: 16384 x 4096 bf16 forward 102 .. 114 (of 537 MB, 5.0 TB/s), backward
 // 161 .. 173 (805 MB, 4.8 TB/s) and its sums' launch 7; 2999 x 1025 fp32, out of the caches, 15, 22 and 5; 40 x 4096 forward 6.
 #include <algorithm>
