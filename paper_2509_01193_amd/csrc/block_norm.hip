@@ -10,7 +10,7 @@
 // neighbouring rows and keep the sums over tokens in registers from row to row; they write them out where their rows end, the gate's also where a
 // segment ends (slot: team + segment, which no two runs share; the slots' tasks stand beside them), and a second launch adds them in order.
 // Bound: memory, 4 T d elements forward and 6 T d backward.  Measured, us: 16384 x 4096 bf16 forward 102 .. 114 (of 537 MB, 5.0 TB/s), backward
-// 161 .. 173 (805 MB, 4.8 TB/s) and its sums' launch 7; 2999 x 1025 fp32, out of the caches, 15, 22 and 5; 40 x 4096 forward 6.
+// 161 .. 173 (805 MB, 4.8 TB/s) and its sums' launch 7; 2999 x 1025 fp32, out of the caches, 15, 22 and 5; 40 x 4096 forward 4.
 #include <algorithm>
 
 #include "kernels.h"
@@ -95,9 +95,6 @@ template <typename E> struct NormArgs {
     bool post;
 };
 
-// task of a row, -1: none
-__device__ __forceinline__ int32_t row_task(const PlanDev& pd, int32_t row) { return pd.cseg_task[segment_of_row(pd, row)]; }
-
 // I packets of N elements per thread hold a row of up to NT I N; BT / NT teams per workgroup, a row each, from row0 on.
 template <typename E, bool RAGGED, int NT, int I>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT)
@@ -135,7 +132,7 @@ void block_norm_fwd_kernel(PlanDev pd, NormArgs<E> a, int32_t row0)
             n = 1.f / sqrtf(sums[0] / float(a.d) + a.eps);
             if (t == 0 && a.rstd_post) a.rstd_post[row] = n;
         }
-        const int32_t task = a.gate ? row_task(pd, row) : -1;
+        const int32_t task = a.gate ? wave_segment(pd, row).task : -1;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int32_t c = (t + i * NT) * N;
@@ -213,8 +210,8 @@ void block_norm_bwd_kernel(PlanDev pd, NormGradArgs<E> a)
 #pragma unroll
         for (int e = 0; e < N; ++e) sum_run[i][e] = sum_post[i][e] = sum_pre[i][e] = 0.f;
     const bool gated = a.gate != nullptr;             // the rows' tasks matter
-    int32_t seg = gated ? segment_of_row(pd, row0) : 0;
-    int32_t seg_end = gated ? pd.cseg_off[seg + 1] : row1, task = gated ? pd.cseg_task[seg] : -1;
+    const Segment own = gated ? wave_segment(pd, row0) : Segment{0, -1};
+    int32_t seg = own.seg, task = own.task, seg_end = gated ? pd.cseg_off[seg + 1] : row1;
     // (a segment that begins with a team's first row leaves a slot between its run and the one before)
     if (SUMS && a.part_gate && t == 0 && team > 0 && pd.cseg_off[seg] == row0) a.slot_task[team + seg - 1] = -1;
     // gains and the task's gate stay in registers as they are in memory, and a row is fetched while the one before is worked on

@@ -38,7 +38,7 @@ __device__ __forceinline__ void project(const PlanDev& pd, const float* x, const
     const int32_t groups = pd.r_max / ROWS;
     for (int32_t n = wave; n < pd.T * groups; n += waves) {
         const int32_t token = n / groups, row = (n - token * groups) * ROWS;
-        const int32_t task = pd.cseg_task[segment_of_row(pd, token)];
+        const int32_t task = wave_segment(pd, token).task;
         if (task < 0) continue;
         const int32_t r0 = pd.rank_off[task];
         if (row >= pd.rank_off[task + 1] - r0) continue;
@@ -183,7 +183,7 @@ void gated_few_finish_kernel(PlanDev pd, const float* __restrict__ part, const f
                              float* __restrict__ gu, float* __restrict__ h)
 {
     const int32_t col = (int32_t(blockIdx.x) * 64 + int32_t(threadIdx.x)) * 4, i = blockIdx.y, T = pd.T;
-    const int32_t task = H ? pd.cseg_task[segment_of_row(pd, i)] : -1;
+    const int32_t task = H ? wave_segment(pd, i).task : -1;
     if (col >= f) return;
     const int32_t tile = col / COLS;
     const float* at = part + (size_t(tile) * 2 * T + i) * COLS + col % COLS;
