@@ -196,6 +196,22 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_torch_types = {}
+
+
+def _typed(t, kind, least=0):
+    """_ptr of a tensor that the library takes for `kind` ("fp32", "bf16", "int32"), of at least so many elements."""
+    if t is None or isinstance(t, int):
+        return t
+    if not _torch_types:
+        import torch
+        _torch_types.update(fp32=torch.float32, bf16=torch.bfloat16, int32=torch.int32)
+    assert t.dtype is _torch_types[kind], "a %s tensor where the library reads or writes %s" % (t.dtype, kind)
+    assert not least or t.numel() >= least, "a tensor of %d elements where the library reads or writes %d" % (t.numel(), least)
+    assert t.is_contiguous(), "tensors must be contiguous"
+    return t.data_ptr()
+
+
 _current_stream = None
 
 
@@ -443,16 +459,17 @@ def lobra_token_logprob_bwd(desc: LogprobDesc, logits, target, lse, lse_rest, en
     return st
 
 
-def make_grad_tensors(tensors):
-    """(array of GradTensor, keepalive) of [(grad, out or None, rank_off)]: fp32 tensors [R, D]."""
+def make_grad_tensors(tensors, n_tasks):
+    """(array of GradTensor, keepalive) of [(grad, out or None, rank_off)]: fp32 tensors [R, D], tables of n_tasks + 1 entries."""
     arr, keep, tables = (GradTensor * max(len(tensors), 1))(), [], {}
     for i, (g, out, rank_off) in enumerate(tensors):
         ro = tuple(rank_off)            # one table for all layers of the same ranks
+        assert len(ro) == int(n_tasks) + 1, "a rank_off of %d entries for %d tasks" % (len(ro), n_tasks)
         if ro not in tables:
             tables[ro] = (ctypes.c_int32 * len(ro))(*map(int, ro))
         keep += [g, out]
         a = arr[i]
-        a.grad, a.out, a.D, a.rank_off = _ptr(g), _ptr(out), g.shape[1], tables[ro]
+        a.grad, a.out, a.D, a.rank_off = _typed(g, "fp32"), _typed(out, "fp32"), g.shape[1], tables[ro]
         assert g.shape[0] == ro[-1] and len(g.shape) == 2 and (out is None or out.shape == g.shape), "a gradient of another shape than its ranks'"
     keep += tables.values()
     return arr, keep
@@ -464,7 +481,7 @@ class GradSet:
     def __init__(self, tensors, n_tasks, device_mem=None, stream=None):
         """device_mem (a device uint8 tensor of at least grad_set_device_bytes(...)): lobra_grad_set_init places the set there with
         an asynchronous copy on `stream`; None: lobra_grad_set_create allocates."""
-        arr, self._keep = make_grad_tensors(tensors)
+        arr, self._keep = make_grad_tensors(tensors, n_tasks)
         self.handle, self.n_tasks = ctypes.c_void_p(), int(n_tasks)
         if device_mem is None:
             _check(lib().lobra_grad_set_create(arr, len(tensors), self.n_tasks, ctypes.byref(self.handle)), "lobra_grad_set_create")
@@ -489,7 +506,7 @@ class GradSet:
 
 
 def grad_set_device_bytes(tensors, n_tasks) -> int:
-    arr, _keep = make_grad_tensors(tensors)
+    arr, _keep = make_grad_tensors(tensors, n_tasks)
     n = ctypes.c_size_t()
     _check(lib().lobra_grad_set_device_bytes(arr, len(tensors), int(n_tasks), ctypes.byref(n)), "lobra_grad_set_device_bytes")
     return n.value

@@ -345,6 +345,21 @@ def test_grad_set_refusals():
     assert L.lobra_grad_set_destroy(None) == bd.OK
 
 
+@pytest.mark.parametrize("use", [lambda t, n: bd.GradSet(t, n), lambda t, n: bd.grad_set_device_bytes(t, n)], ids=["set", "bytes"])
+def test_grad_set_refuses_other_types_and_tables(use):
+    """What the library would read or write beyond its end: elements of two bytes, and a table of fewer tasks.  Nothing is launched or looked up."""
+    f32, short = torch.zeros(8, 16), [0, 4, 8]
+    for other in (torch.bfloat16, torch.float16, torch.float64, torch.int32):
+        with pytest.raises(AssertionError, match="fp32"):
+            use([(f32, None, short), (torch.zeros(8, 16, dtype=other), None, short)], 2)
+        with pytest.raises(AssertionError, match="fp32"):
+            use([(f32, torch.zeros(8, 16, dtype=other), short)], 2)
+    for n_tasks, table in ((3, [0, 4, 8]), (1, [0, 4, 8]), (2, [0, 8]), (2, [0])):
+        with pytest.raises(AssertionError, match="rank_off"):
+            use([(f32, None, table)], n_tasks)
+    assert bd.grad_set_device_bytes([(f32, f32, short)], 2) > 0
+
+
 @pytest.mark.gpu
 def test_grad_clip_refusals():
     g = torch.zeros(8, 16, device=DEV)
