@@ -197,16 +197,21 @@ def _ptr(t):
 
 
 _torch_types = {}
+_KINDS = {F32: "fp32", BF16: "bf16"}
+
+
+def _is_type(t, kind):
+    if not _torch_types:
+        import torch
+        _torch_types.update(fp32=torch.float32, bf16=torch.bfloat16, int32=torch.int32)
+    return t.dtype is _torch_types[kind]
 
 
 def _typed(t, kind, least=0):
     """_ptr of a tensor that the library takes for `kind` ("fp32", "bf16", "int32"), of at least so many elements."""
     if t is None or isinstance(t, int):
         return t
-    if not _torch_types:
-        import torch
-        _torch_types.update(fp32=torch.float32, bf16=torch.bfloat16, int32=torch.int32)
-    assert t.dtype is _torch_types[kind], "a %s tensor where the library reads or writes %s" % (t.dtype, kind)
+    assert _is_type(t, kind), "a %s tensor where the library reads or writes %s" % (t.dtype, kind)
     assert not least or t.numel() >= least, "a tensor of %d elements where the library reads or writes %d" % (t.numel(), least)
     assert t.is_contiguous(), "tensors must be contiguous"
     return t.data_ptr()
@@ -433,7 +438,7 @@ def _rows_ptr(t, desc: LogprobDesc):
         return t
     T, V = t.shape
     ld, one = t.stride()
-    assert t.element_size() == (4 if desc.dtype == F32 else 2) and t.is_floating_point(), "logits of another type than the descriptor's"
+    assert desc.dtype not in _KINDS or _is_type(t, _KINDS[desc.dtype]), "logits of another type than the descriptor's"
     assert T == desc.T and V == desc.V, "logits of another shape than the descriptor's"
     assert T <= 1 or ld == (desc.ld or V), "rows of logits are not ld elements apart"
     assert V <= 1 or one == 1, "rows of logits must be contiguous"
@@ -443,8 +448,10 @@ def _rows_ptr(t, desc: LogprobDesc):
 def lobra_token_logprob_fwd(desc: LogprobDesc, logits, target, logp=None, lse=None, lse_rest=None, entropy=None, top_logp=None, top_id=None,
                             stream=None, check=True):
     """logp = ln softmax(logits)[target], lse, entropy and the top_k likeliest tokens of every row.  Returns the status."""
-    st = lib().lobra_token_logprob_fwd(ctypes.byref(desc), _rows_ptr(logits, desc), _ptr(target), _ptr(logp), _ptr(lse), _ptr(lse_rest), _ptr(entropy),
-                                       _ptr(top_logp), _ptr(top_id), _stream(stream))
+    T = desc.T
+    st = lib().lobra_token_logprob_fwd(ctypes.byref(desc), _rows_ptr(logits, desc), _typed(target, "int32", T), _typed(logp, "fp32", T),
+                                       _typed(lse, "fp32", T), _typed(lse_rest, "fp32", T), _typed(entropy, "fp32", T),
+                                       _typed(top_logp, "fp32", T * desc.top_k), _typed(top_id, "int32", T * desc.top_k), _stream(stream))
     if check:
         _check(st, "lobra_token_logprob_fwd")
     return st
@@ -452,8 +459,10 @@ def lobra_token_logprob_fwd(desc: LogprobDesc, logits, target, logp=None, lse=No
 
 def lobra_token_logprob_bwd(desc: LogprobDesc, logits, target, lse, lse_rest, entropy, dlogp, dentropy, dlogits, stream=None, check=True):
     """dlogits (may be logits) from dlogp and dentropy.  Returns the status."""
-    st = lib().lobra_token_logprob_bwd(ctypes.byref(desc), _rows_ptr(logits, desc), _ptr(target), _ptr(lse), _ptr(lse_rest), _ptr(entropy), _ptr(dlogp),
-                                       _ptr(dentropy), _rows_ptr(dlogits, desc), _stream(stream))
+    T = desc.T
+    st = lib().lobra_token_logprob_bwd(ctypes.byref(desc), _rows_ptr(logits, desc), _typed(target, "int32", T), _typed(lse, "fp32", T),
+                                       _typed(lse_rest, "fp32", T), _typed(entropy, "fp32", T), _typed(dlogp, "fp32", T), _typed(dentropy, "fp32", T),
+                                       _rows_ptr(dlogits, desc), _stream(stream))
     if check:
         _check(st, "lobra_token_logprob_bwd")
     return st

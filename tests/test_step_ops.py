@@ -241,6 +241,48 @@ def test_logprob_refusals():
         bd.lobra_token_logprob_fwd(bd.make_logprob_desc("f32", 4, 100, ld=104), z, None, stream=0)
 
 
+def test_logprob_refuses_other_types_and_short_rows():
+    """fp16 logits are no bf16 ones, int64 targets no int32 ones, and every array of the rows has a number for each: what is refused is not
+    read as what it is not.  (On the CPU: a call that goes through has no rows.)"""
+    T, V, k = 4, 100, 3
+    f, i = torch.zeros(T), torch.zeros(T, dtype=torch.int32)
+    top = dict(top_logp=torch.zeros(T, k), top_id=torch.zeros(T, k, dtype=torch.int32))
+    z = torch.zeros(T, V, dtype=torch.bfloat16)
+    desc, wide = bd.make_logprob_desc("bf16", T, V, top_k=k), bd.make_logprob_desc("f32", T, V)
+
+    def fwd(**kw):
+        a = {**dict(desc=desc, logits=z, target=i, logp=f, lse=f, lse_rest=f, entropy=f), **top, **kw}
+        bd.lobra_token_logprob_fwd(**a, stream=0)
+
+    def bwd(**kw):
+        a = {**dict(desc=desc, logits=z, target=i, lse=f, lse_rest=f, entropy=f, dlogp=f, dentropy=f, dlogits=z), **kw}
+        bd.lobra_token_logprob_bwd(**a, stream=0)
+
+    for call, names in ((fwd, ("logp", "lse", "lse_rest", "entropy")), (bwd, ("lse", "lse_rest", "entropy", "dlogp", "dentropy"))):
+        for bad in (z.half(), z.float(), z.short()):
+            with pytest.raises(AssertionError):
+                call(logits=bad)
+        for bad in (z.float().int(), z.float().double()[:, :V]):
+            with pytest.raises(AssertionError):
+                call(desc=wide, logits=bad)
+        for bad in (i.long(), i.float(), i[:T - 1]):
+            with pytest.raises(AssertionError):
+                call(target=bad)
+        for name in names:
+            for bad in (f.double(), f.bfloat16(), f.int(), f[:T - 1]):
+                with pytest.raises(AssertionError):
+                    call(**{name: bad})
+    with pytest.raises(AssertionError):
+        bwd(dlogits=z.half())
+    for bad in (dict(top_id=top["top_id"].long()), dict(top_id=top["top_id"][:, :2].contiguous()), dict(top_logp=top["top_logp"].double()),
+                dict(top_logp=top["top_logp"][1:])):
+        with pytest.raises(AssertionError):
+            fwd(**bad)
+    none = bd.make_logprob_desc("bf16", 0, V, top_k=k)
+    bd.lobra_token_logprob_fwd(none, z[:0], i[:0], f[:0], f[:0], f[:0], f[:0], top["top_logp"][:0], top["top_id"][:0], stream=0)
+    bd.lobra_token_logprob_bwd(none, z[:0], i[:0], f[:0], f[:0], f[:0], f[:0], f[:0], z[:0], stream=0)
+
+
 # ------------------------------------------------------------------------------------------------------------------
 # gradient norms and clipping
 # ------------------------------------------------------------------------------------------------------------------
