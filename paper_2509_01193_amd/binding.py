@@ -523,8 +523,9 @@ def grad_set_device_bytes(tensors, n_tasks) -> int:
 
 def lobra_grad_clip(gset: GradSet, max_norm, grad_scale, step, norm, clip_scale, step_out, flags=0, ws=None, stream=None, check=True):
     """Every task's gradient norm, and the factor (for lobra_mlora_adam_step's grad_scale) that clips it.  Returns the status."""
-    st = lib().lobra_grad_clip(gset.handle, _ptr(max_norm), _ptr(grad_scale), _ptr(step), _ptr(norm), _ptr(clip_scale), _ptr(step_out), int(flags),
-                               _ptr(ws), _nbytes(ws), _stream(stream))
+    n = gset.n_tasks
+    st = lib().lobra_grad_clip(gset.handle, _typed(max_norm, "fp32", n), _typed(grad_scale, "fp32", n), _typed(step, "int32", n), _typed(norm, "fp32", n),
+                               _typed(clip_scale, "fp32", n), _typed(step_out, "int32", n), int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_grad_clip")
     return st

@@ -413,6 +413,28 @@ def test_grad_clip_refusals():
     assert call(ws=None) == -7 and call(ws=ws[:gset.ws_bytes - 1]) == -7 and call(ws=torch.empty(gset.ws_bytes + 16, dtype=torch.uint8, device=DEV)[4:]) == -8
 
 
+def test_grad_clip_refuses_other_types_and_fewer_tasks():
+    """Per-task arrays of another type, or of fewer tasks than the set has.  (On the CPU: the set has no tensors and is never made.)"""
+    n = 3
+    gset = bd.GradSet.__new__(bd.GradSet)
+    gset.handle, gset.n_tasks, gset.ws_bytes = ctypes.c_void_p(), n, 16
+    f, i = torch.zeros(n), torch.zeros(n, dtype=torch.int32)
+
+    def clip(**kw):
+        a = {**dict(max_norm=f, grad_scale=f, step=i, norm=f, clip_scale=f, step_out=i), **kw}
+        return bd.lobra_grad_clip(gset, **a, stream=0, check=False)
+
+    assert clip() == -10                     # (no set: the library's own refusal)
+    for name in ("max_norm", "grad_scale", "norm", "clip_scale"):
+        for bad in (f.double(), f.bfloat16(), f.int(), f[:n - 1]):
+            with pytest.raises(AssertionError):
+                clip(**{name: bad})
+    for name in ("step", "step_out"):
+        for bad in (i.long(), i.float(), i[:n - 1]):
+            with pytest.raises(AssertionError):
+                clip(**{name: bad})
+
+
 # ------------------------------------------------------------------------------------------------------------------
 # norms around a residual block
 # ------------------------------------------------------------------------------------------------------------------
