@@ -196,22 +196,22 @@ def _ptr(t):
     return t.data_ptr()
 
 
-_torch_types = {}
-_KINDS = {F32: "fp32", BF16: "bf16"}
-
-
-def _is_type(t, kind):
-    if not _torch_types:
+class _TorchTypes(dict):
+    def __missing__(self, kind):
         import torch
-        _torch_types.update(fp32=torch.float32, bf16=torch.bfloat16, int32=torch.int32)
-    return t.dtype is _torch_types[kind]
+        self.update(fp32=torch.float32, bf16=torch.bfloat16, int32=torch.int32)
+        return dict.__getitem__(self, kind)
+
+
+_torch_types = _TorchTypes()
+_KINDS = {F32: "fp32", BF16: "bf16"}
 
 
 def _typed(t, kind, least=0):
     """_ptr of a tensor that the library takes for `kind` ("fp32", "bf16", "int32"), of at least so many elements."""
     if t is None or isinstance(t, int):
         return t
-    assert _is_type(t, kind), "a %s tensor where the library reads or writes %s" % (t.dtype, kind)
+    assert t.dtype is _torch_types[kind], "a %s tensor where the library reads or writes %s" % (t.dtype, kind)
     assert not least or t.numel() >= least, "a tensor of %d elements where the library reads or writes %d" % (t.numel(), least)
     assert t.is_contiguous(), "tensors must be contiguous"
     return t.data_ptr()
@@ -256,7 +256,7 @@ class Plan:
                                             ctypes.byref(c)), "lobra_mlora_plan_sizes")
         self.h_save_bytes, self.fwd_ws_bytes, self.bwd_ws_bytes = a.value, b.value, c.value
         self.T, self.d_in, self.d_out = int(T), int(d_in), int(d_out)
-        self.n_tasks = self.desc.n_tasks
+        self.n_tasks, self.kind = self.desc.n_tasks, _KINDS[self.desc.dtype]
         self.R_tot = int(np.asarray(rank_off)[-1]) if self.n_tasks > 0 else 0
 
     @classmethod
@@ -385,8 +385,9 @@ def lobra_mlora_gated_workspace_bytes(plan: Plan, save: bool) -> int:
 
 def lobra_mlora_gated_fwd(plan: Plan, act, x, W, A, B, s, gu, h, h_save=None, ws=None, stream=None, check=True):
     """h = a(g) u of the plan's gate and up projection; gu [T, 2 f] keeps [g | u] for backward, or None.  Returns the status."""
-    st = lib().lobra_mlora_gated_fwd(plan.handle, int(act), _ptr(x), _ptr(W), _ptr(A), _ptr(B), _ptr(s), _ptr(gu), _ptr(h), _ptr(h_save),
-                                     _ptr(ws), _nbytes(ws), _stream(stream))
+    e = plan.kind
+    st = lib().lobra_mlora_gated_fwd(plan.handle, int(act), _typed(x, e), _typed(W, e), _typed(A, e), _typed(B, e), _typed(s, "fp32"), _typed(gu, e),
+                                     _typed(h, e), _ptr(h_save), _ptr(ws), _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_mlora_gated_fwd")
     return st
@@ -394,8 +395,10 @@ def lobra_mlora_gated_fwd(plan: Plan, act, x, W, A, B, s, gu, h, h_save=None, ws
 
 def lobra_mlora_gated_bwd(plan: Plan, act, x, W, A, B, s, gu, dh, h_saved, dgu, dx, dA, dB, flags=0, ws=None, stream=None, check=True):
     """dgu = [dg | du] (may be gu), then the layer's dx, dA, dB.  Returns the status."""
-    st = lib().lobra_mlora_gated_bwd(plan.handle, int(act), _ptr(x), _ptr(W), _ptr(A), _ptr(B), _ptr(s), _ptr(gu), _ptr(dh), _ptr(h_saved),
-                                     _ptr(dgu), _ptr(dx), _ptr(dA), _ptr(dB), int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
+    e = plan.kind
+    st = lib().lobra_mlora_gated_bwd(plan.handle, int(act), _typed(x, e), _typed(W, e), _typed(A, e), _typed(B, e), _typed(s, "fp32"), _typed(gu, e),
+                                     _typed(dh, e), _ptr(h_saved), _typed(dgu, e), _typed(dx, e), _typed(dA, "fp32"), _typed(dB, "fp32"), int(flags),
+                                     _ptr(ws), _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_mlora_gated_bwd")
     return st
@@ -410,8 +413,9 @@ def lobra_mlora_block_norm_workspace_bytes(plan: Plan) -> int:
 def lobra_mlora_block_norm_fwd(plan: Plan, cfg: BlockNormConfig, r, b, w_post, gate, w_pre, r_out, x, rstd_post=None, rstd_pre=None,
                                stream=None, check=True):
     """r_out = r + alpha gate_t w_post b / rms(b), x = w_pre r_out / rms(r_out).  Returns the status."""
-    st = lib().lobra_mlora_block_norm_fwd(plan.handle, ctypes.byref(cfg), _ptr(r), _ptr(b), _ptr(w_post), _ptr(gate), _ptr(w_pre), _ptr(r_out),
-                                          _ptr(x), _ptr(rstd_post), _ptr(rstd_pre), _stream(stream))
+    e = plan.kind
+    st = lib().lobra_mlora_block_norm_fwd(plan.handle, ctypes.byref(cfg), _typed(r, e), _typed(b, e), _typed(w_post, e), _typed(gate, e), _typed(w_pre, e),
+                                          _typed(r_out, e), _typed(x, e), _typed(rstd_post, "fp32"), _typed(rstd_pre, "fp32"), _stream(stream))
     if check:
         _check(st, "lobra_mlora_block_norm_fwd")
     return st
@@ -419,9 +423,11 @@ def lobra_mlora_block_norm_fwd(plan: Plan, cfg: BlockNormConfig, r, b, w_post, g
 
 def lobra_mlora_block_norm_bwd(plan: Plan, cfg: BlockNormConfig, r_out, b, w_post, gate, w_pre, rstd_post, rstd_pre, dr_out, dx, dr, db,
                                dgate=None, dw_post=None, dw_pre=None, flags=0, ws=None, stream=None, check=True):
-    st = lib().lobra_mlora_block_norm_bwd(plan.handle, ctypes.byref(cfg), _ptr(r_out), _ptr(b), _ptr(w_post), _ptr(gate), _ptr(w_pre),
-                                          _ptr(rstd_post), _ptr(rstd_pre), _ptr(dr_out), _ptr(dx), _ptr(dr), _ptr(db), _ptr(dgate), _ptr(dw_post),
-                                          _ptr(dw_pre), int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
+    e = plan.kind
+    st = lib().lobra_mlora_block_norm_bwd(plan.handle, ctypes.byref(cfg), _typed(r_out, e), _typed(b, e), _typed(w_post, e), _typed(gate, e),
+                                          _typed(w_pre, e), _typed(rstd_post, "fp32"), _typed(rstd_pre, "fp32"), _typed(dr_out, e), _typed(dx, e),
+                                          _typed(dr, e), _typed(db, e), _typed(dgate, "fp32"), _typed(dw_post, "fp32"), _typed(dw_pre, "fp32"),
+                                          int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_mlora_block_norm_bwd")
     return st
@@ -438,7 +444,7 @@ def _rows_ptr(t, desc: LogprobDesc):
         return t
     T, V = t.shape
     ld, one = t.stride()
-    assert desc.dtype not in _KINDS or _is_type(t, _KINDS[desc.dtype]), "logits of another type than the descriptor's"
+    assert desc.dtype not in _KINDS or t.dtype is _torch_types[_KINDS[desc.dtype]], "logits of another type than the descriptor's"
     assert T == desc.T and V == desc.V, "logits of another shape than the descriptor's"
     assert T <= 1 or ld == (desc.ld or V), "rows of logits are not ld elements apart"
     assert V <= 1 or one == 1, "rows of logits must be contiguous"

@@ -873,6 +873,44 @@ def test_gated_refusals():
     assert bwd() == bd.OK
 
 
+def _typed_calls():
+    """name -> (call with keyword arguments in the place of its own, names of tensors of the plan's type, names of fp32 ones); plans of the
+    host alone, which the library itself refuses."""
+    T, d, f, n = 4, 16, 8, 2
+    plan = lambda dt: bd.Plan(dt, T, d, 2 * f, [0, 16, 32], [0, 1, T], [0, 1], bd.PLAN_HOST_ONLY, n_proj=2)
+    cfg = bd.BlockNormConfig(1e-5, 1.0)
+
+    def calls(dt):
+        e, g = (lambda *s: torch.zeros(*s, dtype=DT[dt])), torch.zeros
+        p = plan(dt)
+        norm = dict(r=e(T, d), b=e(T, d), w_post=e(d), gate=e(n, d), w_pre=e(d), r_out=e(T, d), x=e(T, d), rstd_post=g(T), rstd_pre=g(T))
+        back = dict(r_out=e(T, d), b=e(T, d), w_post=e(d), gate=e(n, d), w_pre=e(d), rstd_post=g(T), rstd_pre=g(T), dr_out=e(T, d), dx=e(T, d),
+                    dr=e(T, d), db=e(T, d), dgate=g(n, d), dw_post=g(d), dw_pre=g(d))
+        layer = dict(x=e(T, d), W=e(d, 2 * f), A=e(32, d), B=e(32, f), s=g(n))
+        gated = {**layer, "gu": e(T, 2 * f), "h": e(T, f)}
+        gback = {**layer, "gu": e(T, 2 * f), "dh": e(T, f), "h_saved": None, "dgu": e(T, 2 * f), "dx": e(T, d), "dA": g(32, d), "dB": g(32, f)}
+        return [(bd.lobra_mlora_block_norm_fwd, (p, cfg), norm, ("rstd_post", "rstd_pre")),
+                (bd.lobra_mlora_block_norm_bwd, (p, cfg), back, ("rstd_post", "rstd_pre", "dgate", "dw_post", "dw_pre")),
+                (bd.lobra_mlora_gated_fwd, (p, 0), gated, ("s",)), (bd.lobra_mlora_gated_bwd, (p, 0), gback, ("s", "dA", "dB"))]
+    return calls
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("which", range(4), ids=["norm_fwd", "norm_bwd", "gated_fwd", "gated_bwd"])
+def test_norms_and_gated_block_refuse_other_types(dtype, which):
+    """The plan's element type and fp32 differ in their bytes: a gradient of a gain made like the gain, for one, is written to twice its length."""
+    call, head, args, fp32 = _typed_calls()(dtype)[which]
+    assert call(*head, **args, stream=0, check=False) == -10
+    for name, t in args.items():
+        if t is None:
+            continue
+        own = torch.float32 if name in fp32 else DT[dtype]
+        for other in (torch.float32, torch.bfloat16, torch.float16, torch.float64):
+            if other is not own:
+                with pytest.raises(AssertionError):
+                    call(*head, **{**args, name: t.to(other)}, stream=0, check=False)
+
+
 @pytest.mark.gpu
 def test_on_another_stream_and_in_a_graph():
     """The calls run on the stream that they are given, allocate nothing and can be captured; a replay sees new inputs."""
