@@ -353,9 +353,10 @@ LOBRA_API lobra_status lobra_mlora_gated_bwd(const lobra_mlora_plan *plan, int32
  *   db                  : device [T, d], the gradient of b; may be dx
  *   dgate, dw_post, dw_pre : device fp32 [n_tasks, d], [d], [d], overwritten, or added to with LOBRA_FLAG_ACCUMULATE_GRADS; NULL: not
  *                         wanted.  (rows of a task without tokens: 0, or left alone)
- *   ws                  : lobra_mlora_block_norm_workspace_bytes; may be NULL when none of the three is wanted
+ *   ws                  : lobra_mlora_block_norm_workspace_bytes; may be NULL when none of the three is wanted, or T = 0
  * Sums over channels and tokens are held in fp32, in a fixed order: bit-identical from run to run.  LOBRA_ERR_SHAPE for d above
- * LOBRA_MAX_NORM_WIDTH; LOBRA_ERR_NULL where the gradient of a gain or gate that is not there is asked for. */
+ * LOBRA_MAX_NORM_WIDTH; LOBRA_ERR_NULL where the gradient of a gain or gate that is not there is asked for.  Tensors of no tokens (T = 0) may
+ * be NULL. */
 enum { LOBRA_MAX_NORM_WIDTH = 16384 };
 typedef struct {
     float eps, alpha;        /* eps >= 0, both finite */

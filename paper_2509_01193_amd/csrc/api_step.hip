@@ -290,8 +290,9 @@ lobra_status lobra_mlora_block_norm_bwd(const lobra_mlora_plan* plan, const lobr
     const Plan& p = *plan;
     if ((rs = block_norm_check(p, cfg)) != LOBRA_OK) return rs;
     const bool post = b && w_post;
-    // what has no norm, or no gate, has no gradient of it
-    if ((dgate && (!b || !gate)) || (dw_post && !post) || (dw_pre && (!w_pre || !dx))) return LOBRA_ERR_NULL;
+    // what has no norm, or no gate, has no gradient of it (an empty batch's tensors have no address: it says nothing of them)
+    const bool block = b || p.desc.T == 0, normed = dx || p.desc.T == 0;
+    if ((dgate && (!gate || !block)) || (dw_post && (!w_post || !block)) || (dw_pre && (!w_pre || !normed))) return LOBRA_ERR_NULL;
     if (p.desc.T > 0) {
         if (!dr || (b && !db) || (dx && (!w_pre || !r_out || !rstd_pre)) || (post && !rstd_post)) return LOBRA_ERR_NULL;
     }
@@ -300,9 +301,8 @@ lobra_status lobra_mlora_block_norm_bwd(const lobra_mlora_plan* plan, const lobr
                           static_cast<const void*>(ws)})
         if (!aligned16(q)) return LOBRA_ERR_ALIGN;
     if (!aligned4(rstd_post) || !aligned4(rstd_pre)) return LOBRA_ERR_ALIGN;
-    if ((dgate || dw_post || dw_pre) &&
-        (!ws || ws_bytes < block_norm_part_bytes(p.desc.T, p.desc.d_in, int32_t(p.cseg_task.size()), p.desc.dtype)))
-        return LOBRA_ERR_WORKSPACE;
+    const size_t need = dgate || dw_post || dw_pre ? block_norm_part_bytes(p.desc.T, p.desc.d_in, int32_t(p.cseg_task.size()), p.desc.dtype) : 0;
+    if (need > 0 && (!ws || ws_bytes < need)) return LOBRA_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const PlanDev pd = device_view(p);
     const BlockNorm bn{cfg->eps, cfg->alpha, w_post, gate, w_pre, post, b != nullptr};

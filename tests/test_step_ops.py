@@ -661,6 +661,34 @@ def test_block_norm_of_no_tokens():
     assert not bool(dg.any()) and not bool(dp.any()) and not bool(dq.any())
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_block_norm_of_an_empty_batch(dtype, accumulate):
+    """A chunk without tokens, its tensors those of no rows (which have no address) and no byte of workspace: gradients of 0, or as they were."""
+    n, d = 3, 72
+    plan, cfg = bd.Plan(dtype, 0, d, 64, [0, 4, 8, 12], [0, 0, 0], [2, -1]), bd.BlockNormConfig(1e-5, 0.5)
+    e, st = torch.empty(0, d, dtype=DT[dtype], device=DEV), torch.empty(0, device=DEV)
+    assert e.data_ptr() == 0
+    w, gate = torch.ones(d, dtype=DT[dtype], device=DEV), torch.ones(n, d, dtype=DT[dtype], device=DEV)
+    ws = torch.empty(bd.lobra_mlora_block_norm_workspace_bytes(plan), dtype=torch.uint8, device=DEV)
+    bd.lobra_mlora_block_norm_fwd(plan, cfg, e, e, w, gate, w, e, e, st, st)
+    for want in ("dgate dw_post dw_pre", "dgate", "dw_post", "dw_pre", ""):
+        G = {k: guarded(*s, dtype=torch.float32) for k, s in (("dgate", (n, d)), ("dw_post", (d,)), ("dw_pre", (d,))) if k in want.split()}
+        for t, _ in G.values():
+            t.fill_(5.0)
+        for scratch in (ws, None):
+            bd.lobra_mlora_block_norm_bwd(plan, cfg, e, e, w, gate, w, st, st, e, e, e, e, *[G[k][0] if k in G else None for k in ("dgate", "dw_post", "dw_pre")],
+                                          flags=bd.FLAG_ACCUMULATE_GRADS if accumulate else 0, ws=scratch)
+        torch.cuda.synchronize()
+        for k, (t, ok) in G.items():
+            assert ok() and bool((t == (5.0 if accumulate else 0.0)).all()), k
+    # what a gradient needs apart from the batch is still asked for
+    back = lambda *frozen, **kw: bd.lobra_mlora_block_norm_bwd(plan, cfg, e, e, *frozen, st, st, e, e, e, e, **kw, ws=ws, check=False)
+    g1 = torch.zeros(n, d, device=DEV)
+    assert back(w, None, w, dgate=g1) == -1 and back(None, gate, w, dw_post=g1) == -1 and back(w, gate, None, dw_pre=g1) == -1
+
+
 # ------------------------------------------------------------------------------------------------------------------
 # gated feed-forward block
 # ------------------------------------------------------------------------------------------------------------------
