@@ -409,6 +409,8 @@ LOBRA_API lobra_status lobra_token_logprob_bwd(const lobra_logprob_desc *desc, c
  *     clip_scale_t = grad_scale_t min(1, max_norm_t / norm_t)
  * which is what lobra_mlora_adam_step takes as its grad_scale, so that clipping costs no pass of its own.  A norm that is not finite
  * stops its task alone: clip_scale_t = 0 and step_out_t = 0, at which Adam leaves the task's rows as they are (else step_out_t = step_t).
+ * (step_t: the 1-based count of the step being taken, as in Adam.  A task that is left out has not taken it: the caller counts the step only where
+ * step_out_t > 0.)
  * Squares are summed in fp64: no gradient that fp32 holds overflows or vanishes, and the order is fixed.
  *   max_norm    : device fp32 [n_tasks]; NULL, or a value that is negative or NaN: no limit
  *   grad_scale  : device fp32 [n_tasks] or NULL (1);  step, step_out : device int32 [n_tasks], step_out may be step; both or neither

@@ -133,9 +133,11 @@ class JointStep:
                                      a["gu"], self.dx if l else None, blk["dA_gu"], blk["dB_gu"], 0 if l else lo.FLAG_NO_DX, self.ws)
 
     def update(self):
-        """Clips every task's gradients to its max_norm and takes a step: Adam for the adapters, plain descent for the gates."""
-        self.steps += 1
-        lobra.lobra_grad_clip(self.grads, self.max_norm, None, self.steps, self.norm, self.clip_scale, self.step_now, 0, self.ws)
+        """Clips every task's gradients to its max_norm and takes a step: Adam for the adapters, plain descent for the gates.  A task whose norm is
+        not finite is left out: its parameters, moments and count stay."""
+        torch.add(self.steps, 1, out=self.step_now)
+        lobra.lobra_grad_clip(self.grads, self.max_norm, None, self.step_now, self.norm, self.clip_scale, self.step_now, 0, self.ws)
+        self.steps += self.step_now > 0               # (a task that is left out has not taken its step)
         for blk in self.blocks:
             for name, plan in (("gu", self.p_gu), ("down", self.p_down)):
                 a, b = "A_" + name, "B_" + name
