@@ -376,8 +376,8 @@ LOBRA_API lobra_status lobra_mlora_block_norm_bwd(const lobra_mlora_plan *plan, 
  *     lse = ln sum_j exp(z_j)    logp = z_target - lse    entropy = - sum_j p_j ln p_j
  *     dz_j = dlogp (1[j = target] - p_j) - dentropy p_j (ln p_j + entropy)
  * A target outside [0, V) (a prompt or pad token) is none: logp is 0, and dlogp of that row is ignored.  Logits of -inf (barred tokens)
- * have p = 0 and gradient 0.  A row of nothing else: lse = -inf, logp = -inf, entropy = 0, gradient 0.  A row with NaN or +inf:
- * lse, logp and entropy are NaN.
+ * have p = 0 and gradient 0; a barred target has logp = -inf and, as the formula says, the gradient dlogp.  A row of nothing else: lse = -inf,
+ * logp = -inf, entropy = 0, gradient 0.  A row with NaN or +inf: lse, logp and entropy are NaN.
  *   logits              : device, row i at logits + i ld elements, 16-byte aligned (ld need not keep the rows aligned)
  *   target              : device int32 [T], or NULL: no row has one
  *   logp, lse, entropy  : device fp32 [T], each may be NULL

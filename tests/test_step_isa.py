@@ -70,3 +70,34 @@ def test_lds_writes_are_waited_for(tmp_path, source):
 @pytest.mark.parametrize("source,least", [("gemm_persistent_gated.hip", 4), ("gated_skinny.hip", 6), ("logprob.hip", 16), ("grad_clip.hip", 3), ("gated.hip", 8)])
 def test_no_scratch_memory(tmp_path, source, least):
     SCRATCH(tmp_path, source, least)
+
+
+# Registers that do not fit and stand in scratch memory, bytes a lane at most.  The norms' backward kernels with sums over tokens hold a row, (one
+# packet a lane) the next one, gains, the task's gate and three fp32 sums per element: more than the 128 registers that 16 waves a compute unit
+# leave.  The four-block fp32 product of few tokens is at the 256 of two workgroups.  None of them waits for copies by count, which scratch
+# memory's loads would disturb.  (element type, threads of a team, packets of a lane, sums)
+NORM_BACKWARD = {("t", 64, 1, 1): 40, ("t", 256, 1, 1): 40, ("t", 512, 1, 1): 40, ("t", 1024, 2, 1): 360,
+                 ("f", 1024, 2, 1): 120, ("f", 1024, 4, 1): 620, ("f", 1024, 4, 0): 180}
+
+
+@pytest.mark.parametrize("source,kernels", [("block_norm.hip", 104), ("gated_few_f32.hip", 6)])
+def test_scratch_memory_has_its_bounds(tmp_path, source, kernels):
+    out = str(tmp_path / "k.s")
+    cmd = [HIPCC, "--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang",
+           "-packed-fp32-ops", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-x", "hip", "--cuda-device-only",
+           "-S", os.path.join(CSRC, source), "-o", out]
+    r = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stderr[-3000:]
+    parts = re.split(r"^\s*\.amdhsa_kernel (\w+)$", open(out).read(), flags=re.M)
+    sizes = {name: int(re.search(r"; ScratchSize: (\d+)", body).group(1)) for name, body in zip(parts[1::2], parts[2::2])}
+    assert len(sizes) == kernels, (source, len(sizes))
+    for name, size in sizes.items():
+        most = 72 if "gated_few_kernelILi4E" in name else 0
+        m = re.search(r"block_norm_bwd_kernelI([ft])Lb[01]ELi(\d+)ELi(\d)ELb([01])ELb[01]E", name)
+        if m:
+            most = NORM_BACKWARD.get((m.group(1), int(m.group(2)), int(m.group(3)), int(m.group(4))), 0)
+        assert size <= most, (name, size, most)
+
+
+def test_lds_writes_of_the_fp32_product_of_few_tokens_are_waited_for(tmp_path):
+    test_lds_writes_are_waited_for(tmp_path, "gated_few_f32.hip")

@@ -192,6 +192,30 @@ def test_logprob_backward(dtype, in_place, T, V, pad, kind, with_ent):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logprob_of_a_barred_target(dtype):
+    """logp is -inf; the gradient is dlogp at the target, -dlogp p elsewhere, 0 at the other barred tokens."""
+    T, V = 3, 1000
+    z = torch.randn(T, V, generator=torch.Generator().manual_seed(2))
+    z[:, 100:200] = -math.inf
+    z = z.to(DT[dtype])
+    target, w = torch.tensor([150, 199, 5], dtype=torch.int32), torch.tensor([0.75, -2.0, 1.0])
+    desc, zd = bd.make_logprob_desc(dtype, T, V), z.to(DEV)
+    logp, lse, rest, dz = torch.empty(T, device=DEV), torch.empty(T, device=DEV), torch.empty(T, device=DEV), torch.empty_like(zd)
+    bd.lobra_token_logprob_fwd(desc, zd, target.to(DEV), logp, lse, rest)
+    bd.lobra_token_logprob_bwd(desc, zd, target.to(DEV), lse, rest, None, w.to(DEV), None, dz)
+    torch.cuda.synchronize()
+    assert logp[:2].tolist() == [-math.inf, -math.inf] and math.isfinite(float(logp[2]))
+    ref = -w.double()[:, None] * torch.softmax(z.double(), dim=1)
+    ref[torch.arange(T), target.long()] += w.double()
+    assert dz[0, 150].item() == 0.75 and dz[1, 199].item() == -2.0
+    others = dz[:, 100:200].clone()
+    others[0, 50], others[1, 99] = 0, 0
+    assert not bool(others.any())
+    near(dz, ref, dtype, "dlogits", scale=2.0)
+
+
+@pytest.mark.gpu
 def test_logprob_gradient_against_differences():
     T, V, eps = 6, 777, 2e-2
     g = torch.Generator(device=DEV).manual_seed(5)
