@@ -94,6 +94,31 @@ def test_gradients_of_the_whole_step_and_serving():
     assert torch.equal(top[1][:, 0].long(), step.logits.argmax(dim=1))
 
 
+def test_gradients_of_the_whole_step_in_bf16():
+    """The step in bf16 against 64 bits from the same bf16 parameters.  What is stored is rounded to 2^-8 of itself at most: some 15 tensors lie
+    between the embedding and a gradient of the first block and back, so 15 * 2^-8 = 6e-2 of a tensor's largest."""
+    from paper_2509_01193_amd.joint_step import JointStep
+    seg_off, seg_task = [0, 170, 300, 310, 450], [1, 0, -1, 1]
+    step = JointStep("bf16", 256, 384, 1000, 2, [8, 16], seg_off, seg_task)
+    gen = torch.Generator().manual_seed(4)
+    for blk in step.blocks:
+        for k in ("B_gu", "B_down"):
+            blk[k].copy_(torch.randn(blk[k].shape, generator=gen) * 0.1)
+        blk["gate"].copy_(torch.randn(blk["gate"].shape, generator=gen))
+    tokens = torch.randint(1000, (450,), generator=gen).cuda()
+    target = torch.randint(1000, (450,), generator=gen).int()
+    target[5], target[400] = -100, 1000
+    target, dlogp = target.cuda(), torch.randn(450, generator=gen).cuda()
+    logp, leaves = reference(step, tokens, target, seg_off, seg_task, dlogp)
+    got = step.forward(tokens, target).clone()
+    step.backward(target, dlogp)
+    torch.cuda.synchronize()
+    close(got, logp, "logp", 6e-2)
+    for i, (blk, p) in enumerate(zip(step.blocks, leaves)):
+        for k, v in p.items():
+            close(blk["d" + k], v.grad, "block %d, d%s" % (i, k), 6e-2)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_the_example_learns(dtype, capsys):
     from paper_2509_01193_amd import joint_step

@@ -605,6 +605,17 @@ def test_block_norm(dtype, T, d, batch, form):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,T,d,batch,form", [
+    ("bf16", 120, 2560, "mixed", "all"), ("bf16", 75, 4608, "mixed", "plain"), ("bf16", 75, 5120, "mixed", "all"), ("bf16", 40, 6144, "tokens", "all"),
+    ("bf16", 33, 6152, "mixed", "no_gate"), ("bf16", 20, 12288, "mixed", "all"), ("f32", 30, 2560, "mixed", "plain"), ("f32", 30, 5121, "mixed", "all"),
+    ("f32", 15, 12289, "mixed", "no_dr"),
+])
+def test_block_norm_between_the_widths_of_whole_teams(dtype, T, d, batch, form):
+    """Rows that leave lanes or whole waves of their team without a packet."""
+    test_block_norm(dtype, T, d, batch, form)
+
+
+@pytest.mark.gpu
 def test_block_norm_gradient_against_differences():
     T, d, n, eps = 20, 96, 2, 1e-2
     g = torch.Generator(device=DEV).manual_seed(3)
@@ -925,6 +936,30 @@ def test_gated_refusals():
     assert bwd() == bd.OK
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", [bd.ACT_SILU, bd.ACT_GELU_TANH])
+@pytest.mark.parametrize("T,d,f,keep", [(1, 512, 72, False), (40, 512, 1376, True), (128, 1000, 264, False), (192, 4096, 1376, False), (192, 4096, 1376, True),
+                                        (2100, 512, 1160, False), (4500, 256, 1024, True)])
+def test_gated_output_starts_from_unrounded_projections(T, d, f, keep, act):
+    """bf16, no adapters: one rounding of h (2^-8 of it at most) next to fp32 sums, in the forms that have the projections in fp32.  From [g | u] as
+    rounded it would be off by up to 2^-8 (1 + |g a' / a|) more, which the same bound does not hold."""
+    v = gated_inputs("bf16", T, d, f, [8], T * f)
+    plan = bd.Plan("bf16", T, d, 2 * f, None, [0, T], [-1], n_proj=2)
+    y = v["x"].double() @ v["W"].double()
+    h_of = lambda y: act64(act, y[:, :f])[0] * y[:, f:]
+    ref = h_of(y)
+    gu = torch.empty(T, 2 * f, dtype=torch.bfloat16, device=DEV) if keep else None
+    h = torch.empty(T, f, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(max(bd.lobra_mlora_gated_workspace_bytes(plan, keep), 16), dtype=torch.uint8, device=DEV)
+    bd.lobra_mlora_gated_fwd(plan, act, v["x"].to(DEV), v["W"].to(DEV), None, None, None, gu, h, None, ws)
+    torch.cuda.synchronize()
+    near(h, ref, "bf16", "h")
+    if gu is not None:
+        near(gu, y, "bf16", "gu")
+    with pytest.raises(AssertionError):               # (the bound can tell)
+        near(h_of(y.bfloat16().double()).bfloat16(), ref, "bf16", "h")
+
+
 def _typed_calls():
     """name -> (call with keyword arguments in the place of its own, names of tensors of the plan's type, names of fp32 ones); plans of the
     host alone, which the library itself refuses."""
@@ -996,6 +1031,65 @@ def test_on_another_stream_and_in_a_graph():
         z.mul_(0.9).add_(0.01 * k)
         b.mul_(1.1)
         grads[1].mul_(1.5)
+        work()
+        torch.cuda.synchronize()
+        ref = [o.clone() for o in outs]
+        for o in outs:
+            o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, q) for o, q in zip(outs, ref)), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,T,d,f,form", [("bf16", 40, 512, 264, "few tokens"), ("bf16", 192, 4096, 136, "split product"), ("bf16", 2304, 512, 1024, "persistent"),
+                                              ("f32", 40, 260, 72, "few tokens"), ("f32", 300, 96, 200, "the layer's product")])
+def test_passes_with_their_gradients_on_another_stream_and_in_a_graph(dtype, T, d, f, form):
+    """Gated block and norms, both passes, and clipped gradients written: on a stream of their own, captured, and replayed on new inputs."""
+    n, edt = 2, DT[dtype]
+    g = torch.Generator(device=DEV).manual_seed(T)
+    mk = lambda *s, std=1.0: (torch.randn(*s, device=DEV, generator=g) * std).to(edt)
+    new = lambda *s, dt=edt: torch.empty(*s, dtype=dt, device=DEV)
+    off, task = [0, T // 3, T - 5, T], [1, -1, 0]
+    plan, cfg = bd.Plan(dtype, T, d, 2 * f, [0, 16, 48], off, task, n_proj=2), bd.BlockNormConfig(1e-5, 0.5)
+    r, b, w_post, gate, w_pre, dh, dro = mk(T, d), mk(T, d), mk(d), mk(n, d), mk(d), mk(T, f), mk(T, d)
+    W, A, B, s = mk(d, 2 * f, std=d ** -0.5), mk(48, d, std=d ** -0.5), mk(48, f, std=0.3), torch.ones(n, device=DEV)
+    ro, x, h, h0, gu, dgu, dx, dr, db = new(T, d), new(T, d), new(T, f), new(T, f), new(T, 2 * f), new(T, 2 * f), new(T, d), new(T, d), new(T, d)
+    f32 = torch.float32
+    rp, rr, dA, dB, dgate, dwo, dwr = new(T, dt=f32), new(T, dt=f32), new(48, d, dt=f32), new(48, f, dt=f32), new(n, d, dt=f32), new(d, dt=f32), new(d, dt=f32)
+    cA, cB, norm, scale, limit = new(48, d, dt=f32), new(48, f, dt=f32), new(n, dt=f32), new(n, dt=f32), torch.full((n,), 0.1, device=DEV)
+    gset = bd.GradSet([(dA, cA, [0, 16, 48]), (dB, cB, [0, 16, 48]), (dgate, None, [0, 1, 2])], n)
+    hs = new(max(plan.h_save_bytes, 16), dt=torch.uint8)
+    ws = new(max(bd.lobra_mlora_gated_workspace_bytes(plan, True), bd.lobra_mlora_gated_workspace_bytes(plan, False), plan.bwd_ws_bytes,
+                 bd.lobra_mlora_block_norm_workspace_bytes(plan), gset.ws_bytes), dt=torch.uint8)
+
+    def work():
+        bd.lobra_mlora_block_norm_fwd(plan, cfg, r, b, w_post, gate, w_pre, ro, x, rp, rr)
+        bd.lobra_mlora_gated_fwd(plan, 0, x, W, A, B, s, None, h0, None, ws)
+        bd.lobra_mlora_gated_fwd(plan, 0, x, W, A, B, s, gu, h, hs, ws)
+        bd.lobra_mlora_gated_bwd(plan, 0, x, W, A, B, s, gu, dh, hs, dgu, dx, dA, dB, 0, ws)
+        bd.lobra_mlora_block_norm_bwd(plan, cfg, ro, b, w_post, gate, w_pre, rp, rr, dro, dx, dr, db, dgate, dwo, dwr, 0, ws)
+        bd.lobra_grad_clip(gset, limit, None, None, norm, scale, None, ws=ws)
+
+    outs = (ro, x, rp, rr, h0, gu, h, dgu, dx, dA, dB, dr, db, dgate, dwo, dwr, norm, scale, cA, cB)
+    work()
+    torch.cuda.synchronize()
+    ref = [o.clone() for o in outs]
+    assert all(bool(torch.isfinite(o).all()) for o in ref)
+    for o in outs:
+        o.fill_(float("nan"))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        work()
+    side.synchronize()
+    assert all(torch.equal(o, q) for o, q in zip(outs, ref))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for k in range(3):
+        b.mul_(1.25).add_(0.01 * k)
+        dh.mul_(0.5)
         work()
         torch.cuda.synchronize()
         ref = [o.clone() for o in outs]
