@@ -40,6 +40,8 @@ size_t gated_skinny_bytes(const Plan& p)
     return (p.mfma ? gated_skinny_ws_bytes : gated_few_ws_bytes)(p.desc.T, p.desc.d_in, p.dg, p.tb.empty() ? 0 : p.r_max);
 }
 
+// (The forms below that project in a launch of their own hand the projected activations s_t A_t x on as the layer does, rounded to bf16: operands of
+// the matrix instructions in the up projection and in dB.  The few-token kernels keep them in fp32.)
 // A layer product whose K is split leaves its fp32 sums to the activation, if the workspace has room for those of both projections.
 size_t gated_sums_bytes(const Plan& p) { return p.mfma && p.desc.T > 0 ? p.fwd_part * (p.fwd_group > 0 ? 1 : 2) : 0; }
 

@@ -6,11 +6,16 @@
 //     dgate_t = alpha w_post sum_t g bh   dw_post = alpha sum gate_t g bh   dw_pre = sum dx rh
 // The two means of backward are one reduction: with s1 = sum u rh, s2 = sum q bh (dr' + m u), s3 = sum q bh rh, mean(u rh) = s1 / d and
 // mean(q g bh) = (s2 - m s1 / d s3) / d.
-// A row lives in the registers of a team of threads - a wave, or a workgroup of up to 1024 - from its read to its write.  Backward's teams take
-// neighbouring rows and keep the sums over tokens in registers from row to row; they write them out where their rows end, the gate's also where a
+// Forward, a row lives in the registers of a team of threads - a wave, or a workgroup of up to 1024 - from its read to its write.  Backward's teams
+// take neighbouring rows and keep the sums over tokens from row to row; they write them out where their rows end, the gate's also where a
 // segment ends (slot: team + segment, which no two runs share; the slots' tasks stand beside them), and a second launch adds them in order.
+// A row, the next one, gains, gate and sums are more than the 128 registers that 16 waves a compute unit leave to each; what does not fit is in
+// scratch memory, bytes a lane with sums: bf16 32 - 36 at one packet a lane (teams of up to 512), 356 at two (d > 8192); fp32 104 - 116 at two (d >
+// 4096), 604 - 616 at four (d > 8192; without sums 136 - 176).  The few of the first are not seen in the time; the others are what bounds the pass.
 // Bound: memory, 4 T d elements forward and 6 T d backward.  Measured, us: 16384 x 4096 bf16 forward 102 .. 114 (of 537 MB, 5.0 TB/s), backward
-// 161 .. 173 (805 MB, 4.8 TB/s) and its sums' launch 7; 2999 x 1025 fp32, out of the caches, 15, 22 and 5; 40 x 4096 forward 4.
+// 161 .. 178 (805 MB, 4.7 TB/s) and its sums' launch 7; 2999 x 1025 fp32, out of the caches, 15, 22 and 5; 40 x 4096 forward 4.  Widths between those
+// of whole teams leave lanes idle: bf16 forward, TB/s, 2560 3.9, 4096 4.7, 5120 4.1, 6144 4.3, 8192 4.9; backward with sums 3.8, 4.5, 4.6, 4.6, 4.7.
+// Scratch memory, backward with / without sums: bf16 4096 x 12288 574 / 125, 4096 x 16384 618 / 153; fp32 4096 x 8192 191 / 149, 2048 x 16384 571 / 245.
 #include <algorithm>
 
 #include "kernels.h"
