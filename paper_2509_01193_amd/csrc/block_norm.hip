@@ -11,7 +11,7 @@
 // segment ends (slot: team + segment, which no two runs share; the slots' tasks stand beside them), and a second launch adds them in order.
 // A row, the next one, gains, gate and sums are more than the 128 registers that 16 waves a compute unit leave to each; what does not fit is in
 // scratch memory, bytes a lane with sums: bf16 32 - 36 at one packet a lane (teams of up to 512), 356 at two (d > 8192); fp32 104 - 116 at two (d >
-// 4096), 604 - 616 at four (d > 8192; without sums 136 - 176).  The few of the first are not seen in the time; the others are what bounds the pass.
+// 4096), 604 - 616 at four (d > 8192; without sums 136 - 176).  (The first were not timed apart; the widest are what bounds the pass.)
 // Bound: memory, 4 T d elements forward and 6 T d backward.  Measured, us: 16384 x 4096 bf16 forward 102 .. 114 (of 537 MB, 5.0 TB/s), backward
 // 161 .. 178 (805 MB, 4.7 TB/s) and its sums' launch 7; 2999 x 1025 fp32, out of the caches, 15, 22 and 5; 40 x 4096 forward 4.  Widths between those
 // of whole teams leave lanes idle: bf16 forward, TB/s, 2560 3.9, 4096 4.7, 5120 4.1, 6144 4.3, 8192 4.9; backward with sums 3.8, 4.5, 4.6, 4.6, 4.7.

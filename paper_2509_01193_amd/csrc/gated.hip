@@ -3,8 +3,8 @@
 //     gelu: a = g (1 + th) / 2, a' = (1 + th) / 2 + g (1 - th^2) / 2 c (1 + 3 k g^2), th = tanh(c (g + k g^3))
 // f is a multiple of 8, so that rows of all three tensors keep 16-byte packets.
 // Roundings (bf16): h starts here from [g | u] as stored, which is off by up to 2^-8 of each; the forms that hold the fp32 projections do not use this
-// kernel.  [dg | du] is rounded because the products that read it (dx, dA, dB) take bf16 operands.  Mean error of h, dA and dB, as stored, of their mean
-// size: 0.0030, where the rounding of the result alone leaves 0.0017.
+// kernel.  [dg | du] is rounded because the products that read it (dx, dA, dB) take bf16 operands.  Error of h from here, and of dA and dB rounded to
+// bf16 (2-norms, of the result's): 0.0030, where the rounding of the result alone leaves 0.0017.
 // Bound: memory.  Measured: backward of 16384 x 2 x 11008 bf16 335 us (of 1804 MB, 5.4 TB/s), of 8190 x 2 x 1376 20.  A pass that derives and
 // projects (G of [dg | du]) per token block reads two tensors less but reaches 3.9 TB/s like the projection's own: 475 us against 335 + 184
 // there, nothing gained at 1376 columns, 10 - 25 % lost where segments have 3 to 20 tokens; not kept.
