@@ -960,6 +960,32 @@ def test_gated_output_starts_from_unrounded_projections(T, d, f, keep, act):
         near(h_of(y.bfloat16().double()).bfloat16(), ref, "bf16", "h")
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gated_block_and_loss_of_an_empty_batch(dtype):
+    """Tensors of no rows, which have no address: the adapters' gradients are 0, or stay as they are where they are added to."""
+    d, f, edt = 64, 72, DT[dtype]
+    plan = bd.Plan(dtype, 0, d, 2 * f, [0, 16, 48], [0, 0], [1], n_proj=2)
+    v = gated_inputs(dtype, 0, d, f, [8, 16], 1)
+    w = [v[k].to(DEV) for k in ("x", "W", "A", "B", "s")]
+    e = lambda c, dt=edt: torch.empty(0, c, dtype=dt, device=DEV)
+    for save in (False, True):
+        ws = torch.empty(bd.lobra_mlora_gated_workspace_bytes(plan, save), dtype=torch.uint8, device=DEV)
+        bd.lobra_mlora_gated_fwd(plan, 0, *w, e(2 * f) if save else None, e(f), e(0, torch.uint8) if save else None, ws)
+    for flags, want in ((0, 0.0), (bd.FLAG_ACCUMULATE_GRADS, 5.0), (bd.FLAG_NO_DX, 0.0)):
+        (dA, okA), (dB, okB) = guarded(48, d, dtype=torch.float32), guarded(48, f, dtype=torch.float32)
+        dA.fill_(5.0)
+        dB.fill_(5.0)
+        ws = torch.empty(plan.bwd_ws_bytes, dtype=torch.uint8, device=DEV)
+        bd.lobra_mlora_gated_bwd(plan, 0, *w, e(2 * f), e(f), None, e(2 * f), e(d), dA, dB, flags, ws)
+        torch.cuda.synchronize()
+        assert okA() and okB() and bool((dA == want).all()) and bool((dB == want).all())
+    desc, row, ids = bd.make_logprob_desc(dtype, 0, 100, top_k=3), torch.empty(0, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV)
+    bd.lobra_token_logprob_fwd(desc, e(100), ids, row, row, row, row, e(3, torch.float32), e(3, torch.int32))
+    bd.lobra_token_logprob_bwd(desc, e(100), ids, row, row, row, row, row, e(100))
+    torch.cuda.synchronize()
+
+
 def _typed_calls():
     """name -> (call with keyword arguments in the place of its own, names of tensors of the plan's type, names of fp32 ones); plans of the
     host alone, which the library itself refuses."""
