@@ -4,7 +4,7 @@ and in 64 bits.
 A case is a plain dict.  Its `kind` says which operator one pass goes through:
 
   q8        the LoRA linear on a frozen base held in 8-bit integers with a scale per channel, the tokens quantised with a scale each as
-            they come: lobra_mlora_q8_fwd, with `back` also lobra_mlora_q8_bwd
+            they come: lobra_mlora_quant_fwd, with `back` also lobra_mlora_quant_bwd
   distill   the loss of rows of logits against the likeliest tokens of a teacher, and the gradient of the logits:
             lobra_token_distill_fwd, _bwd
   beam      a step of beam search: the best continuations over the beams and the vocabulary of every request, then what is kept per
@@ -188,11 +188,11 @@ def prepare(case, seed):
     if kind == "q8":
         T, d, f = case["T"], case["d_in"], case["d_out"]
         st["plan"] = lobra.Plan("bf16", T, d, f, st["rank_off"], st["off"], st["task"])
-        st["Wq"], st["w_scale"] = empty(f, lobra.lobra_q8_pitch(d), dtype=torch.int8), empty(f)
-        lobra.lobra_q8_quantise_weight(st["W"], st["Wq"], st["w_scale"])
+        st["Wq"], st["w_scale"] = empty(f, lobra.lobra_quant_pitch(d), dtype=torch.int8), empty(f)
+        lobra.lobra_quantise_weight(st["W"], st["Wq"], st["w_scale"])
         del st["W"]
         st["y"] = empty(T, f, dtype=dt)
-        fwd, bwd = lobra.lobra_mlora_q8_workspace_bytes(st["plan"])
+        fwd, bwd = lobra.lobra_mlora_quant_workspace_bytes(st["plan"])
         st["ws"] = empty(max(fwd, bwd if case["back"] else 0, 16), dtype=torch.uint8)
         if case["back"]:
             st.update(dx=empty(T, d, dtype=dt), dA=torch.empty_like(st["A"], dtype=torch.float32), dB=torch.empty_like(st["B"], dtype=torch.float32))
@@ -223,10 +223,10 @@ def _own_q8(st):
     from paper_2509_01193_amd import binding as lobra
     w = (st["x"], st["Wq"], st["w_scale"], st["A"], st["B"], st["s"])
     if not st["case"]["back"]:
-        lobra.lobra_mlora_q8_fwd(st["plan"], *w, st["y"], None, st["ws"])
+        lobra.lobra_mlora_quant_fwd(st["plan"], *w, st["y"], None, st["ws"])
         return dict(y=st["y"])
-    lobra.lobra_mlora_q8_fwd(st["plan"], *w, st["y"], st["h_save"], st["ws"])
-    lobra.lobra_mlora_q8_bwd(st["plan"], *w, st["dy"], st["h_save"], st["dx"], st["dA"], st["dB"], 0, st["ws"])
+    lobra.lobra_mlora_quant_fwd(st["plan"], *w, st["y"], st["h_save"], st["ws"])
+    lobra.lobra_mlora_quant_bwd(st["plan"], *w, st["dy"], st["h_save"], st["dx"], st["dA"], st["dB"], 0, st["ws"])
     # the adapters' gradients: summed in 32 bits over a step's chunks, handed on in the adapters' type, as an exchange between replicas takes them
     return dict(y=st["y"], dx=st["dx"], dA=st["dA"].to(st["A"].dtype), dB=st["dB"].to(st["B"].dtype))
 
