@@ -403,6 +403,111 @@ LOBRA_API lobra_status lobra_token_logprob_bwd(const lobra_logprob_desc *desc, c
                                      const float *lse, const float *lse_rest, const float *entropy, const float *dlogp,
                                      const float *dentropy, void *dlogits, void *hip_stream);
 
+/* ---- an 8-bit base (section 2.1: the layer, its frozen W held in 8-bit integers) --------------------------------------------------------
+ *
+ * W is frozen, so it can be kept as whole numbers q between -127 and 127 with a scale per output channel, at half of bf16's bytes, and a token
+ * quantised as it comes with a scale of its own is multiplied with it in whole numbers, at twice the rate.  The adapters stay as they are:
+ *     y_i = sx_i sw (qx_i Wq) + s_t (A_t x_i) B_t          sx_i = max |x_i| / 127,  qx_i = x_i / sx_i
+ *     dx_i = dy_i Ŵ^T + s_t (B_t dy_i) A_t                 Ŵ = sw Wq;  dA, dB as ever, from x
+ * with quotients rounded to the nearest whole number, halves to the even one, and whole sums (d_in <= LOBRA_MAX_QUANT_IN).  Backward passes by the
+ * rounding of x, as if it were none; Ŵ is rounded to bf16 there.  A token (channel) that holds NaN or infinity makes its row (column) of y NaN;
+ * one whose largest magnitude is below 127 x 2^-126 counts as zeros.
+ *
+ * lobra_quantise_weight: once per weight, W [d_in, d_out] of element type `dtype`, row i at W + i ldw elements (0: d_out) ->
+ *   Wq      : device int8 [d_out, lobra_quant_pitch(d_in)], 16-byte aligned: a row per channel, zero beyond d_in
+ *   w_scale : device fp32 [d_out], 16-byte aligned */
+enum { LOBRA_MAX_QUANT_IN = 1 << 17 };
+LOBRA_API int64_t lobra_quant_pitch(int32_t d_in);        /* bytes of a row of Wq: the next multiple of 256; 0 for d_in < 1 */
+LOBRA_API lobra_status lobra_quantise_weight(int32_t dtype, int32_t d_in, int32_t d_out, int64_t ldw, const void *W, int8_t *Wq,
+                                      float *w_scale, void *hip_stream);
+/* The layer on such a base, for a bf16 plan of any n_proj (projection j: rows j dg .. of Wq and w_scale).  The arguments are those of
+ * lobra_mlora_plan_fwd / _bwd, and h_save is what lobra_mlora_plan_fwd writes.
+ *   ws : lobra_mlora_quant_workspace_bytes (either out pointer may be NULL); all of it is needed: the quantised tokens and a split product's
+ *        sums, in backward Ŵ in front of the plan's own
+ * LOBRA_ERR_DTYPE for an fp32 plan or one of plain kernels, LOBRA_ERR_SHAPE for d_in above LOBRA_MAX_QUANT_IN. */
+LOBRA_API lobra_status lobra_mlora_quant_workspace_bytes(const lobra_mlora_plan *plan, size_t *fwd_bytes, size_t *bwd_bytes);
+LOBRA_API lobra_status lobra_mlora_quant_fwd(const lobra_mlora_plan *plan, const void *x, const int8_t *Wq, const float *w_scale, const void *A,
+                                const void *B, const float *s, void *y, void *h_save, void *ws, size_t ws_bytes, void *hip_stream);
+LOBRA_API lobra_status lobra_mlora_quant_bwd(const lobra_mlora_plan *plan, const void *x, const int8_t *Wq, const float *w_scale, const void *A,
+                                const void *B, const float *s, const void *dy, const void *h_saved, void *dx, float *dA, float *dB,
+                                uint32_t flags, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* ---- rows of logits beyond their own tokens: a teacher's, and a beam's -------------------------------------------------------------------
+ *
+ * Loss of rows of logits against the likeliest tokens of a teacher, and the gradient.  Row i has up to top_k tokens with the teacher's log
+ * probabilities l_j (what lobra_token_logprob_fwd writes as top_logp and top_id).  With p = softmax(z / temperature) over the vocabulary:
+ *     tail = 0:  q = softmax(l / temperature) over the row's tokens        loss = sum_j q_j (ln q_j - ln p_j)
+ *     tail = 1:  q_j = exp(l_j) (l at the temperature), and all tokens that are not listed count as one more with the probabilities q_r =
+ *                1 - sum q_j and p_r = sum of p over them:                 loss = sum_j q_j (ln q_j - ln p_j) + q_r (ln q_r - ln p_r)
+ *                (q_r below 2^-20 is the rounding of the l_j, and counts as 0)
+ *     dz_j = dloss / temperature ((q_r + sum q) p_j - q_j [listed] - q_r p_j / p_r [not listed, tail])
+ * A place of the list with an id outside [0, V) is empty, one with l = -inf has the probability 0.  A row without a token is one without a
+ * teacher: loss 0, gradient 0.  A token that is listed twice counts twice.  Logits of -inf have p = 0; where the teacher gives them a
+ * probability the loss is infinite and the gradient what the formula says.  A row with NaN or +inf, of the logits or the listed l: loss NaN, and so its gradient.
+ * All sums in fp32, fixed order; q_r and sums over the list in fp64.
+ *   logits, dlogits : as in lobra_token_logprob_fwd / _bwd; dlogits may be logits itself
+ *   teacher_logp, teacher_id : device fp32 / int32 [T, top_k]
+ *   loss            : device fp32 [T] or NULL
+ *   stat            : device fp32 [T, 4], 16-byte aligned, what backward starts from; or NULL
+ *   dloss           : device fp32 [T].  A row in which it is 0 gets a gradient of 0, whatever its logits
+ *   flags           : LOBRA_FLAG_ACCUMULATE_GRADS: added to dlogits (the gradient of another loss of the same logits), which is not logits then
+ * (LOBRA_ERR_SHAPE if it is)
+ * LOBRA_ERR_SHAPE for a temperature that is not positive and finite, or 1 / temperature not finite. */
+enum { LOBRA_MAX_TEACHER = 128 };
+typedef struct {
+    int32_t dtype;           /* lobra_dtype of logits and dlogits */
+    int32_t V;               /* 1 .. LOBRA_MAX_VOCAB */
+    int64_t T;               /* rows, 0 <= T < 2^31 */
+    int64_t ld;              /* row pitch in elements, >= V (0: V), T ld < 2^60 */
+    int32_t top_k;           /* 1 .. LOBRA_MAX_TEACHER */
+    int32_t tail;            /* 0 or 1 */
+    float temperature;
+} lobra_distill_desc;
+LOBRA_API lobra_status lobra_token_distill_fwd(const lobra_distill_desc *desc, const void *logits, const float *teacher_logp,
+                                     const int32_t *teacher_id, float *loss, float *stat, void *hip_stream);
+LOBRA_API lobra_status lobra_token_distill_bwd(const lobra_distill_desc *desc, const void *logits, const float *teacher_logp,
+                                     const int32_t *teacher_id, const float *stat, const float *dloss, void *dlogits, uint32_t flags,
+                                     void *hip_stream);
+
+/* A step of beam search: of every request the n_out best continuations over its beams and the vocabulary.  A beam b of score s continued by
+ * token j has s + ln softmax(z_b)_j, in fp64; the largest come first, among equals the lowest beam, then the lowest token.  No continuations:
+ * logits of -inf; a beam whose score is -inf or NaN (its logits are not looked at); a beam whose logits hold NaN or +inf.
+ *   logits      : device, row (request * beams + beam) at logits + row ld elements, 16-byte aligned (ld need not keep the rows aligned)
+ *   score       : device fp32 [n_req, beams], the beams' scores so far (-inf: no beam, as all but one at a request's first step)
+ *   done        : device int32 [n_req, beams] or NULL: where not 0 the beam is finished, its logits are not looked at, and its one
+ *                 continuation is done_token at the score it has
+ *   out_score, out_beam, out_token : device fp32, int32, int32 [n_req, n_out]; out_beam counts within the request.  Where nothing is left: -inf, -1, -1.
+ *                 out_score may be score where n_out = beams
+ *   ws          : lobra_beam_workspace_bytes */
+typedef struct {
+    int32_t dtype;           /* lobra_dtype of the logits */
+    int32_t V;               /* 1 .. LOBRA_MAX_VOCAB */
+    int64_t ld;              /* row pitch in elements, >= V (0: V), n_req beams ld < 2^60 */
+    int32_t n_req;           /* 0 <= n_req, n_req beams < 2^24 */
+    int32_t beams;           /* 1 .. LOBRA_MAX_TOP */
+    int32_t n_out;           /* 1 .. LOBRA_MAX_TOP */
+} lobra_beam_desc;
+LOBRA_API lobra_status lobra_beam_workspace_bytes(const lobra_beam_desc *desc, size_t *bytes);
+LOBRA_API lobra_status lobra_beam_select(const lobra_beam_desc *desc, const void *logits, const float *score, const int32_t *done,
+                               int32_t done_token, float *out_score, int32_t *out_beam, int32_t *out_token, void *ws, size_t ws_bytes,
+                               void *hip_stream);
+/* What is kept per sequence (tokens so far, caches), put in the order of the beams that go on: row (request, i) of dst becomes row
+ * (request, parent[request][i]) of src, for every tensor of the list.
+ *   states  : HOST array.  src, dst: device, n_req * beams rows of row_bytes, back to back; dst = src reorders in place (a row that stays costs
+ *             nothing), else the two do not overlap (LOBRA_ERR_SHAPE); nor do tensors of the list with each other
+ *   parent  : device int32, row of a request every parent_ld numbers (>= beams): out_beam of lobra_beam_select, for one (n_out >= beams).  Outside
+ *             [0, beams): row i of dst is left as it is
+ *   used    : device int32 [n_req] or NULL: only the first used unit_bytes bytes of a request's rows move, the rest of dst is left as it is
+ *             (caches that are filled up to the same length in all beams of a request; below 0: nothing, above row_bytes / unit_bytes: all) */
+typedef struct {
+    const void *src;
+    void *dst;
+    int64_t row_bytes;       /* >= 0; n_req beams row_bytes < 2^60 */
+    int64_t unit_bytes;      /* >= 0: bytes of a position; without `used` not looked at */
+} lobra_beam_state;
+LOBRA_API lobra_status lobra_beam_reorder(const lobra_beam_state *states, int32_t n_states, int32_t n_req, int32_t beams,
+                                const int32_t *parent, int64_t parent_ld, const int32_t *used, void *hip_stream);
+
 /* Norms of the tasks' gradients over many tensors, and clipping.  The set lists the gradients of all layers (dA and dB of each);
  * every tensor says with the rank_off of its layer which of its rows belong to which task.  Per task t
  *     norm_t = |grad_scale_t| sqrt(sum over all tensors and rows of t of g^2)
@@ -478,7 +583,8 @@ LOBRA_API lobra_status lobra_padded_segments(int64_t n_seq, const int32_t *padde
  * (host, may be NULL) counts the launches seen.  n_pairs = 0 or events = NULL detaches.
  * A plan with a trace attached must not be used from two threads at once. */
 enum { LOBRA_K_SHRINK = 1, LOBRA_K_GEMM = 2, LOBRA_K_GRAD_STAGE1 = 3, LOBRA_K_GRAD_STAGE2 = 4,
-       LOBRA_K_TOKEN_TASK = 5, LOBRA_K_ADAM = 6, LOBRA_K_SHRINK_GEMM = 7, LOBRA_K_GATED = 8, LOBRA_K_BLOCK_NORM = 9 };
+       LOBRA_K_TOKEN_TASK = 5, LOBRA_K_ADAM = 6, LOBRA_K_SHRINK_GEMM = 7, LOBRA_K_GATED = 8, LOBRA_K_BLOCK_NORM = 9,
+       LOBRA_K_QUANT = 10 };
 LOBRA_API lobra_status lobra_mlora_plan_set_trace(lobra_mlora_plan *plan, void *const *events,
                                         int32_t n_pairs, int32_t *kernel_ids,
                                         int32_t *n_launched);

@@ -25,6 +25,7 @@ Q_SLICED, Q_FUSED_WG_RUNS, Q_FUSED_RUN_ROW, Q_FUSED_COUNT, Q_FUSED_TASK_ROW = 8,
 Q_GEMM_TILE_ROWS, Q_BESIDE, Q_PRODUCT_TABLES = 13, 14, 15
 MAX_RANK = 128
 MAX_TOP, MAX_VOCAB, MAX_NORM_WIDTH = 32, 1 << 24, 16384
+MAX_QUANT_IN, MAX_TEACHER = 1 << 17, 128
 
 EXPORTS = [
     "lobra_mlora_validate", "lobra_mlora_workspace_bytes", "lobra_mlora_fwd", "lobra_mlora_bwd", "lobra_token_task_map",
@@ -37,6 +38,9 @@ EXPORTS = [
     "lobra_token_logprob_fwd", "lobra_token_logprob_bwd",
     "lobra_grad_set_device_bytes", "lobra_grad_set_create", "lobra_grad_set_init", "lobra_grad_set_destroy",
     "lobra_grad_set_workspace_bytes", "lobra_grad_clip",
+    "lobra_quant_pitch", "lobra_quantise_weight", "lobra_mlora_quant_workspace_bytes", "lobra_mlora_quant_fwd", "lobra_mlora_quant_bwd",
+    "lobra_token_distill_fwd", "lobra_token_distill_bwd",
+    "lobra_beam_workspace_bytes", "lobra_beam_select", "lobra_beam_reorder",
     "lobra_mlora_plan_set_trace", "lobra_status_string", "lobra_version",
 ]
 
@@ -69,6 +73,20 @@ class LogprobDesc(ctypes.Structure):
 class GradTensor(ctypes.Structure):
     _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("D", ctypes.c_int32),
                 ("rank_off", ctypes.POINTER(ctypes.c_int32))]
+
+
+class DistillDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("V", ctypes.c_int32), ("T", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("top_k", ctypes.c_int32), ("tail", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+class BeamDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("V", ctypes.c_int32), ("ld", ctypes.c_int64), ("n_req", ctypes.c_int32),
+                ("beams", ctypes.c_int32), ("n_out", ctypes.c_int32)]
+
+
+class BeamState(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("row_bytes", ctypes.c_int64), ("unit_bytes", ctypes.c_int64)]
 
 
 class LobraError(RuntimeError):
@@ -135,6 +153,17 @@ def lib():
         L.lobra_grad_set_destroy.argtypes = [vp]
         L.lobra_grad_set_workspace_bytes.argtypes = [vp, szp]
         L.lobra_grad_clip.argtypes = [vp] * 7 + [u32, vp, sz, vp]
+        i64 = ctypes.c_int64
+        L.lobra_quant_pitch.restype, L.lobra_quant_pitch.argtypes = i64, [i32]
+        L.lobra_quantise_weight.argtypes = [i32, i32, i32, i64] + [vp] * 4
+        L.lobra_mlora_quant_workspace_bytes.argtypes = [vp, szp, szp]
+        L.lobra_mlora_quant_fwd.argtypes = [vp] * 9 + [vp, sz, vp]
+        L.lobra_mlora_quant_bwd.argtypes = [vp] * 12 + [u32, vp, sz, vp]
+        L.lobra_token_distill_fwd.argtypes = [ctypes.POINTER(DistillDesc)] + [vp] * 6
+        L.lobra_token_distill_bwd.argtypes = [ctypes.POINTER(DistillDesc)] + [vp] * 6 + [u32, vp]
+        L.lobra_beam_workspace_bytes.argtypes = [ctypes.POINTER(BeamDesc), szp]
+        L.lobra_beam_select.argtypes = [ctypes.POINTER(BeamDesc)] + [vp] * 3 + [i32] + [vp] * 4 + [sz, vp]
+        L.lobra_beam_reorder.argtypes = [ctypes.POINTER(BeamState), i32, i32, i32, vp, i64, vp, vp]
         L.lobra_status_string.restype = ctypes.c_char_p
         L.lobra_status_string.argtypes = [ctypes.c_int]
         L.lobra_version.restype = ctypes.c_int
@@ -199,7 +228,7 @@ def _ptr(t):
 class _TorchTypes(dict):
     def __missing__(self, kind):
         import torch
-        self.update(fp32=torch.float32, bf16=torch.bfloat16, int32=torch.int32)
+        self.update(fp32=torch.float32, bf16=torch.bfloat16, int32=torch.int32, int8=torch.int8)
         return dict.__getitem__(self, kind)
 
 
@@ -208,7 +237,7 @@ _KINDS = {F32: "fp32", BF16: "bf16"}
 
 
 def _typed(t, kind, least=0):
-    """_ptr of a tensor that the library takes for `kind` ("fp32", "bf16", "int32"), of at least so many elements."""
+    """_ptr of a tensor that the library takes for `kind` ("fp32", "bf16", "int32", "int8"), of at least so many elements."""
     if t is None or isinstance(t, int):
         return t
     assert t.dtype is _torch_types[kind], "a %s tensor where the library reads or writes %s" % (t.dtype, kind)
@@ -438,14 +467,14 @@ def make_logprob_desc(dtype, T, V, ld=0, top_k=0) -> LogprobDesc:
     return LogprobDesc(int({"f32": F32, "bf16": BF16}.get(dtype, dtype)), int(V), int(T), int(ld), int(top_k))
 
 
-def _rows_ptr(t, desc: LogprobDesc):
+def _rows_ptr(t, desc, rows=None):
     """A [T, V] tensor of the descriptor's type whose rows are ld elements apart (a slice of wider rows, for one)."""
     if t is None or isinstance(t, int):
         return t
     T, V = t.shape
     ld, one = t.stride()
     assert desc.dtype not in _KINDS or t.dtype is _torch_types[_KINDS[desc.dtype]], "logits of another type than the descriptor's"
-    assert T == desc.T and V == desc.V, "logits of another shape than the descriptor's"
+    assert T == (desc.T if rows is None else rows) and V == desc.V, "logits of another shape than the descriptor's"
     assert T <= 1 or ld == (desc.ld or V), "rows of logits are not ld elements apart"
     assert V <= 1 or one == 1, "rows of logits must be contiguous"
     return t.data_ptr()
@@ -534,6 +563,133 @@ def lobra_grad_clip(gset: GradSet, max_norm, grad_scale, step, norm, clip_scale,
                                _typed(clip_scale, "fp32", n), _typed(step_out, "int32", n), int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_grad_clip")
+    return st
+
+
+# ---- an 8-bit base ---------------------------------------------------------------------------------------------------------
+def lobra_quant_pitch(d_in) -> int:
+    """Bytes of a row of Wq [d_out, lobra_quant_pitch(d_in)]."""
+    return lib().lobra_quant_pitch(int(d_in))
+
+
+def lobra_quantise_weight(W, Wq, w_scale, stream=None, check=True):
+    """Wq (int8 [d_out, lobra_quant_pitch(d_in)]) and w_scale (fp32 [d_out]) of W [d_in, d_out], bf16 or fp32, whose rows may lie in wider ones.
+    Returns the status."""
+    d_in, d_out = W.shape
+    kind = {str(_torch_types["fp32"]): F32, str(_torch_types["bf16"]): BF16}.get(str(W.dtype))
+    assert kind is not None, "a weight of another type than fp32 and bf16"
+    assert d_out <= 1 or W.stride(1) == 1, "rows of a weight must be contiguous"
+    assert Wq.shape == (d_out, lobra_quant_pitch(d_in)), "Wq of another shape than [d_out, lobra_quant_pitch(d_in)]"
+    st = lib().lobra_quantise_weight(kind, d_in, d_out, W.stride(0) if d_in > 1 else 0, W.data_ptr(), _typed(Wq, "int8"),
+                                        _typed(w_scale, "fp32", d_out), _stream(stream))
+    if check:
+        _check(st, "lobra_quantise_weight")
+    return st
+
+
+def lobra_mlora_quant_workspace_bytes(plan: Plan):
+    """(fwd bytes, bwd bytes) of workspace."""
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib().lobra_mlora_quant_workspace_bytes(plan.handle, ctypes.byref(a), ctypes.byref(b)), "lobra_mlora_quant_workspace_bytes")
+    return a.value, b.value
+
+
+def _quant_weight(plan: Plan, Wq, w_scale):
+    return _typed(Wq, "int8", plan.d_out * lobra_quant_pitch(plan.d_in)), _typed(w_scale, "fp32", plan.d_out)
+
+
+def lobra_mlora_quant_fwd(plan: Plan, x, Wq, w_scale, A, B, s, y, h_save=None, ws=None, stream=None, check=True):
+    """y = x W + s_t (A_t x) B_t with W and x in 8-bit integers in the first product.  Returns the status."""
+    e, T = plan.kind, plan.T
+    st = lib().lobra_mlora_quant_fwd(plan.handle, _typed(x, e, T * plan.d_in), *_quant_weight(plan, Wq, w_scale), _typed(A, e), _typed(B, e), _typed(s, "fp32"),
+                                  _typed(y, e, T * plan.d_out), _ptr(h_save), _ptr(ws), _nbytes(ws), _stream(stream))
+    if check:
+        _check(st, "lobra_mlora_quant_fwd")
+    return st
+
+
+def lobra_mlora_quant_bwd(plan: Plan, x, Wq, w_scale, A, B, s, dy, h_saved, dx, dA, dB, flags=0, ws=None, stream=None, check=True):
+    """dx, dA, dB of the layer on an 8-bit base.  Returns the status."""
+    e, T = plan.kind, plan.T
+    st = lib().lobra_mlora_quant_bwd(plan.handle, _typed(x, e, T * plan.d_in), *_quant_weight(plan, Wq, w_scale), _typed(A, e), _typed(B, e), _typed(s, "fp32"),
+                                  _typed(dy, e, T * plan.d_out), _ptr(h_saved), _typed(dx, e, T * plan.d_in), _typed(dA, "fp32"), _typed(dB, "fp32"),
+                                  int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
+    if check:
+        _check(st, "lobra_mlora_quant_bwd")
+    return st
+
+
+# ---- rows of logits: a teacher's likeliest tokens, and beams ---------------------------------------------------------------
+def make_distill_desc(dtype, T, V, top_k, tail=False, temperature=1.0, ld=0) -> DistillDesc:
+    """`dtype` is "f32"/"bf16" or the enum value; ld = row pitch of the logits in elements (0: V)."""
+    return DistillDesc(int({"f32": F32, "bf16": BF16}.get(dtype, dtype)), int(V), int(T), int(ld), int(top_k), int(tail), float(temperature))
+
+
+def _teacher(desc: DistillDesc, teacher_logp, teacher_id):
+    n = desc.T * desc.top_k
+    return _typed(teacher_logp, "fp32", n), _typed(teacher_id, "int32", n)
+
+
+def lobra_token_distill_fwd(desc: DistillDesc, logits, teacher_logp, teacher_id, loss, stat=None, stream=None, check=True):
+    """loss [T] of every row against the teacher's tokens [T, top_k]; stat (fp32 [T, 4]) for backward.  Returns the status."""
+    T = desc.T
+    st = lib().lobra_token_distill_fwd(ctypes.byref(desc), _rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id), _typed(loss, "fp32", T),
+                                       _typed(stat, "fp32", 4 * T), _stream(stream))
+    if check:
+        _check(st, "lobra_token_distill_fwd")
+    return st
+
+
+def lobra_token_distill_bwd(desc: DistillDesc, logits, teacher_logp, teacher_id, stat, dloss, dlogits, flags=0, stream=None, check=True):
+    """dlogits (may be logits) from dloss [T].  Returns the status."""
+    T = desc.T
+    st = lib().lobra_token_distill_bwd(ctypes.byref(desc), _rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id),
+                                       _typed(stat, "fp32", 4 * T), _typed(dloss, "fp32", T), _rows_ptr(dlogits, desc), int(flags), _stream(stream))
+    if check:
+        _check(st, "lobra_token_distill_bwd")
+    return st
+
+
+def make_beam_desc(dtype, n_req, beams, V, n_out=None, ld=0) -> BeamDesc:
+    """`dtype` is "f32"/"bf16" or the enum value; n_out: continuations of a request (None: as many as beams)."""
+    return BeamDesc(int({"f32": F32, "bf16": BF16}.get(dtype, dtype)), int(V), int(ld), int(n_req), int(beams), int(beams if n_out is None else n_out))
+
+
+def lobra_beam_workspace_bytes(desc: BeamDesc) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().lobra_beam_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)), "lobra_beam_workspace_bytes")
+    return n.value
+
+
+def lobra_beam_select(desc: BeamDesc, logits, score, done, done_token, out_score, out_beam, out_token, ws, stream=None, check=True):
+    """The n_out best continuations of every request: scores, beams within the request, tokens.  Returns the status."""
+    rows, n = desc.n_req * desc.beams, desc.n_req * desc.n_out
+    st = lib().lobra_beam_select(ctypes.byref(desc), _rows_ptr(logits, desc, rows), _typed(score, "fp32", rows), _typed(done, "int32", rows),
+                                 int(done_token), _typed(out_score, "fp32", n), _typed(out_beam, "int32", n), _typed(out_token, "int32", n), _ptr(ws),
+                                 _nbytes(ws), _stream(stream))
+    if check:
+        _check(st, "lobra_beam_select")
+    return st
+
+
+def lobra_beam_reorder(states, n_req, beams, parent, used=None, stream=None, check=True):
+    """states: [(src, dst)] of tensors [n_req * beams, ...] of any type, dst may be src; with `used` (int32 [n_req]) only the first used positions
+    (dimension 1) of a request's rows move.  parent: int32 [n_req, >= beams], whose rows may lie in wider ones.  Returns the status."""
+    arr = (BeamState * max(len(states), 1))()
+    for a, (src, dst) in zip(arr, states):
+        assert src.dtype is dst.dtype and src.shape == dst.shape, "a state that goes to a tensor of another type or shape"
+        assert src.shape[0] == n_req * beams, "a state of another number of rows than beams"
+        assert used is None or src.dim() >= 2, "a state without positions"
+        rows, n = max(src.shape[0], 1), src.numel() * src.element_size()
+        a.src, a.dst, a.row_bytes = _ptr(src), _ptr(dst), n // rows
+        a.unit_bytes = 0 if used is None else n // (rows * max(src.shape[1], 1))
+    assert parent.dtype is _torch_types["int32"] and parent.dim() == 2 and parent.shape[0] == n_req and parent.shape[1] >= beams, \
+        "parents other than int32 [n_req, beams]"
+    assert parent.shape[1] <= 1 or parent.stride(1) == 1, "rows of parents must be contiguous"
+    st = lib().lobra_beam_reorder(arr, len(states), int(n_req), int(beams), parent.data_ptr(), parent.stride(0) if n_req > 1 else int(beams),
+                                  _typed(used, "int32", n_req), _stream(stream))
+    if check:
+        _check(st, "lobra_beam_reorder")
     return st
 
 
@@ -670,7 +826,7 @@ class DeviceProblem:
 # ---------------------------------------------------------------------------------------------
 # launch trace: per-kernel durations from HIP events recorded on the stream the kernels run on
 # ---------------------------------------------------------------------------------------------
-KERNEL_NAMES = {1: "shrink", 2: "gemm", 3: "grad_stage1", 4: "grad_stage2", 5: "token_task", 6: "adam", 7: "shrink_gemm", 8: "gated", 9: "block_norm"}
+KERNEL_NAMES = {1: "shrink", 2: "gemm", 3: "grad_stage1", 4: "grad_stage2", 5: "token_task", 6: "adam", 7: "shrink_gemm", 8: "gated", 9: "block_norm", 10: "quant"}
 
 
 class LaunchTrace:

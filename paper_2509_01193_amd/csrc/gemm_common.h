@@ -13,6 +13,7 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int BM = 256, BN = 256, BK = 64;
 
@@ -165,6 +166,46 @@ __device__ __forceinline__ void mfma2_dma16(bf16x8 a0, bf16x8 a1, bf16x8 b, uint
                  :
                  : "v"(a0), "v"(a1), "v"(b), "s"(la), "v"(voff), "s"(gu), "n"(R0), "n"(R0 + 3), "n"(R1), "n"(R1 + 3)
                  : LOBRA_MFMA_CLOB_MEM);
+}
+
+// The same in 8-bit integers, whole sums: a lane's 16 bytes are 16 k of a row where bf16's are 8, and a 16 x 16 block of the result has the
+// same layout.  An MFMA of this shape keeps its pipe as long as one of bf16 for twice as many products.
+template <int R> __device__ __forceinline__ void mfma_acc_i8(bf16x8 a, bf16x8 b)
+{
+    asm volatile("v_mfma_i32_16x16x64_i8 a[%2:%3], %0, %1, a[%2:%3]"
+                 :
+                 : "v"(a), "v"(b), "n"(R), "n"(R + 3)
+                 : LOBRA_MFMA_CLOB);
+}
+template <int R> __device__ __forceinline__ void mfma_first_i8(bf16x8 a, bf16x8 b)
+{
+    asm volatile("v_mfma_i32_16x16x64_i8 a[%2:%3], %0, %1, 0"
+                 :
+                 : "v"(a), "v"(b), "n"(R), "n"(R + 3)
+                 : LOBRA_MFMA_CLOB);
+}
+template <int R0, int R1>
+__device__ __forceinline__ void mfma2_dma16_i8(bf16x8 a0, bf16x8 a1, bf16x8 b, uint32_t lds_addr,
+                                               const unsigned char* gbase, uint32_t voff)
+{
+    const uint32_t la = __builtin_amdgcn_readfirstlane(lds_addr);
+    const uint64_t gp = reinterpret_cast<uint64_t>(gbase);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(gp));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(gp >> 32));
+    const uint64_t gu = (uint64_t(hi) << 32) | lo;
+    asm volatile("v_mfma_i32_16x16x64_i8 a[%6:%7], %0, %2, a[%6:%7]\n\t"
+                 "s_mov_b32 m0, %3\n\t"
+                 "v_mfma_i32_16x16x64_i8 a[%8:%9], %1, %2, a[%8:%9]\n\t"
+                 "global_load_lds_dwordx4 %4, %5"
+                 :
+                 : "v"(a0), "v"(a1), "v"(b), "s"(la), "v"(voff), "s"(gu), "n"(R0), "n"(R0 + 3), "n"(R1), "n"(R1 + 3)
+                 : LOBRA_MFMA_CLOB_MEM);
+}
+
+// One register of an accumulator, written (the MFMAs behind it have to stay the documented wait states away).
+template <int R> __device__ __forceinline__ void acc_write(float v)
+{
+    asm volatile("v_accvgpr_write_b32 a[%1], %0" : : "v"(v), "n"(R) : LOBRA_MFMA_CLOB);
 }
 
 // One register of an accumulator, for the epilogue.  (Volatile: it stays behind the MFMAs before it.)

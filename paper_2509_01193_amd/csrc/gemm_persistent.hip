@@ -53,9 +53,13 @@
                              // accumulators; 0 / 2: timing variants (hardly any stores / plain stores)
 #endif
 
-// This file is compiled three times: as it is for K that is a multiple of 128, by gemm_persistent_ktail.hip for any other K,
+// This file is compiled four times: as it is for K that is a multiple of 128, by gemm_persistent_ktail.hip for any other K,
 // as kernels of another name (a flag of one template would do, but the two together cost the first one its last free
-// registers), and by gemm_persistent_gated.hip for the forward product of a gated feed-forward block.
+// registers), by gemm_persistent_gated.hip for the forward product of a gated feed-forward block, and by gemm_persistent_q8.hip
+// for a base in 8-bit integers.
+// Q8: Z and W are 8-bit integers, both with K fastest.  A unit of K is two of them, so that every address, copy and swizzle is
+// what it is in bf16, and an MFMA multiplies 64 k of whole numbers; in front of the up projection the sums become fp32 times the
+// scale of their token and of their channel.
 // GATED: W's columns are gate (N of them) and up (N), and a column tile is 128 of the one and the matching 128 of the other: of a
 // wave's 128 columns the first 64 are gate's, the other 64 the same columns of up, so that a lane holds g and u of an output in the same
 // place of two accumulators and stores h = a(g) u, from fp32 (and [g | u] where backward is to come: SAVE).  An up projection's step has 16
@@ -73,6 +77,14 @@
 #endif
 #if LOBRA_GP_GATED
 #include "activation.h"
+#endif
+#ifndef LOBRA_GP_Q8
+#define LOBRA_GP_Q8 0
+#endif
+#if LOBRA_GP_Q8
+#define LOBRA_GP_MFMA(name) name##_i8
+#else
+#define LOBRA_GP_MFMA(name) name
 #endif
 
 namespace lobra {
@@ -128,6 +140,8 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
                      const int32_t* __restrict__ cseg_task, const int32_t* __restrict__ rank_off
 #if LOBRA_GP_GATED
                      , uint16_t* __restrict__ gated_h
+#elif LOBRA_GP_Q8
+                     , const float* __restrict__ z_scale, const float* __restrict__ w_scale
 #endif
 )
 {
@@ -332,22 +346,22 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
         static_for<0, NU>([&](auto u_c) {
             constexpr int u = decltype(u_c)::value, mb = u / 2, nb0 = (NB / 2) * (u % 2);
             if constexpr (copies && u >= 2) {
-                mfma2_dma16<acc_reg(mb, nb0), acc_reg(mb, nb0 + 1)>(wc[nb0], wc[nb0 + 1], zf[mb], copy_lds_addr(cst, u - 2),
+                LOBRA_GP_MFMA(mfma2_dma16)<acc_reg(mb, nb0), acc_reg(mb, nb0 + 1)>(wc[nb0], wc[nb0 + 1], zf[mb], copy_lds_addr(cst, u - 2),
                                                                    copy_src(u - 2), copy_off(u - 2));
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (u < 4) {
-                    mfma2_dma16<acc_reg(mb, nb0 + 2), acc_reg(mb, nb0 + 3)>(wc[nb0 + 2], wc[nb0 + 3], zf[mb],
+                    LOBRA_GP_MFMA(mfma2_dma16)<acc_reg(mb, nb0 + 2), acc_reg(mb, nb0 + 3)>(wc[nb0 + 2], wc[nb0 + 3], zf[mb],
                                                                            copy_lds_addr(cst, 12 + u), copy_src(12 + u), copy_off(12 + u));
                 } else {
-                    mfma_acc<acc_reg(mb, nb0 + 2)>(wc[nb0 + 2], zf[mb]);
+                    LOBRA_GP_MFMA(mfma_acc)<acc_reg(mb, nb0 + 2)>(wc[nb0 + 2], zf[mb]);
                     __builtin_amdgcn_sched_barrier(0);
-                    mfma_acc<acc_reg(mb, nb0 + 3)>(wc[nb0 + 3], zf[mb]);
+                    LOBRA_GP_MFMA(mfma_acc)<acc_reg(mb, nb0 + 3)>(wc[nb0 + 3], zf[mb]);
                 }
             } else {
                 static_for<0, 4>([&](auto q_c) {
                     constexpr int q = decltype(q_c)::value;
-                    if constexpr (mode == STEP_FIRST) mfma_first<acc_reg(mb, nb0 + q)>(wc[nb0 + q], zf[mb]);
-                    else mfma_acc<acc_reg(mb, nb0 + q)>(wc[nb0 + q], zf[mb]);
+                    if constexpr (mode == STEP_FIRST) LOBRA_GP_MFMA(mfma_first)<acc_reg(mb, nb0 + q)>(wc[nb0 + q], zf[mb]);
+                    else LOBRA_GP_MFMA(mfma_acc)<acc_reg(mb, nb0 + q)>(wc[nb0 + q], zf[mb]);
                     if constexpr (u == 1 && q == 0) hook();
                     if constexpr (q < 3) __builtin_amdgcn_sched_barrier(0);
                 });
@@ -514,6 +528,29 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
         const int32_t row_end = min(row0 + BM, T);
         const int32_t wrow0 = row0 + wm * TM;        // the wave's rows are wrow0 .. wrow0 + TM - 1
+#if LOBRA_GP_Q8
+        // whole sums -> fp32 (rounded once: they have up to 31 bits) times the scales
+        {
+            f32x4 ws[NB];
+            float zs[MB];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                ws[nb] = *reinterpret_cast<const f32x4*>(w_scale + col0 + wn * TN + block_col(nb, 4 * kg));
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) zs[mb] = z_scale[wrow0 + 16 * mb + j];
+            static_for<0, MB>([&](auto mb_c) {
+                constexpr int mb = decltype(mb_c)::value;
+                static_for<0, NB>([&](auto nb_c) {
+                    constexpr int nb = decltype(nb_c)::value;
+                    static_for<0, 4>([&](auto v_c) {
+                        constexpr int v = decltype(v_c)::value, reg = acc_reg(mb, nb) + v;
+                        acc_write<reg>(float(__float_as_int(acc_read<reg>())) * zs[mb] * ws[nb][v]);
+                    });
+                });
+            });
+        }
+        if (P) asm volatile("s_nop 15" ::: "memory");          // (the up projection's MFMAs read what was written)
+#endif
         // ---- the up projection's steps (uniform over the workgroup, the barriers too)
         Walk walk;
         bool up = P && rec[3] > 0;
@@ -807,7 +844,8 @@ template <bool W_KN>
 #endif
 hipError_t launch_persistent(const PlanDev& pd, const void* Z, const void* W, const void* P, const void* M, void* C,
                              int32_t K, int32_t N, int32_t ldw, int32_t ldc, int32_t nproj, int32_t proj,
-                             int32_t tiles_m, int32_t tiles_n, int32_t gm, hipStream_t st, [[maybe_unused]] void* gated_h = nullptr)
+                             int32_t tiles_m, int32_t tiles_n, int32_t gm, hipStream_t st, [[maybe_unused]] void* gated_h = nullptr,
+                             [[maybe_unused]] const float* z_scale = nullptr, [[maybe_unused]] const float* w_scale = nullptr)
 {
     // once per device: the kernel needs more dynamic LDS than the default limit; one workgroup per compute unit
     static std::atomic<int32_t> cus[64];
@@ -837,6 +875,8 @@ hipError_t launch_persistent(const PlanDev& pd, const void* Z, const void* W, co
         K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, gm, cpx, tpw, pd.gemm_tile_seg, pd.cseg_off, pd.cseg_task, pd.rank_off
 #if LOBRA_GP_GATED
         , (uint16_t*)gated_h
+#elif LOBRA_GP_Q8
+        , z_scale, w_scale
 #endif
     );
     return hipGetLastError();
@@ -852,6 +892,14 @@ hipError_t LOBRA_GP_HOST(const PlanDev& pd, int act, const void* x, const void* 
     if (act == LOBRA_ACT_SILU) return gu ? LOBRA_GATED(LOBRA_ACT_SILU, true) : LOBRA_GATED(LOBRA_ACT_SILU, false);
     return gu ? LOBRA_GATED(LOBRA_ACT_GELU_TANH, true) : LOBRA_GATED(LOBRA_ACT_GELU_TANH, false);
 #undef LOBRA_GATED
+}
+#elif LOBRA_GP_Q8
+hipError_t LOBRA_GP_HOST(const PlanDev& pd, const void* Z, const float* z_scale, const void* W, const float* w_scale, const void* P, const void* M,
+                         void* C, int32_t K, int32_t N, int32_t ldc, int32_t nproj, int32_t proj, hipStream_t st)
+{
+    if (pd.T < BM || N < BN || K % (2 * BK) != 0) return hipErrorInvalidValue;          // (what choose_q8 asks for)
+    const int32_t tiles_m = (pd.T + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+    return launch_persistent<false>(pd, Z, W, P, M, C, K, N, K, ldc, nproj, proj, tiles_m, tiles_n, K > 4096 ? 4 : 6, st, nullptr, z_scale, w_scale);
 }
 #else
 hipError_t LOBRA_GP_HOST(const PlanDev& pd, bool transW, const void* Z, const void* W, const void* P,

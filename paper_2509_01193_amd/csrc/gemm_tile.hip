@@ -42,6 +42,14 @@ namespace lobra {
 
 using namespace gemm;
 
+// Compiled once more by gemm_tile_q8.hip, as kernels of other names, for a base in 8-bit integers: Z and W are those, both with K fastest, a unit
+// of K is two of them (copies, swizzles and addresses stay what they are), an MFMA multiplies 64 k of whole numbers, and behind the main loop the
+// sums become fp32 times the scale of their token and of their channel.
+#ifndef LOBRA_GT_Q8
+#define LOBRA_GT_Q8 0
+#define LOBRA_GT_KERNEL gemm_tile_kernel
+#endif
+
 static_assert(kGemmKTile == BK && kGemmTiles[0].tm == BM && kGemmTiles[0].tn == BN, "the plan's choice is about these kernels");
 
 namespace {
@@ -112,7 +120,8 @@ void tile_body(const PlanDev& pd, const uint16_t* __restrict__ Z, const uint16_t
                const uint16_t* __restrict__ P, const uint16_t* __restrict__ M,
                uint16_t* __restrict__ C, int32_t K, int32_t N, int32_t ldw, int32_t ldc,
                int32_t nproj, int32_t proj, int32_t tiles_m, int32_t tiles_n, int32_t GM, int32_t splits,
-               float* __restrict__ part, int32_t wg, unsigned char* lds)
+               float* __restrict__ part, int32_t wg, unsigned char* lds,
+               [[maybe_unused]] const float* __restrict__ z_scale = nullptr, [[maybe_unused]] const float* __restrict__ w_scale = nullptr)
 {
     // splits > 1: that many workgroups per tile share the K tiles, and one more has the adapter term (if P): in the time
     // that its chain of table reads, copies and products takes, the others are done with theirs.  Their fp32 sums go to
@@ -254,7 +263,12 @@ void tile_body(const PlanDev& pd, const uint16_t* __restrict__ Z, const uint16_t
         constexpr int NM = MB * NB, NR = READ ? MB + NB : 0;
         static_for<0, NM>([&](auto q_c) {
             constexpr int q = decltype(q_c)::value, mb = q / NB, nb = q % NB;
+#if LOBRA_GT_Q8
+            acc[mb][nb] = __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, wf[nb]), __builtin_bit_cast(i32x4, zf[mb]),
+                                                                                         __builtin_bit_cast(i32x4, acc[mb][nb]), 0, 0, 0));
+#else
             acc[mb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[nb], zf[mb], acc[mb][nb], 0, 0, 0);
+#endif
             static_for<q * NR / NM, (q + 1) * NR / NM>([&](auto i_c) {
                 constexpr int i = decltype(i_c)::value;
                 if constexpr (i < NB) wn_[i] = read_w(rst, rks, i);
@@ -467,6 +481,24 @@ void tile_body(const PlanDev& pd, const uint16_t* __restrict__ Z, const uint16_t
         slot = ns;
     }
 
+#if LOBRA_GT_Q8
+    {
+        f32x4 ws[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) ws[nb] = *reinterpret_cast<const f32x4*>(w_scale + min(col0 + wn * WTN + nb * 16 + 4 * kg, N - 4));
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            const float zs = z_scale[min(row0 + wm * WTM + mb * 16 + j, T - 1)];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const i32x4 sum = __builtin_bit_cast(i32x4, acc[mb][nb]);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[mb][nb][v] = float(sum[v]) * zs * ws[nb][v];
+            }
+        }
+    }
+#endif
+
     // ---- the up projection's steps
     if (P) {
         const int32_t nks = (pd.r_max / nproj + 31) >> 5;            // rank steps of the widest window (uniform)
@@ -575,16 +607,26 @@ void tile_body(const PlanDev& pd, const uint16_t* __restrict__ Z, const uint16_t
 
 template <bool W_KN, int TM, int TN, int WM, int WN, int STAGES, int OCC>
 __global__ __launch_bounds__(64 * WM * WN, OCC * WM * WN / 4)
-void gemm_tile_kernel(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t* __restrict__ W,
+void LOBRA_GT_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t* __restrict__ W,
                       const uint16_t* __restrict__ P, const uint16_t* __restrict__ M,
                       uint16_t* __restrict__ C, int32_t K, int32_t N, int32_t ldw, int32_t ldc,
                       int32_t nproj, int32_t proj, int32_t tiles_m, int32_t tiles_n, int32_t GM, int32_t splits,
-                      float* __restrict__ part)
+                      float* __restrict__ part
+#if LOBRA_GT_Q8
+                      , const float* __restrict__ z_scale, const float* __restrict__ w_scale
+#endif
+)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     tile_body<W_KN, TM, TN, WM, WN, STAGES, ahead_rows<TM, TN, WN, STAGES, OCC>()>(pd, Z, W, P, M, C, K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, GM, splits, part,
-                                            int32_t(blockIdx.x), lds);
+                                            int32_t(blockIdx.x), lds
+#if LOBRA_GT_Q8
+                                            , z_scale, w_scale
+#endif
+    );
 }
+
+#if !LOBRA_GT_Q8
 
 // A split product and the rank-r projection of the same Z in one launch: the first pwgs workgroups (a multiple of eight, so that the
 // others keep their XCDs) project, rparts * 2 columns of items as in shrink_ring_kernel<1, 1, 1, 256>, the others multiply.
@@ -675,7 +717,12 @@ __global__ __launch_bounds__(256) void gemm_add_up_kernel(PlanDev pd, const floa
     if (col < N) *reinterpret_cast<bf16x4*>(C + size_t(row) * N + col) = o;
 }
 
+#endif  // !LOBRA_GT_Q8
+
 // C = the sum of the splits' partial products, in split order, rounded once: 8 columns per thread.
+#if LOBRA_GT_Q8
+#define gemm_add_kernel gemm_add_q8_kernel
+#endif
 template <int S>
 __global__ __launch_bounds__(256) void gemm_add_kernel(const float* __restrict__ part, uint16_t* __restrict__ C, int64_t n, int32_t N,
                                                        int32_t ldc)
@@ -709,7 +756,8 @@ template <int S, int LAST, typename F> static void with_splits(int32_t n, F&& f)
 template <bool W_KN, int TM, int TN, int WM, int WN, int STAGES, int OCC>
 static hipError_t launch_tile(const PlanDev& pd, const void* Z, const void* W, const void* P,
                               const void* M, void* C, int32_t K, int32_t N, int32_t ldw, int32_t ldc,
-                              int32_t nproj, int32_t proj, hipStream_t st, int32_t splits, float* part)
+                              int32_t nproj, int32_t proj, hipStream_t st, int32_t splits, float* part,
+                              [[maybe_unused]] const float* z_scale = nullptr, [[maybe_unused]] const float* w_scale = nullptr)
 {
     constexpr int bytes = ring_bytes<TM, TN, WN, STAGES>() + int(sizeof(TileTable<TM>)) + ahead_rows<TM, TN, WN, STAGES, OCC>() * TN * 2;
     static_assert(bytes * OCC <= 160 * 1024 && ahead_rows<TM, TN, WN, STAGES, OCC>() >= 16, "LDS budget");
@@ -720,16 +768,20 @@ static hipError_t launch_tile(const PlanDev& pd, const void* Z, const void* W, c
     if (e != hipSuccess) return e;
     const uint64_t bit = uint64_t(1) << (dev & 63);
     if (!(raised.load(std::memory_order_acquire) & bit)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_tile_kernel<W_KN, TM, TN, WM, WN, STAGES, OCC>),
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&LOBRA_GT_KERNEL<W_KN, TM, TN, WM, WN, STAGES, OCC>),
                                 hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
         raised.fetch_or(bit, std::memory_order_release);
     }
     const int32_t tiles_m = (pd.T + TM - 1) / TM, tiles_n = (N + TN - 1) / TN;
     const int32_t per = splits + (splits > 1 && P ? 1 : 0);          // workgroups per tile
-    gemm_tile_kernel<W_KN, TM, TN, WM, WN, STAGES, OCC><<<dim3(uint32_t(tiles_m) * uint32_t(tiles_n) * uint32_t(per)), 64 * WM * WN, bytes, st>>>(
+    LOBRA_GT_KERNEL<W_KN, TM, TN, WM, WN, STAGES, OCC><<<dim3(uint32_t(tiles_m) * uint32_t(tiles_n) * uint32_t(per)), 64 * WM * WN, bytes, st>>>(
         pd, (const uint16_t*)Z, (const uint16_t*)W, (const uint16_t*)P, (const uint16_t*)M, (uint16_t*)C,
-        K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, 1024 / TM, splits, part);
+        K, N, ldw, ldc, nproj, proj, tiles_m, tiles_n, 1024 / TM, splits, part
+#if LOBRA_GT_Q8
+        , z_scale, w_scale
+#endif
+    );
     e = hipGetLastError();
     if (e != hipSuccess || splits == 1 || !C) return e;
     const int64_t n = int64_t(pd.T) * N;             // (N is a multiple of 8)
@@ -739,6 +791,24 @@ static hipError_t launch_tile(const PlanDev& pd, const void* Z, const void* W, c
     return hipGetLastError();
 }
 
+#if LOBRA_GT_Q8
+hipError_t gemm_tile_q8(const PlanDev& pd, const GemmChoice& choice, const void* Z, const float* z_scale, const void* W, const float* w_scale, const void* P,
+                        const void* M, void* C, int32_t K, int32_t N, int32_t ldc, int32_t nproj, int32_t proj, hipStream_t st, float* part)
+{
+    if (pd.T == 0) return hipSuccess;
+    if (choice.splits > 1 && !part) return hipErrorInvalidValue;
+#define LOBRA_TILE(...) \
+    launch_tile<false, __VA_ARGS__>(pd, Z, W, P, M, C, K, N, K, ldc, nproj, proj, st, choice.splits, part, z_scale, w_scale)
+    switch (choice.tile) {
+    case 1: return LOBRA_TILE(128, 256, 2, 4, 3, 1);
+    case 2: return LOBRA_TILE(128, 128, 2, 2, 4, 1);
+    case 3: return LOBRA_TILE(128, 64, 2, 2, 3, 2);
+    case 4: return LOBRA_TILE(64, 64, 2, 2, 4, 2);
+    default: return hipErrorInvalidValue;
+    }
+#undef LOBRA_TILE
+}
+#else
 template <bool W_KN, int TM, int TN, int WM, int WN, int STAGES>
 static hipError_t launch_beside(const PlanDev& pd, const void* Z, const void* W, const void* D, const float* s, void* P_tok, void* P_blk,
                                 const void* M, void* C, int32_t K, int32_t N, int32_t ldw, hipStream_t st, int32_t splits, float* part)
@@ -826,5 +896,6 @@ hipError_t gemm_mfma(const PlanDev& pd, bool transW, const void* Z, const void* 
     }
 #undef LOBRA_TILE
 }
+#endif
 
 }  // namespace lobra

@@ -93,6 +93,22 @@ hipError_t gemm_persistent_ktail(const PlanDev& pd, bool transW, const void* Z, 
 hipError_t gemm_staged(const PlanDev& pd, bool transW, const void* Z, const void* W, const void* P,
                        const void* M, void* C, int32_t K, int32_t N, int32_t ldw, int32_t ldc, int32_t nproj,
                        int32_t proj, int32_t tiles_m, int32_t tiles_n, int32_t gm, hipStream_t st);
+// ---- a base in 8-bit integers (q8.hip, gemm_persistent_q8.hip, gemm_tile_q8.hip) -----------------------------------------------
+// Rows of kQ8Pad bytes and whole multiples of them, zero beyond the width, so that no kernel meets a partial K tile.
+constexpr int32_t kQ8Pad = 256;
+constexpr int64_t q8_pitch(int64_t d) { return (d + kQ8Pad - 1) / kQ8Pad * kQ8Pad; }
+// q [T][q8_pitch(d)] and scale [T] of x [T][d]: scale = max |x| / 127, q = x / scale to the nearest, halves to the even one.  A row of zeros has
+// the scale 0, one with NaN or infinity the scale NaN and q = 0.
+hipError_t q8_rows(int64_t T, int32_t d, const void* x, void* q, float* scale, hipStream_t st);
+// The same of the columns of W [d_in][ldw], transposed: q [d_out][q8_pitch(d_in)], scale [d_out]; and W [d_in][d_out] in bf16 from them.
+hipError_t q8_weight(int dtype, int32_t d_in, int32_t d_out, int64_t ldw, const void* W, void* q, float* scale, hipStream_t st);
+hipError_t q8_dequantise(int32_t d_in, int32_t d_out, const void* q, const float* scale, void* W, hipStream_t st);
+// C = z_scale w_scale (Z W^T) + P M_t: Z [T][K], W [N][K] 8-bit integers, K counted in pairs of them (a multiple of 128); the other arguments are
+// those of gemm_mfma.  persistent: T, N >= 256; tile: what choose_q8 chose, part: its sums if it splits K.
+hipError_t gemm_persistent_q8(const PlanDev& pd, const void* Z, const float* z_scale, const void* W, const float* w_scale, const void* P, const void* M,
+                              void* C, int32_t K, int32_t N, int32_t ldc, int32_t nproj, int32_t proj, hipStream_t st);
+hipError_t gemm_tile_q8(const PlanDev& pd, const GemmChoice& choice, const void* Z, const float* z_scale, const void* W, const float* w_scale,
+                        const void* P, const void* M, void* C, int32_t K, int32_t N, int32_t ldc, int32_t nproj, int32_t proj, hipStream_t st, float* part);
 bool gemm_mfma_shape_ok(int64_t T, int32_t K, int32_t N, int32_t ldw);
 // P = s_t Z M_t^T in bf16, written token-major [T][r_pad] and block-transposed [ntb][r_pad][32].
 // (ldz: row pitch of Z; nproj > 1: projection `proj` of a fused call - rank window, see the kernel; proj < 0: all of
@@ -141,6 +157,31 @@ struct LogprobGrad {
 };
 hipError_t logprob_fwd(const LogprobShape& s, const void* logits, const int32_t* target, const LogprobOut& out, hipStream_t st);
 hipError_t logprob_bwd(const LogprobShape& s, const void* logits, const int32_t* target, const LogprobGrad& in, void* dlogits, hipStream_t st);
+
+// Loss against a teacher's likeliest tokens and its gradient (distill.hip): lobra_token_distill_fwd / _bwd with checked arguments (T > 0, ld >= V).
+struct DistillShape {
+    int32_t dtype, V, top_k;
+    bool tail;
+    int64_t T, ld;
+    float temperature;
+};
+hipError_t distill_fwd(const DistillShape& s, const void* logits, const float* teacher_logp, const int32_t* teacher_id, float* loss, float* stat,
+                       hipStream_t st);
+hipError_t distill_bwd(const DistillShape& s, const void* logits, const float* teacher_logp, const int32_t* teacher_id, const float* stat,
+                       const float* dloss, void* dlogits, bool accumulate, hipStream_t st);
+
+// Beam search (beam.hip): lobra_beam_select with checked arguments (n_req > 0, n_req beams beam_parts(V) < 2^24).  keys [n_req beams parts][n_out], sums
+// [n_req beams parts][2].  lobra_beam_reorder likewise.
+struct BeamShape {
+    int32_t dtype, V;
+    int64_t ld;
+    int32_t n_req, beams, n_out;
+};
+int32_t beam_parts(int32_t V);
+hipError_t beam_select(const BeamShape& s, const void* logits, const float* score, const int32_t* done, int32_t done_token, float* out_score,
+                       int32_t* out_beam, int32_t* out_token, uint64_t* keys, float* sums, hipStream_t st);
+hipError_t beam_reorder(const lobra_beam_state* states, int32_t n_states, int32_t n_req, int32_t beams, const int32_t* parent, int64_t parent_ld,
+                        const int32_t* used, hipStream_t st);
 
 // Gradient norms and clipping (grad_clip.hip) over a set's pieces, which are grouped by task: those of task t are
 // task_piece[t] .. task_piece[t + 1] - 1.  partial [pieces] fp64.  once: they are more than the caches hold.

@@ -15,6 +15,7 @@
 // alternatives 186; 40 x 32000 with 20 of them 9; one row of 32000 5, of 256000 20, with 32 alternatives 8 and 27.
 #include "kernels.h"
 #include "row_common.h"
+#include "row_logits.h"
 
 namespace lobra {
 
@@ -22,93 +23,7 @@ using namespace rows;
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kFar = -1e30f;            // below every difference that matters: exp is 0, and 0 times it is 0
 constexpr int kCandidates = 1024;         // logits that may be among the largest: 8 KiB of LDS
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// m, S and U of some elements (U in units of log2: sum of 2^x x with x = (z - m) log2 e)
-struct Stat {
-    float m, s, u;
-};
-
-template <bool ENT> __device__ __forceinline__ void rescale(Stat& a, float m)
-{
-    const float x = fmaxf((a.m - (m == -INFINITY ? 0.f : m)) * kLog2e, kFar);        // (a.m = -inf: s and u are 0)
-    const float f = exp2_fast(x);
-    if (ENT) a.u = f * (a.u + a.s * x);
-    a.s *= f;
-    a.m = m;
-}
-
-// (the more elements at a time, the less often m grows: nearly every time some lane's does)
-template <bool ENT, int N> __device__ __forceinline__ void take(Stat& a, const float (&z)[N])
-{
-    float c = z[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) c = fmaxf(c, z[i]);
-    if (c > a.m) rescale<ENT>(a, c);
-    const float ref = a.m == -INFINITY ? 0.f : a.m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float x = (z[i] - ref) * kLog2e;       // (NaN where z is NaN or m = +inf: s stays NaN from here on)
-        const float e = exp2_fast(x);
-        a.s += e;
-        if (ENT) a.u = fmaf(e, fmaxf(x, kFar), a.u);
-    }
-}
-
-template <typename E> __device__ __forceinline__ float element(const E* p, int32_t i) { return Elem<E>::load(p, size_t(i)); }
-
-// A packet of -inf, which adds nothing.
-template <typename E> __device__ __forceinline__ u32x4 nothing()
-{
-    const uint32_t w = sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;
-    return u32x4{w, w, w, w};
-}
-
-// The statistics of the elements that this thread looks at: batches of U packets, the next one on its way while one is worked on, the
-// last one filled up with -inf.  (One by one, what is left behind the whole batches - up to a quarter of a row - would wait for memory U
-// times more.)
-template <typename E, int NT, bool ENT> __device__ __forceinline__ Stat row_stat(const E* row, const RowShape& sh)
-{
-    constexpr int N = Packet<E>::N, U = 4;
-    Stat a{-INFINITY, 0.f, 0.f};
-    const u32x4* p = reinterpret_cast<const u32x4*>(row + sh.head);
-    const int32_t t = threadIdx.x;
-    auto fetch = [&](u32x4 (&q)[U], int32_t first) {
-        if (first + U * NT <= sh.packets) {           // (uniform)
-#pragma unroll
-            for (int c = 0; c < U; ++c) q[c] = p[first + c * NT + t];
-        } else {
-#pragma unroll
-            for (int c = 0; c < U; ++c) q[c] = first + c * NT + t < sh.packets ? p[first + c * NT + t] : nothing<E>();
-        }
-    };
-    u32x4 q[U], next[U];
-    if (sh.packets > 0) fetch(q, 0);
-    // the elements in front of the first packet and behind the last one: fewer than 2 N, a thread each
-    const bool has_edge = t < sh.head + sh.tail;
-    E edge = E(0);
-    if (has_edge) edge = row[t < sh.head ? t : t + sh.packets * N];
-    for (int32_t first = 0; first < sh.packets; first += U * NT) {
-        if (first + U * NT < sh.packets) fetch(next, first + U * NT);
-        float z[U * N];
-#pragma unroll
-        for (int c = 0; c < U; ++c)
-#pragma unroll
-            for (int e = 0; e < N; ++e) z[c * N + e] = Packet<E>::element(q[c], e);
-        take<ENT>(a, z);
-#pragma unroll
-        for (int c = 0; c < U; ++c) q[c] = next[c];
-    }
-    if (has_edge) {
-        const float z[1] = {Elem<E>::load(&edge, 0)};
-        take<ENT>(a, z);
-    }
-    return a;
-}
 
 // f(first index, values) over the elements of the row that this thread looks at, in ascending order of index within the whole packets
 template <typename E, int NT, typename F> __device__ __forceinline__ void each(const E* row, const RowShape& sh, F&& f)
@@ -140,19 +55,6 @@ template <typename E, int NT, typename F> __device__ __forceinline__ void each(c
         f(at, z);
     }
 }
-
-// A logit and its index as one number that orders by value, the lowest index first among equals.
-__device__ __forceinline__ uint64_t order_key(float z, int32_t index)
-{
-    const uint32_t b = __float_as_uint(z + 0.f);       // (-0 is 0)
-    return (uint64_t(b & 0x80000000u ? ~b : b | 0x80000000u) << 32) | uint32_t(~index);
-}
-__device__ __forceinline__ float key_value(uint64_t key)
-{
-    const uint32_t b = uint32_t(key >> 32);
-    return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
-}
-__device__ __forceinline__ int32_t key_index(uint64_t key) { return int32_t(~uint32_t(key)); }
 
 // The top_k largest of a row, all of whose threads know m and ln S.
 // 64 groups of threads have a maximum each; the top_k-th largest of these, tau, has at least top_k logits at or above it, and what is

@@ -475,6 +475,29 @@ GemmChoice choose_gemm(int64_t T, int32_t K, int32_t N, int32_t group, int32_t n
     return best;
 }
 
+GemmChoice choose_q8(int64_t T, int32_t K, int32_t N, int32_t group, int32_t nseg, size_t part_bytes)
+{
+    const int32_t kt = K / kGemmKTile;
+    const float segments = std::max(0.f, float(nseg) * kGemmTileRows / float(T) - 1.f);
+    GemmChoice best;
+    float least = -1.f;
+    for (int32_t i = 0; i < int32_t(sizeof(kQ8Tiles) / sizeof(kQ8Tiles[0])); ++i) {
+        const GemmTile& t = kQ8Tiles[i];
+        if (i == kPersistentTile && !(T >= t.tm && N >= t.tn)) continue;
+        if (group > 0 && group % t.tn != 0) continue;
+        const float fixed = t.fixed + (i == kPersistentTile ? kSegmentCost.persistent * segments : 0.f);
+        const int64_t tiles = (T + t.tm - 1) / t.tm * ((N + t.tn - 1) / t.tn), slots = cus * t.per_cu;
+        for (int32_t s = 1; s <= kMaxSplits; ++s) {
+            const int64_t bytes = int64_t(s + 1) * T * N * 4;      // (one more for the adapter term)
+            if (s > 1 && (i == kPersistentTile || kt < 4 * s || tiles * s > slots || uint64_t(bytes) > part_bytes)) break;
+            float cost = rounds_cost(t, tiles * s, (kt + s - 1) / s, fixed) + t.once;
+            if (s > 1) cost += 3.f + float(bytes) / 3e6f;
+            if (least < 0.f || cost < least) best = GemmChoice{i, s, cost}, least = cost;
+        }
+    }
+    return best;
+}
+
 bool choose_gated_persistent(int64_t T, int32_t K, int32_t f, int32_t group, int32_t nseg, int32_t rank)
 {
     const GemmTile& t = kGemmTiles[kPersistentTile];

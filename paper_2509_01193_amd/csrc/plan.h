@@ -122,6 +122,15 @@ struct GemmChoice { int32_t tile = -1, splits = 1; float cost = -1.f; };    // t
 // The choice for C [T, N] = Z [T, K] op(W) given part_bytes of scratch.  group > 0: no tile may straddle a multiple of
 // `group` columns (a multiple of 64).  nseg: segments of the batch (0: no adapter); rank: the widest rank window.
 GemmChoice choose_gemm(int64_t T, int32_t K, int32_t N, int32_t group, int32_t nseg, int32_t rank, size_t part_bytes);
+// The same for a base in 8-bit integers, K in units of two of them (a multiple of 128): what a K tile costs there (gemm_persistent_q8.hip, gemm_tile_q8.hip).
+constexpr GemmTile kQ8Tiles[] = {
+    {256, 256, 1, 1.35f, 0.f, 5.f, 7.f},
+    {128, 256, 1, 0.86f, 0.f, 6.5f, 0.f},
+    {128, 128, 1, 0.48f, 0.f, 7.f, 0.f},
+    {128, 64, 2, 0.36f, 0.59f, 7.f, 0.f},
+    {64, 64, 2, 0.23f, 0.39f, 6.f, 0.f},
+};
+GemmChoice choose_q8(int64_t T, int32_t K, int32_t N, int32_t group, int32_t nseg, size_t part_bytes);
 // The same where the projection runs in the product's launch and the adapter term comes with the sum of the splits, of which there may
 // be one (gemm_mfma_beside; ntb: token blocks; halves: 2 if one has more than 16 tokens, else 1): tile -1 where a projection of its own is better.  Given kMaxPartBytes of scratch.
 // Forward passes, a projection of its own / beside the product, us (K x N, rank, n one-token requests or tokens of segments of m):

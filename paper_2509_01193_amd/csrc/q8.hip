@@ -1,0 +1,196 @@
+// A frozen base in 8-bit integers: tokens and channels as whole numbers with a scale each, and the way back.
+//     scale = max |v| / 127     q = v / scale, rounded to the nearest whole number, halves to the even one
+// of a token's row of x or a channel's column of W.  The quotient is the exact one: a product with 1 / scale can land on the other side of a half,
+// so where it comes near one (1e-4 either side; its own error is below 2e-5) the remainder v - q scale, which fp32 holds exactly there,
+// decides.
+#include "kernels.h"
+#include "row_common.h"
+
+namespace lobra {
+
+using namespace rows;
+
+namespace {
+
+// (Magnitudes whose scale is no normal number count as zeros: the scale is 0, and every q.)
+struct Quantiser {
+    float scale, inv;
+};
+__device__ __forceinline__ Quantiser quantiser(float amax)       // amax: finite, >= 0
+{
+    Quantiser z;
+    z.scale = amax >= 127.f * 0x1p-126f ? amax / 127.f : 0.f;
+    z.inv = z.scale > 0.f ? 1.f / z.scale : 0.f;
+    return z;
+}
+
+// q of N values at a time, as floats
+template <int N> __device__ __forceinline__ void quantise(const Quantiser& z, const float (&v)[N], float (&q)[N])
+{
+    float far = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float t = v[i] * z.inv;
+        q[i] = rintf(t);
+        far = fmaxf(far, fabsf(t - q[i]));
+    }
+    if (far > 0.4999f) {                             // (a packet in some hundreds)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float r = fmaf(-q[i], z.scale, v[i]), over = fabsf(r) - 0.5f * z.scale;
+            if (over > 0.f || (over == 0.f && (int32_t(q[i]) & 1))) q[i] += copysignf(1.f, r);
+        }
+    }
+}
+
+template <int N> __device__ __forceinline__ void to_bytes(const float (&q)[N], uint32_t (&b)[N / 4])
+{
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        b[i] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[i] |= (uint32_t(int32_t(q[4 * i + e])) & 255u) << (8 * e);
+    }
+}
+
+constexpr int kHeld = 16;                            // packets a lane keeps of its row: 8192 elements
+
+// The largest magnitude of eight bf16, as bits (NaN and infinity: 0x7f80 and above), joined with m.
+__device__ __forceinline__ uint32_t amax_bits(u32x4 p, uint32_t m)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max(m, max(p[i] & 0x7fffu, p[i] >> 16 & 0x7fffu));
+    return m;
+}
+
+__device__ __forceinline__ void store_packet(const Quantiser& z, u32x4 p, bool finite, uint8_t* out)
+{
+    float v[8], q[8];
+    uint32_t b[2] = {0u, 0u};
+    if (finite) {
+        Packet<uint16_t>::widen(p, v);
+        quantise<8>(z, v, q);
+        to_bytes<8>(q, b);
+    }
+    *reinterpret_cast<uint64_t*>(out) = uint64_t(b[1]) << 32 | b[0];
+}
+
+// A wave per row, whose packets stay in registers between the maximum and the quotients (rows beyond 8192 elements: what does not fit is
+// read again).  Bound: memory.
+__global__ __launch_bounds__(256) void q8_rows_kernel(int32_t T, int32_t d, int32_t pitch, const uint16_t* __restrict__ x, uint8_t* __restrict__ q,
+                                                      float* __restrict__ scale)
+{
+    const int32_t row = int32_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(int32_t(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    if (row >= T) return;
+    const u32x4* p = reinterpret_cast<const u32x4*>(x + size_t(row) * d);
+    uint8_t* out = q + size_t(row) * pitch;
+    const int32_t packets = d / 8, all = pitch / 8;
+    const u32x4 none = {0u, 0u, 0u, 0u};
+    u32x4 held[kHeld];
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c) held[c] = lane + 64 * c < packets ? p[lane + 64 * c] : none;
+    uint32_t m = 0;
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c) m = amax_bits(held[c], m);
+    for (int32_t i = lane + 64 * kHeld; i < packets; i += 64) m = amax_bits(p[i], m);
+    const float amax = wave_max(__uint_as_float(m << 16 > 0x7f800000u ? 0x7f800000u : m << 16));       // (NaN counts as infinity: a maximum would drop it)
+    const bool finite = amax < INFINITY;
+    const Quantiser z = quantiser(finite ? amax : 0.f);
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c)
+        if (lane + 64 * c < all) store_packet(z, held[c], finite, out + 8 * (lane + 64 * c));
+    for (int32_t i = lane + 64 * kHeld; i < all; i += 64) store_packet(z, i < packets ? p[i] : none, finite, out + 8 * i);
+    if (lane == 0) scale[row] = finite ? z.scale : NAN;
+}
+
+// 64 columns per workgroup, a lane each; every wave has a quarter of each 64 rows, so that a lane's 16 values are 16 neighbouring bytes of its
+// column's row of q.  Done once per weight.
+template <typename E>
+__global__ __launch_bounds__(256) void q8_weight_kernel(int32_t d_in, int32_t d_out, int32_t pitch, int64_t ldw, const E* __restrict__ W,
+                                                        uint8_t* __restrict__ q, float* __restrict__ scale)
+{
+    __shared__ float part[4][64];
+    const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t col = int64_t(blockIdx.x) * 64 + lane;
+    const bool in = col < d_out;
+    float m = 0.f;
+    if (in)
+        for (int32_t k = wave; k < d_in; k += 4) {
+            const float v = fabsf(Elem<E>::load(W, size_t(k) * ldw + col));
+            m = v < INFINITY ? fmaxf(m, v) : INFINITY;
+        }
+    part[wave][lane] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, part[w][lane]);
+    if (!in) return;
+    const bool finite = m < INFINITY;
+    const Quantiser z = quantiser(finite ? m : 0.f);
+    for (int32_t k0 = 16 * wave; k0 < pitch; k0 += 64) {
+        float v[16], r[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = finite && k0 + i < d_in ? Elem<E>::load(W, size_t(k0 + i) * ldw + col) : 0.f;
+        quantise<16>(z, v, r);
+        uint32_t b[4];
+        to_bytes<16>(r, b);
+        *reinterpret_cast<u32x4*>(q + size_t(col) * pitch + k0) = u32x4{b[0], b[1], b[2], b[3]};
+    }
+    if (wave == 0) scale[col] = finite ? z.scale : NAN;
+}
+
+// W [d_in][d_out] = q scale, rounded once to bf16 (backward multiplies in bf16).  A block of 64 x 64 through LDS: 64 bytes of each row of q are
+// read, whole 128-byte lines of W written.
+__global__ __launch_bounds__(256) void q8_dequantise_kernel(int32_t d_in, int32_t d_out, int32_t pitch, const uint8_t* __restrict__ q,
+                                                            const float* __restrict__ scale, uint16_t* __restrict__ W)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t tile[64][80];
+    const int32_t t = threadIdx.x, n0 = int32_t(blockIdx.x) * 64, k0 = int32_t(blockIdx.y) * 64;
+    {
+        const int32_t n = t >> 2, c = 16 * (t & 3);
+        if (n0 + n < d_out) *reinterpret_cast<u32x4*>(&tile[n][c]) = *reinterpret_cast<const u32x4*>(q + size_t(n0 + n) * pitch + k0 + c);
+    }
+    __syncthreads();
+    const int32_t n = 8 * (t & 7);
+    if (n0 + n >= d_out) return;                     // (d_out is a multiple of 8)
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = scale[n0 + n + e];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int32_t k = (t >> 3) + 32 * h;
+        if (k0 + k >= d_in) continue;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = float(int32_t(int8_t(tile[n + e][k]))) * s[e];
+        *reinterpret_cast<u32x4*>(W + size_t(k0 + k) * d_out + n0 + n) = Packet<uint16_t>::narrow(v);
+    }
+}
+
+}  // namespace
+
+hipError_t q8_rows(int64_t T, int32_t d, const void* x, void* q, float* scale, hipStream_t st)
+{
+    q8_rows_kernel<<<dim3(uint32_t((T + 3) / 4)), 256, 0, st>>>(int32_t(T), d, int32_t(q8_pitch(d)), static_cast<const uint16_t*>(x),
+                                                               static_cast<uint8_t*>(q), scale);
+    return hipGetLastError();
+}
+
+hipError_t q8_weight(int dtype, int32_t d_in, int32_t d_out, int64_t ldw, const void* W, void* q, float* scale, hipStream_t st)
+{
+    const dim3 grid(uint32_t((int64_t(d_out) + 63) / 64));
+    const int32_t pitch = int32_t(q8_pitch(d_in));
+    if (dtype == LOBRA_F32)
+        q8_weight_kernel<float><<<grid, 256, 0, st>>>(d_in, d_out, pitch, ldw, static_cast<const float*>(W), static_cast<uint8_t*>(q), scale);
+    else
+        q8_weight_kernel<uint16_t><<<grid, 256, 0, st>>>(d_in, d_out, pitch, ldw, static_cast<const uint16_t*>(W), static_cast<uint8_t*>(q), scale);
+    return hipGetLastError();
+}
+
+hipError_t q8_dequantise(int32_t d_in, int32_t d_out, const void* q, const float* scale, void* W, hipStream_t st)
+{
+    const dim3 grid(uint32_t((d_out + 63) / 64), uint32_t((d_in + 63) / 64));
+    q8_dequantise_kernel<<<grid, 256, 0, st>>>(d_in, d_out, int32_t(q8_pitch(d_in)), static_cast<const uint8_t*>(q), scale, static_cast<uint16_t*>(W));
+    return hipGetLastError();
+}
+
+}  // namespace lobra

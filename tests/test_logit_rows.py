@@ -1,0 +1,476 @@
+"""Rows of logits beyond their own tokens: the loss against a teacher's likeliest tokens and its gradient, the selection of beam search, and the
+reordering of what is kept per sequence.
+
+Against plain implementations in 64 bits.  Tolerances: a loss comes from sums of exponentials in fp32, a few units in the last place of 1 (4e-6, and
+2^-22 of what it is itself); a gradient is off by 2e-6 of the row's weight, and in bf16 by half a step, 2^-8 of its value.  A beam's score is rounded once to
+fp32, from a sum in 64 bits whose lse has the losses' error.  Tokens, beams and moved bytes are compared as they are.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from paper_2509_01193_amd import binding as bd
+
+torch = pytest.importorskip("torch")
+from test_step_ops import DEV, DT, guarded, logits_of  # noqa: E402
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# a teacher's likeliest tokens
+# ------------------------------------------------------------------------------------------------------------------
+def ref_distill(z, tl, ids, tail, temperature):
+    """(loss [T], gradient of each row's loss [T, V], teacher [T]) in 64 bits, row by row."""
+    T, V = z.shape
+    loss, grad, taught = torch.zeros(T, dtype=torch.float64), torch.zeros(T, V, dtype=torch.float64), torch.zeros(T, dtype=torch.bool)
+    for i in range(T):
+        x = z[i].double() / temperature
+        places = [(int(j), float(l)) for j, l in zip(ids[i], tl[i]) if 0 <= int(j) < V]
+        if not places or (not tail and all(l == -math.inf for _, l in places)):
+            continue
+        taught[i] = True
+        m = float(x.max())
+        if bool(torch.isnan(x).any()) or m == math.inf or any(math.isnan(l) or l == math.inf for _, l in places):
+            loss[i], grad[i] = math.nan, math.nan
+            continue
+        if m == -math.inf:
+            loss[i] = math.inf                       # (and no gradient)
+            continue
+        e = (x - m).exp()
+        S = e.sum()
+        p = e / S
+        if tail:
+            qs = [math.exp(l) for _, l in places]
+            ln_q = [l for _, l in places]
+        else:
+            top = max(l for _, l in places) / temperature
+            own = sum(math.exp(l / temperature - top) for _, l in places)
+            ln_q = [l / temperature - top - math.log(own) for _, l in places]
+            qs = [math.exp(v) for v in ln_q]
+        total, mass = 0.0, sum(qs)
+        g = mass * p
+        for (j, _), q, lq in zip(places, qs, ln_q):
+            if q > 0:
+                lp = float(x[j]) - m - float(S.log())
+                total += q * (lq - lp)
+            g[j] -= q
+        qr = 1 - mass if tail else 0.0
+        if qr > 2.0 ** -20:
+            rest = x.clone()
+            rest[[j for j, _ in places]] = -math.inf
+            mr = float(rest.max())
+            if mr == -math.inf:
+                total = math.inf
+                g += qr * p
+            else:
+                er = (rest - mr).exp()
+                total += qr * (math.log(qr) - (mr - m + float(er.sum().log()) - float(S.log())))
+                g += qr * (p - er / er.sum())
+        loss[i], grad[i] = total, g / temperature
+    return loss, grad, taught
+
+
+def teacher_of(kind, z, k, tail, temperature, seed):
+    """Log probabilities and ids [T, k] of another model's likeliest tokens, as `kind` has them."""
+    T, V = z.shape
+    g = torch.Generator().manual_seed(seed)
+    t = torch.nan_to_num(z.float(), nan=0.0, posinf=5.0)
+    t = torch.where(t < -1e30, torch.full_like(t, -30.0), t) + torch.randn(T, V, generator=g)
+    kk = min(k, V)
+    lp, ids = torch.log_softmax(t.double() / (temperature if tail else 1.0), dim=1).topk(kk, dim=1)
+    lp = torch.nn.functional.pad(lp, (0, k - kk), value=-math.inf).float()
+    ids = torch.nn.functional.pad(ids, (0, k - kk), value=-1).int()
+    order = torch.randperm(k, generator=g)           # (no order is asked for)
+    lp, ids = lp[:, order].contiguous(), ids[:, order].contiguous()
+    if kind == "short" or kind == "odd":
+        ids[torch.rand(T, k, generator=g) < 0.5] = -1
+    if kind == "odd":
+        ids[0] = -1                                  # a row without a teacher
+        if T > 1:
+            ids[1] = V + 3
+        if T > 2:
+            ids[2] = 0
+            lp[2] = math.log(0.5 / k)                # one token in every place
+        if T > 3:
+            lp[3] = -math.inf
+            ids[3] = torch.arange(k) % V
+        if T > 4:
+            lp[4, k // 2], ids[4, k // 2] = math.nan, 0
+    return lp, ids
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("T,V,k,temperature,kind,teacher,pad", [
+    (1, 1, 1, 1.0, "plain", "full", 0), (3, 7, 8, 2.0, "plain", "full", 0), (5, 64, 64, 1.0, "plain", "short", 0), (6, 1000, 128, 0.7, "plain", "odd", 5),
+    (7, 4099, 20, 1.0, "offset", "odd", 0), (40, 32000, 8, 1.0, "plain", "full", 0), (9, 32000, 65, 2.0, "lowest", "odd", 8), (5, 5000, 20, 1.0, "masked", "full", 0),
+    (6, 257, 32, 1.0, "equal", "odd", 1), (4, 20001, 100, 4.0, "sure", "full", 0), (4, 3000, 4, 1.0, "nan", "full", 0), (3, 300001, 40, 1.0, "plain", "odd", 0),
+    (300, 9001, 3, 1.0, "plain", "odd", 0), (2, 131072, 128, 1.0, "one_stride", "full", 0),
+])
+def test_distill(dtype, tail, T, V, k, temperature, kind, teacher, pad):
+    z = logits_of("plain" if kind == "sure" else kind, T, V, dtype, T + V + k)
+    if kind == "sure":                               # the listed tokens have all of the student's probability but 1e-15
+        z[:, :2] += 60
+        z = z.to(DT[dtype])
+    tl, ids = teacher_of(teacher, z, k, tail, temperature, V)
+    if kind == "sure":
+        ids[:, :2] = torch.tensor([0, 1], dtype=torch.int32)
+        ids[:, 2:] = torch.where(ids[:, 2:] < 2, torch.full_like(ids[:, 2:], -1), ids[:, 2:])
+        tl[:, :2] = math.log(0.1)
+    loss, grad, taught = ref_distill(z, tl, ids, tail, temperature)
+    w = torch.rand(T, generator=torch.Generator().manual_seed(T)) + 0.5
+    if T > 5:
+        w[5] = 0
+    wide = torch.full((T, V + pad), 3.0, dtype=DT[dtype], device=DEV)
+    wide[:, :V] = z.to(DEV)
+    zd = wide[:, :V]
+    desc = bd.make_distill_desc(dtype, T, V, k, tail=tail, temperature=temperature, ld=V + pad)
+    ld, lok = guarded(T, dtype=torch.float32)
+    st, sok = guarded(T, 4, dtype=torch.float32)
+    t_args = tl.to(DEV), ids.to(DEV)
+    bd.lobra_token_distill_fwd(desc, zd, *t_args, ld, st)
+    torch.cuda.synchronize()
+    assert lok() and sok()
+    got = ld.double().cpu()
+    # (a term takes the rounding of its logit's distance from the maximum: 2^-23 of it)
+    far = torch.where(torch.isfinite(loss), loss.abs(), torch.zeros_like(loss))
+    good = (got == loss) | (torch.isnan(got) & torch.isnan(loss)) | ((got - loss).abs() <= 4e-6 + 2.0 ** -22 * far)
+    if kind == "lowest":                             # distances of 1e38: only relative
+        good |= (got - loss).abs() <= 1e-6 * far
+    assert bool(good.all()), [(i, float(got[i]), float(loss[i])) for i in (~good).nonzero().flatten().tolist()[:4]]
+    only, ook = guarded(T, dtype=torch.float32)
+    bd.lobra_token_distill_fwd(desc, zd, *t_args, only)
+    assert torch.equal(torch.nan_to_num(only), torch.nan_to_num(ld)) and ook()
+    want = grad * w.double()[:, None]
+    want[w == 0] = 0
+    scale = (w.double() / temperature)[:, None]
+
+    def check(out, want, extra, what):
+        out = out.double().cpu()
+        bound = 2e-6 * scale + extra + (want.abs() * 2.0 ** -8 if dtype == "bf16" else 0)
+        bad = ~(((out - want).abs() <= bound) | (torch.isnan(out) & torch.isnan(want)))
+        assert not bool(bad.any()), (what, int(bad.sum()), bad.nonzero()[:3].tolist(), out[bad][:3].tolist(), want[bad][:3].tolist())
+
+    base = torch.full((T, V + pad), 9.0, dtype=DT[dtype], device=DEV)
+    dz = base[:, :V]
+    wd = w.to(DEV)
+    bd.lobra_token_distill_bwd(desc, zd, *t_args, st, wd, dz)
+    torch.cuda.synchronize()
+    check(dz, want, 0, "apart")
+    assert bool((base[:, V:] == 9.0).all()) and bool((wide[:, V:] == 3.0).all())
+    # added to another loss's gradient, in which rows without a weight stay as they are
+    other = (torch.randn(T, V, generator=torch.Generator().manual_seed(7)) * 0.1).to(DT[dtype])
+    base[:, :V] = other.to(DEV)
+    bd.lobra_token_distill_bwd(desc, zd, *t_args, st, wd, dz, flags=bd.FLAG_ACCUMULATE_GRADS)
+    check(dz, want + other.double(), 2.0 ** -23 * other.double().abs(), "added")
+    # over the logits
+    bd.lobra_token_distill_bwd(desc, zd, *t_args, st, wd, zd)
+    torch.cuda.synchronize()
+    check(zd, want, 0, "in place")
+    assert bool((wide[:, V:] == 3.0).all())
+
+
+@pytest.mark.gpu
+def test_distill_of_the_own_tokens_is_none():
+    """The student as its own teacher, through the log probabilities as they are written: no loss, no gradient."""
+    T, V, k = 30, 5000, 20
+    z = torch.randn(T, V, generator=torch.Generator().manual_seed(1)).to(DEV) * 4
+    f = lambda *s, dt=torch.float32: torch.empty(*s, dtype=dt, device=DEV)
+    tl, ti = f(T, k), f(T, k, dt=torch.int32)
+    bd.lobra_token_logprob_fwd(bd.make_logprob_desc("f32", T, V, top_k=k), z, None, top_logp=tl, top_id=ti)
+    desc = bd.make_distill_desc("f32", T, V, k, tail=True)
+    loss, st, dz = f(T), f(T, 4), f(T, V)
+    bd.lobra_token_distill_fwd(desc, z, tl, ti, loss, st)
+    bd.lobra_token_distill_bwd(desc, z, tl, ti, st, torch.ones(T, device=DEV), dz)
+    assert float(loss.abs().max()) < 4e-6 and float(dz.abs().max()) < 4e-6
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_gradient_against_differences(tail):
+    T, V, k, t = 4, 50, 6, 1.5
+    g = torch.Generator().manual_seed(4)
+    z = torch.randn(T, V, generator=g).to(DEV)
+    tl, ids = (x.to(DEV) for x in teacher_of("short", z.cpu(), k, tail, t, 3))
+    desc = bd.make_distill_desc("f32", T, V, k, tail=tail, temperature=t)
+    loss, st, dz = torch.empty(T, device=DEV), torch.empty(T, 4, device=DEV), torch.empty(T, V, device=DEV)
+    w = (torch.rand(T, generator=g) + 0.5).to(DEV)
+    bd.lobra_token_distill_fwd(desc, z, tl, ids, loss, st)
+    bd.lobra_token_distill_bwd(desc, z, tl, ids, st, w, dz)
+
+    def value(x):
+        bd.lobra_token_distill_fwd(desc, x, tl, ids, loss)
+        return float((loss.double() * w.double()).sum())
+
+    for _ in range(5):
+        step = torch.randn(T, V, generator=g).to(DEV)
+        h = 2.0 ** -6
+        # central differences: h^2 / 6 times a third derivative of a few; the losses' own error over 2 h
+        slope = (value(z + h * step) - value(z - h * step)) / (2 * h)
+        want = float((dz.double() * step.double()).sum())
+        assert abs(slope - want) < 20 * h * h / 6 + T * 1.5 * 8e-6 / h, (slope, want)
+
+
+def test_distill_refusals():
+    L, p = bd.lib(), 4096
+    mk = lambda dtype="bf16", T=3, V=100, k=5, **kw: bd.make_distill_desc(dtype, T, V, k, **kw)
+    F = lambda d, z=p, l=p, i=p, loss=p, st=p: L.lobra_token_distill_fwd(ctypes.byref(d) if d else None, z, l, i, loss, st, None)
+    B = lambda d, z=p, l=p, i=p, st=p, w=p, dz=p, flags=0: L.lobra_token_distill_bwd(ctypes.byref(d) if d else None, z, l, i, st, w, dz, flags, None)
+    for call in (F, B):
+        assert call(None) == -1 and call(mk(dtype=2)) == -3
+        for bad in (mk(V=0), mk(V=(1 << 24) + 1), mk(T=-1), mk(T=1 << 31), mk(k=0), mk(k=129), mk(ld=99), mk(ld=1 << 59), mk(temperature=0.0), mk(temperature=-1.0),
+                    mk(temperature=math.inf), mk(temperature=math.nan), mk(temperature=1e-40), mk(tail=2), mk(tail=-1)):
+            assert call(bad) == -2
+        assert call(mk(), z=None) == -1 and call(mk(), l=None) == -1 and call(mk(), i=None) == -1
+        assert call(mk(), z=p + 2) == -8 and call(mk(), l=p + 2) == -8 and call(mk(), i=p + 1) == -8 and call(mk(), st=p + 4) == -8
+        assert call(mk(T=0), z=None) == 0
+    assert F(mk(), loss=None, st=None) == 0 and F(mk(), loss=p + 1) == -8
+    assert B(mk(), st=None) == -1 and B(mk(), w=None) == -1 and B(mk(), dz=None) == -1 and B(mk(), w=p + 2) == -8 and B(mk(), dz=p + 8) == -8
+    assert B(mk(), flags=bd.FLAG_ACCUMULATE_GRADS) == -2                 # (dlogits is logits)
+    z, f, i = torch.zeros(3, 100).bfloat16(), torch.zeros(3, 5), torch.zeros(3, 5, dtype=torch.int32)
+    loss, st = torch.zeros(3), torch.zeros(3, 4)
+    for bad in (dict(logits=z.float()), dict(logits=z[:2]), dict(teacher_logp=f[:2]), dict(teacher_logp=f.double()), dict(teacher_id=i.long()), dict(teacher_id=i[:, :4]),
+                dict(loss=loss[:2]), dict(loss=loss.half()), dict(stat=st[:2]), dict(stat=st.double())):
+        with pytest.raises(AssertionError):
+            bd.lobra_token_distill_fwd(mk(), **{**dict(logits=z, teacher_logp=f, teacher_id=i, loss=loss, stat=st), **bad}, stream=0)
+    for bad in (dict(dlogits=z.float()), dict(dlogits=z[:, :99]), dict(dloss=loss[:2]), dict(dloss=loss.bfloat16())):
+        with pytest.raises(AssertionError):
+            bd.lobra_token_distill_bwd(mk(), **{**dict(logits=z, teacher_logp=f, teacher_id=i, stat=st, dloss=loss, dlogits=z), **bad}, stream=0)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# beam search
+# ------------------------------------------------------------------------------------------------------------------
+def ref_select(z, score, done, done_token, k):
+    """Scores, beams, tokens [n, k], from all continuations sorted in 64 bits; equal ones stay in order."""
+    n, b = score.shape
+    V = z.shape[1]
+    out = [], [], []
+    for i in range(n):
+        total = torch.full((b, V + 1), -math.inf, dtype=torch.float64)       # (the last column: a beam that is done)
+        for j in range(b):
+            s = float(score[i, j])
+            if not s > -math.inf:
+                continue
+            if done is not None and int(done[i, j]):
+                total[j, V] = s
+                continue
+            x = z[i * b + j].double()
+            m = float(x.max())
+            if bool(torch.isnan(x).any()) or not abs(m) < math.inf:
+                continue
+            total[j, :V] = (s - (m + math.log(float((x - m).exp().sum())))) + x
+        v, at = torch.sort(total.flatten(), descending=True, stable=True)
+        v, at = v[:k], at[:k]
+        some = v > -math.inf
+        tok = torch.where(at % (V + 1) == V, done_token, at % (V + 1))
+        pad = (0, k - len(v))
+        out[0].append(torch.nn.functional.pad(v, pad, value=-math.inf))
+        out[1].append(torch.nn.functional.pad(torch.where(some, at // (V + 1), -1), pad, value=-1))
+        out[2].append(torch.nn.functional.pad(torch.where(some, tok, -1), pad, value=-1))
+    return tuple(torch.stack(o) for o in out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,b,V,k,kind,pad", [
+    (1, 1, 1, 1, "plain", 0), (2, 3, 2, 8, "plain", 0), (1, 4, 32000, 4, "plain", 0), (3, 5, 4099, 10, "plain", 3), (40, 2, 8192, 4, "plain", 0), (2, 4, 8193, 8, "plain", 1),
+    (3, 8, 20001, 16, "offset", 0), (2, 16, 1000, 32, "plain", 0), (2, 32, 30, 32, "plain", 2), (2, 4, 5000, 32, "masked", 0), (2, 3, 9000, 8, "lowest", 0),
+    (2, 4, 20000, 32, "equal", 0), (2, 2, 40960, 32, "constant", 0), (3, 4, 3001, 8, "twins", 0), (2, 4, 3000, 4, "nan", 0), (5, 4, 50257, 8, "first", 0),
+    (7, 4, 500, 4, "done", 0), (2, 3, 70, 8, "none", 0), (1, 2, 300000, 32, "one_stride", 0),
+])
+def test_beam_select(dtype, n, b, V, k, kind, pad):
+    z = logits_of(kind if kind in ("offset", "masked", "lowest", "equal", "nan", "one_stride") else "plain", n * b, V, dtype, n + b + V)
+    g = torch.Generator().manual_seed(k)
+    score = -10 * torch.rand(n, b, generator=g)
+    done = None
+    if kind == "constant":                           # nothing but equals
+        z[:] = 0.5
+        score[:] = -1.0
+    elif kind == "twins":                            # beams of the same logits and score, whose rows begin at other alignments
+        z = z[::b].repeat_interleave(b, dim=0).contiguous()
+        score[:] = score[:, :1]
+    elif kind == "first":
+        score[:, 1:] = -math.inf
+    elif kind == "done":
+        done = (torch.rand(n, b, generator=g) < 0.6).int()
+        done[0] = 1
+        score[1, 2], score[2, 0] = math.nan, -math.inf
+        z[0] = math.nan                              # (of a beam that is done)
+    elif kind == "none":
+        score[0] = -math.inf
+        z[b:] = -math.inf
+    want = ref_select(z, score, done, 2, k)
+    wide = torch.full((n * b, V + pad), 1e4, dtype=DT[dtype], device=DEV)
+    wide[:, :V] = z.to(DEV)
+    desc = bd.make_beam_desc(dtype, n, b, V, k, ld=V + pad)
+    ws, wok = guarded(bd.lobra_beam_workspace_bytes(desc), dtype=torch.uint8)
+    os_, ob, ot = guarded(n, k, dtype=torch.float32), guarded(n, k, dtype=torch.int32), guarded(n, k, dtype=torch.int32)
+    sd, dd = score.to(DEV), None if done is None else done.to(DEV)
+    bd.lobra_beam_select(desc, wide[:, :V], sd, dd, 2, os_[0], ob[0], ot[0], ws)
+    torch.cuda.synchronize()
+    assert wok() and os_[1]() and ob[1]() and ot[1]()
+    got, ref = os_[0].double().cpu(), want[0]
+    assert bool(((got == ref) | ((got - ref).abs() <= 4e-6 + 2.0 ** -23 * ref.abs())).all()), (got, ref)
+    assert torch.equal(ob[0].cpu().long(), want[1]), (ob[0], want[1])
+    assert torch.equal(ot[0].cpu().long(), want[2]), (ot[0], want[2])
+    if k == b:                                       # over the scores
+        bd.lobra_beam_select(desc, wide[:, :V], sd, dd, 2, sd, ob[0], ot[0], ws)
+        assert torch.equal(sd, os_[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n,b,shapes,dtype,limited", [
+    (1, 1, [(3,)], torch.float32, False), (3, 4, [(5, 8), (7, 33), (1, 1)], torch.bfloat16, True), (2, 5, [(77, 33)], torch.float32, True),
+    (5, 8, [(64, 512)] * 3, torch.bfloat16, True), (2, 32, [(11, 7)], torch.uint8, True), (2, 16, [(2000, 64), (3, 5), (2, 16)], torch.bfloat16, False),
+    (3, 2, [(4, 6)] * 150, torch.float32, True), (2, 3, [(0, 4), (6, 0), (9, 4)], torch.float32, True), (70, 3, [(5,)], torch.int64, False),
+])
+def test_beam_reorder(in_place, n, b, shapes, dtype, limited):
+    g = torch.Generator().manual_seed(n + b)
+    parent = torch.randint(0, b, (n, b + 2), generator=g, dtype=torch.int32)
+    parent[0, :b] = torch.arange(1, b + 1) % b       # a cycle
+    if n > 1:
+        parent[1, 0] = -1
+        parent[1, b - 1] = b
+    used = None
+    if limited:
+        used = torch.randint(0, 12, (n,), generator=g, dtype=torch.int32)
+        used[0] = 1 << 30
+        if n > 2:
+            used[2] = -5
+    src = [torch.randint(-100, 100, (n * b, *s), generator=g).to(dtype) for s in shapes]
+    want, states, checks = [], [], []
+    for s in src:
+        d = s.clone() if in_place else torch.full_like(s, 99)
+        for i in range(n):
+            rows = s[i * b:(i + 1) * b].clone()
+            for j in range(b):
+                p = int(parent[i, j])
+                if not 0 <= p < b:
+                    continue
+                if used is None:
+                    d[i * b + j] = rows[p]
+                else:
+                    u = min(max(int(used[i]), 0), s.shape[1])
+                    d[i * b + j, :u] = rows[p, :u]
+        want.append(d)
+        dev, ok = guarded(*s.shape, dtype=dtype)
+        dev.copy_(s)
+        out, ok2 = (dev, ok) if in_place else guarded(*s.shape, dtype=dtype)
+        if not in_place:
+            out.fill_(99)
+        states.append((dev, out))
+        checks += [ok, ok2]
+    bd.lobra_beam_reorder(states, n, b, parent.to(DEV), None if used is None else used.to(DEV))
+    torch.cuda.synchronize()
+    assert all(ok() for ok in checks)
+    for (s0, d), s, ref in zip(states, src, want):
+        assert torch.equal(d.cpu(), ref)
+        assert in_place or torch.equal(s0.cpu(), s)
+
+
+@pytest.mark.gpu
+def test_beam_reorder_beyond_32_bits():
+    """Rows of 1.5 GB: offsets that 32 bits do not hold."""
+    n, b, L = 1, 3, 3 * 2 ** 28
+    s = torch.empty(n * b, L, dtype=torch.int16, device=DEV)
+    for i in range(b):
+        s[i].fill_(i + 1)
+        s[i, -1] = 100 + i
+    bd.lobra_beam_reorder([(s, s)], n, b, torch.tensor([[2, 1, 0]], dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    assert [int(v) for v in s[:, -1]] == [102, 101, 100]
+    for i, v in enumerate((3, 2, 1)):
+        assert bool((s[i, :-1] == v).all())
+
+
+def test_beam_refusals():
+    L, p, n = bd.lib(), 4096, ctypes.c_size_t()
+    mk = lambda dtype="bf16", n=2, b=3, V=100, k=4, **kw: bd.make_beam_desc(dtype, n, b, V, k, **kw)
+    size = lambda d: L.lobra_beam_workspace_bytes(ctypes.byref(d) if d else None, ctypes.byref(n))
+    S = lambda d, z=p, s=p, done=p, os=p + 64, ob=p, ot=p, ws=p, nb=1 << 30: L.lobra_beam_select(ctypes.byref(d) if d else None, z, s, done, 2, os, ob, ot, ws, nb, None)
+    for call in (size, S):
+        assert call(None) == -1 and call(mk(dtype=2)) == -3
+        for bad in (mk(V=0), mk(V=(1 << 24) + 1), mk(n=-1), mk(b=0), mk(b=33), mk(k=0), mk(k=33), mk(ld=99), mk(ld=1 << 58), mk(n=1 << 23), mk(n=1 << 17, V=1 << 20)):
+            assert call(bad) == -2
+    assert size(mk()) == 0 and n.value == 6 * (4 * 8 + 8) and L.lobra_beam_workspace_bytes(ctypes.byref(mk()), None) == -1
+    assert S(mk(n=0), z=None) == 0
+    assert S(mk(), z=None) == -1 and S(mk(), s=None) == -1 and S(mk(), os=None) == -1 and S(mk(), ob=None) == -1 and S(mk(), ot=None) == -1
+    assert S(mk(), z=p + 2) == -8 and S(mk(), s=p + 2) == -8 and S(mk(), done=p + 2) == -8 and S(mk(), ws=p + 8) == -8 and S(mk(), ot=p + 1) == -8
+    assert S(mk(), ws=None) == -7 and S(mk(), nb=6 * 40 - 1) == -7
+    assert S(mk(), os=p) == -2                       # (over the scores, of which there are fewer)
+    z, f, i = torch.zeros(6, 100).bfloat16(), torch.zeros(2, 3), torch.zeros(2, 3, dtype=torch.int32)
+    of, oi, ws = torch.zeros(2, 4), torch.zeros(2, 4, dtype=torch.int32), torch.zeros(512, dtype=torch.uint8)
+    ok = dict(logits=z, score=f, done=i, done_token=2, out_score=of, out_beam=oi, out_token=oi, ws=ws)
+    for bad in (dict(logits=z.float()), dict(logits=z[:5]), dict(score=f[:1]), dict(score=f.double()), dict(done=i.bool()), dict(done=i[:1]), dict(out_score=of[:1]),
+                dict(out_beam=oi.long()), dict(out_token=oi[:, :2])):
+        with pytest.raises(AssertionError):
+            bd.lobra_beam_select(mk(), **{**ok, **bad}, stream=0)
+
+
+def test_reorder_refusals():
+    L, p = bd.lib(), 1 << 20
+
+    def R(src=p, dst=p, row=64, unit=8, n_states=1, n=2, b=3, parent=p, ld=3, used=p, arr=True):
+        t = (bd.BeamState * 1)(bd.BeamState(src, dst, row, unit))
+        return L.lobra_beam_reorder(t if arr else None, n_states, n, b, parent, ld, used, None)
+
+    for bad in (dict(n_states=-1), dict(n=-1), dict(b=0), dict(b=33), dict(ld=2), dict(ld=1 << 40), dict(n=1 << 23), dict(row=-1), dict(unit=-1), dict(row=1 << 58)):
+        assert R(**bad) == -2, bad
+    assert R(arr=False) == -1 and R(src=None) == -1 and R(dst=None) == -1 and R(parent=None) == -1
+    assert R(parent=p + 2) == -8 and R(used=p + 1) == -8
+    for shift in (1, 64, 383, -1, -383):             # six rows of 64 bytes
+        assert R(dst=p + shift) == -2
+    assert R(n_states=0) == 0 and R(n=0) == 0 and R(row=0, src=None, dst=None) == 0
+    s, par = torch.zeros(6, 4, 5), torch.zeros(2, 3, dtype=torch.int32)
+    for bad in (dict(states=[(s, s.half())]), dict(states=[(s, s[:, :3].contiguous())]), dict(states=[(s[:5], s[:5])]), dict(parent=par.long()), dict(parent=par[:1]),
+                dict(parent=par[:, :2]), dict(used=par[0, :1]), dict(states=[(s[:, 0, 0].contiguous(),) * 2]), dict(states=[(s[:, :, 1:],) * 2])):
+        with pytest.raises(AssertionError):
+            bd.lobra_beam_reorder(**{**dict(states=[(s, s)], n_req=2, beams=3, parent=par, used=torch.zeros(2, dtype=torch.int32)), **bad}, stream=0)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+def test_on_another_stream_and_in_a_graph():
+    """A teacher's tokens from the library's own log probabilities, loss and gradient; a step of beam search with its states."""
+    n, b, V, k, L = 3, 4, 5003, 4, 20
+    g = torch.Generator().manual_seed(2)
+    teacher, z = (torch.randn(n * b, V, generator=g).bfloat16().to(DEV) * 3 for _ in range(2))
+    score, hist = -torch.rand(n, b, generator=g).to(DEV), torch.randint(0, V, (n * b, L), generator=g, dtype=torch.int32).to(DEV)
+    w = torch.rand(n * b, generator=g).to(DEV)
+    ld, dd, bdsc = bd.make_logprob_desc("bf16", n * b, V, top_k=20), bd.make_distill_desc("bf16", n * b, V, 20, tail=True), bd.make_beam_desc("bf16", n, b, V, k)
+    ws = torch.empty(bd.lobra_beam_workspace_bytes(bdsc), dtype=torch.uint8, device=DEV)
+
+    def outputs():
+        f = lambda *s, dt=torch.float32: torch.zeros(*s, dtype=dt, device=DEV)
+        return dict(tl=f(n * b, 20), ti=f(n * b, 20, dt=torch.int32), loss=f(n * b), st=f(n * b, 4), dz=torch.zeros_like(z), s=f(n, k), bm=f(n, k, dt=torch.int32),
+                    tk=f(n, k, dt=torch.int32), next=torch.zeros_like(hist))
+
+    def go(o):
+        bd.lobra_token_logprob_fwd(ld, teacher, None, top_logp=o["tl"], top_id=o["ti"])
+        bd.lobra_token_distill_fwd(dd, z, o["tl"], o["ti"], o["loss"], o["st"])
+        bd.lobra_token_distill_bwd(dd, z, o["tl"], o["ti"], o["st"], w, o["dz"])
+        bd.lobra_beam_select(bdsc, z, score, None, 2, o["s"], o["bm"], o["tk"], ws)
+        bd.lobra_beam_reorder([(hist, o["next"])], n, b, o["bm"])
+
+    eager, other, graphed = outputs(), outputs(), outputs()
+    go(eager)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        go(other)
+    torch.cuda.synchronize()
+    assert all(torch.equal(eager[i], other[i]) for i in eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go(graphed)
+    for r in range(3):
+        z.mul_(1.0 if r == 0 else 0.7)
+        graph.replay()
+        torch.cuda.synchronize()
+        go(eager)
+        torch.cuda.synchronize()
+        assert all(torch.equal(eager[i], graphed[i]) for i in eager), r
