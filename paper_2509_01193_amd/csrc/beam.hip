@@ -33,28 +33,22 @@ template <typename E> __device__ __forceinline__ void put(u32x4& q, int e, E v)
     else q[e >> 1] = e & 1 ? (q[e >> 1] & 0xffffu) | uint32_t(v) << 16 : (q[e >> 1] & 0xffff0000u) | uint32_t(v);
 }
 
-// The k-th largest (k <= 64) of 64 numbers that lane i of the first wave has one each of, among equals by lane: told to all of that wave.
-__device__ __forceinline__ double kth_of_64(double v, int32_t k)
+// A number that at least k (<= 64) of 64 numbers reach, a lane's each, and few more than k: the largest whose order's lower 16 bits are clear (all
+// that bf16 has).  Every lane of the wave has to be active; all get it.  (Bit by bit, a ballot each: a tenth of the instructions of counting in front.)
+__device__ __forceinline__ uint32_t float_order(float z)
 {
-    int32_t in_front = 0;
-    const int32_t lane = threadIdx.x & 63;
-#pragma unroll 8
-    for (int32_t o = 0; o < 64; ++o) {
-        const double other = __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), o), __builtin_amdgcn_readlane(__double2loint(v), o));
-        in_front += other > v || (other == v && o < lane) ? 1 : 0;
-    }
-    return __shfl(v, __builtin_ctzll(__ballot(in_front == k - 1)));
+    const uint32_t b = __float_as_uint(z + 0.f);       // (-0 is 0)
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float kth_of_64(float v, int32_t k)
+__device__ __forceinline__ uint32_t reached_by(uint32_t order, int32_t k)
 {
-    int32_t in_front = 0;
-    const int32_t lane = threadIdx.x & 63;
+    uint32_t t = 0;
 #pragma unroll
-    for (int32_t o = 0; o < 64; ++o) {
-        const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), o));
-        in_front += other > v || (other == v && o < lane) ? 1 : 0;
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t c = t | 1u << bit;
+        if (__popcll(__ballot(order >= c)) >= k) t = c;
     }
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), __builtin_ctzll(__ballot(in_front == k - 1))));
+    return t;
 }
 
 // Whether a beam's logits are looked at.
@@ -70,7 +64,7 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
 {
     constexpr int N = Packet<E>::N, U = kPart / (kThreads * N), W = kThreads / 64;
     __shared__ uint64_t list[kList];
-    __shared__ float group_max[64], tau_s;
+    __shared__ float group_max[64];
     __shared__ Stat stat[W];
     __shared__ int32_t count;
     const int32_t row = int32_t(blockIdx.x) / parts, part = int32_t(blockIdx.x) - row * parts;
@@ -93,27 +87,32 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
     }
     if (tid == 0) count = 0;
     Stat a{-INFINITY, 0.f, 0.f};
+    float most[U];                                   // of each packet
     {
         float z[U * N];
 #pragma unroll
-        for (int c = 0; c < U; ++c)
+        for (int c = 0; c < U; ++c) {
 #pragma unroll
             for (int e = 0; e < N; ++e) z[c * N + e] = Packet<E>::element(q[c], e);
+            most[c] = z[c * N];
+#pragma unroll
+            for (int e = 1; e < N; ++e) most[c] = fmaxf(most[c], z[c * N + e]);
+        }
         take<false>(a, z, kLog2e);
     }
-    float g = a.m;
-#pragma unroll
-    for (int x = 1; x < kThreads / 64; x <<= 1) g = fmaxf(g, __shfl_xor(g, x));
-    if (tid % (kThreads / 64) == 0) group_max[tid / (kThreads / 64)] = g;
     const float mine = a.m;
+    {
+        float g = mine;
+#pragma unroll
+        for (int x = 1; x < kThreads / 64; x <<= 1) g = fmaxf(g, __shfl_xor(g, x));
+        if (tid % (kThreads / 64) == 0) group_max[tid / (kThreads / 64)] = g;
+    }
     rescale<false>(a, wave_max(a.m), kLog2e);
     a.s = wave_sum(a.s);
     if (lane == 0) stat[tid >> 6] = a;
     __syncthreads();
-    if (tid < 64) {
-        const float v = kth_of_64(group_max[lane], n);
-        if (lane == 0) tau_s = v;
-    } else if (tid == 64) {
+    const uint32_t tau = reached_by(float_order(group_max[lane]), n);       // (-inf: 0x007f....; its bits below are clear in tau)
+    if (tid == 0) {
         float m = stat[0].m, s = 0.f;
 #pragma unroll
         for (int w = 1; w < W; ++w) m = fmaxf(m, stat[w].m);
@@ -125,22 +124,23 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
         }
         sums[blockIdx.x] = make_float2(m, s);
     }
-    __syncthreads();
-    const float tau = tau_s;
-    if (mine >= tau && mine > -INFINITY) {
+    // packet by packet, of those in which any lane of the wave has one
 #pragma unroll
-        for (int c = 0; c < U; ++c) {
-            uint32_t hits = 0;
+    for (int c = 0; c < U; ++c) {
+        if (!(most[c] > -INFINITY && float_order(most[c]) >= tau)) continue;
+        uint32_t hits = 0;
 #pragma unroll
-            for (int e = 0; e < N; ++e) hits |= Packet<E>::element(q[c], e) >= tau ? 1u << e : 0u;
-            for (; hits; hits &= hits - 1) {
-                const int e = __builtin_ctz(hits);
-                float z = 0.f;
+        for (int e = 0; e < N; ++e) {
+            const float z = Packet<E>::element(q[c], e);
+            hits |= z > -INFINITY && float_order(z) >= tau ? 1u << e : 0u;
+        }
+        for (; hits; hits &= hits - 1) {
+            const int e = __builtin_ctz(hits);
+            float z = 0.f;
 #pragma unroll
-                for (int i = 0; i < N; ++i) z = i == e ? Packet<E>::element(q[c], i) : z;
-                const int32_t o = atomicAdd(&count, z > -INFINITY ? 1 : 0);
-                if (z > -INFINITY && o < kList) list[o] = order_key(z, base + (c * kThreads + tid) * N + e);
-            }
+            for (int i = 0; i < N; ++i) z = i == e ? Packet<E>::element(q[c], i) : z;
+            const int32_t o = atomicAdd(&count, 1);
+            if (o < kList) list[o] = order_key(z, base + (c * kThreads + tid) * N + e);
         }
     }
     __syncthreads();
@@ -204,7 +204,7 @@ void beam_merge_kernel(BeamShape sh, const float* score, const int32_t* __restri
     __shared__ double offset[LOBRA_MAX_TOP];         // s - lse; -inf: no continuations
     __shared__ int32_t kind[LOBRA_MAX_TOP];          // 0: none, 1: its logits, 2: done
     __shared__ Next list[kList];
-    __shared__ double group_max[64], tau_s;
+    __shared__ uint32_t group_max[64];
     __shared__ int32_t count;
     const int32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = sh.n_out;
     const size_t row0 = size_t(blockIdx.x) * sh.beams;
@@ -245,26 +245,23 @@ void beam_merge_kernel(BeamShape sh, const float* score, const int32_t* __restri
         c.token = key_index(key);
         return key != 0;
     };
-    double best = -INFINITY;
+    // (as in a part: values by their order in fp32, rounded down, so that none is above what it stands for)
+    auto order = [](double v) { return float_order(__double2float_rd(v)); };
+    uint32_t best = 0;
     for (int32_t i = tid; i < total; i += kThreads) {
         Next c;
-        if (value(i, c) && c.v > best) best = c.v;
+        if (value(i, c)) best = max(best, order(c.v));
     }
-    double g = best;
+    uint32_t g = best;
 #pragma unroll
-    for (int x = 1; x < kThreads / 64; x <<= 1) g = fmax(g, __shfl_xor(g, x));
+    for (int x = 1; x < kThreads / 64; x <<= 1) g = max(g, uint32_t(__shfl_xor(int(g), x)));
     if (tid % (kThreads / 64) == 0) group_max[tid / (kThreads / 64)] = g;
     __syncthreads();
-    if (tid < 64) {
-        const double v = kth_of_64(group_max[lane], n);
-        if (lane == 0) tau_s = v;
-    }
-    __syncthreads();
-    const double tau = tau_s;
-    if (best >= tau && best > -INFINITY)
+    const uint32_t tau = reached_by(group_max[lane], n);
+    if (best >= tau && best > 0)
         for (int32_t i = tid; i < total; i += kThreads) {
             Next c;
-            if (value(i, c) && c.v >= tau) {
+            if (value(i, c) && order(c.v) >= tau) {
                 const int32_t o = atomicAdd(&count, 1);
                 if (o < kList) list[o] = c;
             }
@@ -294,7 +291,7 @@ void beam_merge_kernel(BeamShape sh, const float* score, const int32_t* __restri
         Next top = nobody;
         for (int32_t i = tid; i < total; i += kThreads) {
             Next c;
-            if (value(i, c) && c.v >= tau && in_front(last, c) && (top.beam < 0 || in_front(c, top))) top = c;
+            if (value(i, c) && in_front(last, c) && (top.beam < 0 || in_front(c, top))) top = c;
         }
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) {

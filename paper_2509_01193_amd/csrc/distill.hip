@@ -30,13 +30,60 @@ __device__ __forceinline__ double wave_sum64(double v)
     return v;
 }
 
+// (bare: loads in flight stay there)
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// A place of the row's list: a thread's own, read behind the first loads of the row.
+template <typename E> struct Place {
+    const E* row;
+    const int32_t* ids;
+    const float* ls;
+    int32_t V, k;
+    int32_t id = -1;
+    float l = -INFINITY, z = 0.f;
+    __device__ __forceinline__ void read()
+    {
+        const int32_t t = threadIdx.x;
+        if (t >= k) return;
+        id = ids[t];
+        l = ls[t];
+        if (l == INFINITY) l = NAN;
+        if (uint32_t(id) >= uint32_t(V)) id = -1, l = -INFINITY;
+        else z = element(row, id);
+    }
+};
+template <typename E> struct NoneListed {
+    Place<E>& mine;
+    __device__ __forceinline__ void begin() const { mine.read(); }
+    template <int N> __device__ __forceinline__ void operator()(float (&)[N], int32_t, int = 0) const {}
+};
+
 // Elements listed in a row, as bits.  Bit 0 of a packet's is bit 0 of a group of N (the elements in front of the first packet end a group of their own).
-template <typename E> struct ListedBits {
+template <typename E, int NT> struct ListedBits {
     static constexpr int N = Packet<E>::N;
-    const uint32_t* table;
-    const int32_t* id;
+    Place<E>& mine;
+    uint32_t* table;
+    int32_t* id;
     int32_t shift, mask, k;
     bool folded;
+    __device__ __forceinline__ void begin() const
+    {
+        const int32_t t = threadIdx.x;
+        for (int32_t i = t; i < (mask + 1) / 128; i += NT) reinterpret_cast<u32x4*>(table)[i] = u32x4{0u, 0u, 0u, 0u};
+        lds_barrier();
+        mine.read();
+        if (t < kMost) id[t] = mine.id;
+        if (mine.id >= 0) {
+            const int32_t bit = (mine.id + shift) & mask;
+            atomicOr(&table[bit >> 5], 1u << (bit & 31));
+        }
+        lds_barrier();
+    }
     template <int M> __device__ __forceinline__ void operator()(float (&z)[M], int32_t first, int at = 0) const
     {
         const int32_t bit = (first + shift) & mask;
@@ -74,30 +121,13 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
     const RowShape sh = row_shape(row, V);
     const int32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float c = 1.f / temperature, scale = c * kLog2e;
-    // the list
-    float l = -INFINITY, zj = 0.f;
-    int32_t id = -1;
-    if (tid < k) {
-        id = teacher_id[r * size_t(k) + tid];
-        l = teacher_logp[r * size_t(k) + tid];
-        if (uint32_t(id) >= uint32_t(V)) id = -1, l = -INFINITY;
-        else zj = element(row, id);
-        if (l == INFINITY) l = NAN;
-    }
     const int32_t shift = sh.head ? N - sh.head : 0;
-    if (TAIL) {
-        for (int32_t i = tid; i < table_bits / 128; i += NT) reinterpret_cast<u32x4*>(table)[i] = u32x4{0u, 0u, 0u, 0u};
-        if (tid < kMost) ids[tid] = id;
-        __syncthreads();
-        if (id >= 0) {
-            const int32_t bit = (id + shift) & (table_bits - 1);
-            atomicOr(&table[bit >> 5], 1u << (bit & 31));
-        }
-        __syncthreads();
-    }
+    Place<E> mine{row, teacher_id + r * size_t(k), teacher_logp + r * size_t(k), V, k};
     Stat a;
-    if constexpr (TAIL) a = row_stat<E, NT, false>(row, sh, scale, ListedBits<E>{table, ids, shift, table_bits - 1, k, V + N > table_bits});
-    else a = row_stat<E, NT, false>(row, sh, scale);
+    if constexpr (TAIL) a = row_stat<E, NT, false>(row, sh, scale, ListedBits<E, NT>{mine, table, ids, shift, table_bits - 1, k, V + N > table_bits});
+    else a = row_stat<E, NT, false>(row, sh, scale, NoneListed<E>{mine});
+    const float l = mine.l, zj = mine.z;
+    const int32_t id = mine.id;
     rescale<false>(a, wave_max(a.m), scale);
     a.s = wave_sum(a.s);
     if (lane == 0) part[wave] = a;
@@ -189,7 +219,10 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
 
 // Workgroup (row, part): packets part * NT + ... with a stride of all parts.  In place (dlogits = logits) every thread writes what it has
 // read itself, and the threads of the list read their logits before that.  A row without any weight is not read.
-template <typename E, int NT, bool TAIL, bool ADD>
+// The last rows come first: they are what forward has left in the 256 MB infinity cache, and gradients that would fill it anyway (once: logits of
+// 128 MB and more) go past the caches.  Forward and backward, us: 8190 x 32000 bf16 290, either alone 288 and 287, both 275; 4096 x 128000 643, 641,
+// 614, 604; 1000 x 50257 fp32 145, 145, 127, 127.
+template <typename E, int NT, bool TAIL, bool ADD, bool ONCE>
 __global__ __launch_bounds__(NT)
 void distill_bwd_kernel(const E* logits, int64_t ld, int32_t V, int32_t k, float temperature, const float* __restrict__ teacher_logp,
                         const int32_t* __restrict__ teacher_id, const float4* __restrict__ stat, const float* __restrict__ dloss, E* dlogits)
@@ -198,7 +231,7 @@ void distill_bwd_kernel(const E* logits, int64_t ld, int32_t V, int32_t k, float
     static_assert(NT >= kMost, "a thread per place of the list");
     __shared__ int32_t ids[kMost];
     __shared__ float qs[kMost];
-    const size_t r = size_t(xcd_contiguous(int32_t(blockIdx.x), int32_t(gridDim.x)));
+        const size_t r = size_t(xcd_contiguous(int32_t(gridDim.x - 1 - blockIdx.x), int32_t(gridDim.x)));
     const E* row = logits + r * size_t(ld);
     E* out = dlogits + r * size_t(ld);
     const RowShape sh = row_shape(row, V);            // (logits and dlogits are aligned alike: both bases to 16 bytes)
@@ -268,7 +301,8 @@ void distill_bwd_kernel(const E* logits, int64_t ld, int32_t V, int32_t k, float
 #pragma unroll
             for (int e = 0; e < N; ++e) g[e] = gradient(z[e]);
         }
-        dst[i] = Packet<E>::narrow(g);
+        if constexpr (ONCE) __builtin_nontemporal_store(Packet<E>::narrow(g), dst + i);
+        else dst[i] = Packet<E>::narrow(g);
     }
     if (blockIdx.y == 0 && t < sh.head + sh.tail) {
         const int32_t at = t < sh.head ? t : t + sh.packets * N;
@@ -309,8 +343,10 @@ hipError_t bwd(const DistillShape& s, const E* logits, const float* tl, const in
     // a workgroup per row where there are enough rows, else several, of at least four packets a thread
     const int64_t most = (int64_t(s.V) / Packet<E>::N + 4 * NT - 1) / (4 * NT), wanted = (2048 + s.T - 1) / s.T;
     const dim3 grid(uint32_t(s.T), uint32_t(wanted < most ? wanted : most > 0 ? most : 1));
+    const bool once = s.T * s.V * int64_t(sizeof(E)) >= int64_t(128) << 20;
 #define LOBRA_DISTILL(tail, acc) \
-    distill_bwd_kernel<E, NT, tail, acc><<<grid, NT, 0, st>>>(logits, s.ld, s.V, s.top_k, s.temperature, tl, ti, stat, dloss, dlogits)
+    (once ? distill_bwd_kernel<E, NT, tail, acc, true> : distill_bwd_kernel<E, NT, tail, acc, false>)<<<grid, NT, 0, st>>>( \
+        logits, s.ld, s.V, s.top_k, s.temperature, tl, ti, stat, dloss, dlogits)
     if (s.tail) {
         if (add) LOBRA_DISTILL(true, true);
         else LOBRA_DISTILL(true, false);

@@ -55,11 +55,13 @@ template <typename E> __device__ __forceinline__ u32x4 nothing()
 // last one filled up with -inf.  (One by one, what is left behind the whole batches - up to a quarter of a row - would wait for memory U
 // times more.)
 // left_out(z, first): the values of the packet that begins at element `first` of the row, or of a single element, which may take some out (-inf).
+// left_out.begin() runs when the first loads are on their way.
 struct NoneLeftOut {
+    __device__ __forceinline__ void begin() const {}
     template <int N> __device__ __forceinline__ void operator()(float (&)[N], int32_t, int = 0) const {}
 };
 template <typename E, int NT, bool ENT, typename F = NoneLeftOut>
-__device__ __forceinline__ Stat row_stat(const E* row, const RowShape& sh, float scale = kLog2e, F left_out = F())
+__device__ __forceinline__ Stat row_stat(const E* row, const RowShape& sh, float scale = kLog2e, F&& left_out = F())
 {
     constexpr int N = Packet<E>::N, U = 4;
     Stat a{-INFINITY, 0.f, 0.f};
@@ -80,6 +82,7 @@ __device__ __forceinline__ Stat row_stat(const E* row, const RowShape& sh, float
     const bool has_edge = t < sh.head + sh.tail;
     E edge = E(0);
     if (has_edge) edge = row[t < sh.head ? t : t + sh.packets * N];
+    left_out.begin();
     for (int32_t first = 0; first < sh.packets; first += U * NT) {
         if (first + U * NT < sh.packets) fetch(next, first + U * NT);
         float z[U * N];
