@@ -675,14 +675,19 @@ def lobra_beam_select(desc: BeamDesc, logits, score, done, done_token, out_score
 def lobra_beam_reorder(states, n_req, beams, parent, used=None, stream=None, check=True):
     """states: [(src, dst)] of tensors [n_req * beams, ...] of any type, dst may be src; with `used` (int32 [n_req]) only the first used positions
     (dimension 1) of a request's rows move.  parent: int32 [n_req, >= beams], whose rows may lie in wider ones.  Returns the status."""
-    arr = (BeamState * max(len(states), 1))()
-    for a, (src, dst) in zip(arr, states):
-        assert src.dtype is dst.dtype and src.shape == dst.shape, "a state that goes to a tensor of another type or shape"
-        assert src.shape[0] == n_req * beams, "a state of another number of rows than beams"
-        assert used is None or src.dim() >= 2, "a state without positions"
-        rows, n = max(src.shape[0], 1), src.numel() * src.element_size()
-        a.src, a.dst, a.row_bytes = _ptr(src), _ptr(dst), n // rows
-        a.unit_bytes = 0 if used is None else n // (rows * max(src.shape[1], 1))
+    rows, vals = n_req * beams, []
+    for src, dst in states:
+        shape = src.shape
+        assert src.dtype is dst.dtype and shape == dst.shape, "a state that goes to a tensor of another type or shape"
+        assert shape[0] == rows, "a state of another number of rows than beams"
+        assert src.is_contiguous() and dst.is_contiguous(), "tensors must be contiguous"
+        row = src.nbytes // rows if rows else 0
+        unit = 0
+        if used is not None:
+            assert len(shape) >= 2, "a state without positions"
+            unit = row // (shape[1] or 1)
+        vals += (src.data_ptr(), dst.data_ptr(), row, unit)
+    arr = ctypes.cast((ctypes.c_int64 * max(len(vals), 4))(*vals), ctypes.POINTER(BeamState))
     assert parent.dtype is _torch_types["int32"] and parent.dim() == 2 and parent.shape[0] == n_req and parent.shape[1] >= beams, \
         "parents other than int32 [n_req, beams]"
     assert parent.shape[1] <= 1 or parent.stride(1) == 1, "rows of parents must be contiguous"

@@ -19,7 +19,8 @@ using namespace rows;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPart = 8192;               // elements of a row to a workgroup
+constexpr int kPart = 8192;               // elements of a row that a workgroup works on at a time
+constexpr int kPackets = 128;             // 16 bytes each of a part's logits that may hold one of the best
 constexpr int kList = 512;                // of a part's logits, or a request's continuations, that may be among the best
 
 // 16 bytes of a row that may begin at any element.
@@ -55,24 +56,29 @@ __device__ __forceinline__ uint32_t reached_by(uint32_t order, int32_t k)
 __device__ __forceinline__ bool looked_at(float score, const int32_t* done, size_t row) { return score > -INFINITY && !(done && done[row] != 0); }
 
 // Part blockIdx.x % parts of row blockIdx.x / parts: keys [n] (0: none left) in order, {max, sum exp(z - max)}.
-// 64 groups of four threads have a maximum each; the n-th largest of these has at least n logits at or above it, which go on a list and find
-// their place there by counting who is larger.  Parts with more of them than the list holds (equal logits) take the largest n times over.
+// 64 groups of four threads have a maximum each; what the n-th largest of these (or a little less) reaches, n logits at least, goes on a list and
+// finds its place there by counting who is larger.  Parts with more of them than the list holds (equal logits) take the largest n times over.
 template <typename E>
 __global__ __launch_bounds__(kThreads)
 void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* __restrict__ score, const int32_t* __restrict__ done, int32_t parts,
-                      uint64_t* __restrict__ keys, float2* __restrict__ sums)
+                      bool at_once, uint64_t* __restrict__ keys, float2* __restrict__ sums)
 {
     constexpr int N = Packet<E>::N, U = kPart / (kThreads * N), W = kThreads / 64;
     __shared__ uint64_t list[kList];
     __shared__ float group_max[64];
     __shared__ Stat stat[W];
-    __shared__ int32_t count;
-    const int32_t row = int32_t(blockIdx.x) / parts, part = int32_t(blockIdx.x) - row * parts;
-    if (!looked_at(score[row], done, size_t(row))) return;
-    const int32_t tid = threadIdx.x, lane = tid & 63, base = part * kPart, n = sh.n_out;
-    const int32_t len = min(kPart, sh.V - base);
+    __shared__ u32x4 packet[kPackets];
+    __shared__ int32_t packet_at[kPackets], packets, count;
+    const int32_t tid = threadIdx.x, lane = tid & 63, n = sh.n_out;
+    const int32_t row = int32_t(blockIdx.x) / parts, base = (int32_t(blockIdx.x) - row * parts) * kPart, len = min(kPart, sh.V - base);
+    // (at_once: the logits are fetched before it is known whether they are looked at, a round trip less; many parts find out first)
+    if (!at_once && !looked_at(score[row], done, size_t(row))) return;
     const E* p = logits + size_t(row) * size_t(sh.ld) + base;
     u32x4 q[U];
+    if (len == kPart) {                              // (uniform)
+#pragma unroll
+        for (int c = 0; c < U; ++c) q[c] = *reinterpret_cast<const typename Loose<E>::type*>(p + (c * kThreads + tid) * N);
+    } else
 #pragma unroll
     for (int c = 0; c < U; ++c) {
         const int32_t at = (c * kThreads + tid) * N;
@@ -85,21 +91,24 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
                 if (at + e < len) put<E>(q[c], e, p[at + e]);
         }
     }
-    if (tid == 0) count = 0;
-    Stat a{-INFINITY, 0.f, 0.f};
+    if (at_once && !looked_at(score[row], done, size_t(row))) return;
+    if (tid == 0) count = packets = 0;
+    // (widened twice, so that 32 elements wait in 16 registers: twice the workgroups on a compute unit)
     float most[U];                                   // of each packet
-    {
-        float z[U * N];
+    Stat a{-INFINITY, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < U; ++c) {
+    for (int c = 0; c < U; ++c) {
+        most[c] = Packet<E>::element(q[c], 0);
 #pragma unroll
-            for (int e = 0; e < N; ++e) z[c * N + e] = Packet<E>::element(q[c], e);
-            most[c] = z[c * N];
-#pragma unroll
-            for (int e = 1; e < N; ++e) most[c] = fmaxf(most[c], z[c * N + e]);
-        }
-        take<false>(a, z, kLog2e);
+        for (int e = 1; e < N; ++e) most[c] = fmaxf(most[c], Packet<E>::element(q[c], e));
+        a.m = fmaxf(a.m, most[c]);
+        asm volatile("" : "+v"(q[c]));
     }
+    const float ref = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+    for (int c = 0; c < U; ++c)
+#pragma unroll
+        for (int e = 0; e < N; ++e) a.s += exp2_fast((Packet<E>::element(q[c], e) - ref) * kLog2e);
     const float mine = a.m;
     {
         float g = mine;
@@ -124,27 +133,26 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
         }
         sums[blockIdx.x] = make_float2(m, s);
     }
-    // packet by packet, of those in which any lane of the wave has one
+    // the packets that reach tau, then their elements, one a thread (looking through every thread's packets is four times the code)
 #pragma unroll
-    for (int c = 0; c < U; ++c) {
-        if (!(most[c] > -INFINITY && float_order(most[c]) >= tau)) continue;
-        uint32_t hits = 0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float z = Packet<E>::element(q[c], e);
-            hits |= z > -INFINITY && float_order(z) >= tau ? 1u << e : 0u;
+    for (int c = 0; c < U; ++c)
+        if (most[c] > -INFINITY && float_order(most[c]) >= tau) {
+            const int32_t o = atomicAdd(&packets, 1);
+            if (o < kPackets) packet[o] = q[c], packet_at[o] = (c * kThreads + tid) * N;
         }
-        for (; hits; hits &= hits - 1) {
-            const int e = __builtin_ctz(hits);
-            float z = 0.f;
-#pragma unroll
-            for (int i = 0; i < N; ++i) z = i == e ? Packet<E>::element(q[c], i) : z;
-            const int32_t o = atomicAdd(&count, 1);
-            if (o < kList) list[o] = order_key(z, base + (c * kThreads + tid) * N + e);
-        }
-    }
     __syncthreads();
-    const int32_t found = count;
+    const int32_t some = packets;
+    if (some <= kPackets)
+        for (int32_t i = tid; i < some * N; i += kThreads) {
+            const uint32_t w = reinterpret_cast<const uint32_t*>(packet)[sizeof(E) == 4 ? i : i >> 1];
+            const float z = __uint_as_float(sizeof(E) == 4 ? w : i & 1 ? w & 0xffff0000u : w << 16);
+            if (z > -INFINITY && float_order(z) >= tau) {
+                const int32_t o = atomicAdd(&count, 1);
+                if (o < kList) list[o] = order_key(z, base + packet_at[i / N] + i % N);
+            }
+        }
+    __syncthreads();
+    const int32_t found = some <= kPackets ? count : kList + 1;
     uint64_t* const out = keys + size_t(blockIdx.x) * n;
     if (found <= kList) {
         for (int32_t c = tid; c < found; c += kThreads) {
@@ -160,14 +168,12 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
     uint64_t last = ~uint64_t(0);
     for (int32_t r = 0; r < n; ++r) {
         uint64_t best = 0;
-#pragma unroll
-        for (int c = 0; c < U; ++c)
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float z = Packet<E>::element(q[c], e);
-                const uint64_t key = z > -INFINITY ? order_key(z, base + (c * kThreads + tid) * N + e) : 0;
-                best = key < last && key > best ? key : best;
-            }
+        // (from memory once more: from the registers they would all be keys there, and those are few)
+        for (int32_t i = tid; i < len; i += kThreads) {
+            const float z = element(p, i);
+            const uint64_t key = z > -INFINITY ? order_key(z, base + i) : 0;
+            best = key < last && key > best ? key : best;
+        }
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) {
             const uint64_t o = __shfl_xor((unsigned long long)best, x);
@@ -183,127 +189,135 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
     }
 }
 
-// A continuation: larger first, then the lower beam, then the lower token.
+// A continuation as two numbers: its value's order, and beam and token, the lower the better.
 struct Next {
-    double v;
-    int32_t beam, token;
+    uint64_t order, place;
+    __device__ __forceinline__ bool operator>(const Next& o) const { return order > o.order || (order == o.order && place < o.place); }
 };
-__device__ __forceinline__ bool in_front(const Next& a, const Next& b)
+__device__ __forceinline__ uint64_t double_order(double v)
 {
-    if (a.v != b.v) return a.v > b.v;
-    return a.beam != b.beam ? a.beam < b.beam : a.token < b.token;
+    const uint64_t b = uint64_t(__double_as_longlong(v + 0.));
+    return b >> 63 ? ~b : b | uint64_t(1) << 63;
+}
+__device__ __forceinline__ double order_value(uint64_t o)
+{
+    return __longlong_as_double((long long)(o >> 63 ? o & ~(uint64_t(1) << 63) : ~o));
 }
 
-// A workgroup per request.
+// A workgroup per request: 16 lanes per beam for its lse, then the continuations as the logits in a part, by the upper halves of their orders.
 __global__ __launch_bounds__(kThreads)
 void beam_merge_kernel(BeamShape sh, const float* score, const int32_t* __restrict__ done, int32_t done_token, int32_t parts,
                        const uint64_t* __restrict__ keys, const float2* __restrict__ sums, float* out_score, int32_t* __restrict__ out_beam,
                        int32_t* __restrict__ out_token)
 {
-    constexpr int W = kThreads / 64;
-    __shared__ double offset[LOBRA_MAX_TOP];         // s - lse; -inf: no continuations
-    __shared__ int32_t kind[LOBRA_MAX_TOP];          // 0: none, 1: its logits, 2: done
+    constexpr int W = kThreads / 64, G = 16, H = 4;  // H: continuations that a thread keeps
+    __shared__ double offset[LOBRA_MAX_TOP];         // s - lse; of a beam that is done: s
+    __shared__ int32_t kind[LOBRA_MAX_TOP];          // 0: no continuations, 1: its logits, 2: done
     __shared__ Next list[kList];
     __shared__ uint32_t group_max[64];
     __shared__ int32_t count;
-    const int32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = sh.n_out;
+    const int32_t tid = threadIdx.x, lane = tid & 63, n = sh.n_out;
     const size_t row0 = size_t(blockIdx.x) * sh.beams;
-    for (int32_t b = wave; b < sh.beams; b += W) {   // a wave per beam
-        const float s = score[row0 + b];
-        if (!looked_at(s, done, row0 + b)) {
-            if (lane == 0) kind[b] = s > -INFINITY ? 2 : 0, offset[b] = double(s);
-            continue;
-        }
-        const float2* part = sums + (row0 + b) * parts;
-        float m = -INFINITY;
-        for (int32_t i = lane; i < parts; i += 64) m = fmaxf(m, part[i].x);
-        m = wave_max(m);
-        double sum = 0;
-        for (int32_t i = lane; i < parts; i += 64) {
-            const float2 v = part[i];
-            sum += v.y > 0.f ? double(v.y) * exp(double(v.x) - double(m)) : double(v.y);        // (NaN stays NaN)
-        }
-#pragma unroll
-        for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
-        const double l = double(m) + log(sum);
-        if (lane == 0) kind[b] = l > -INFINITY && l < INFINITY ? 1 : 0, offset[b] = double(s) - l;
-    }
-    if (tid == 0) count = 0;
-    __syncthreads();
     const int32_t per = parts * n, total = sh.beams * per;
     const uint64_t* const k0 = keys + row0 * per;
-    auto value = [&](int32_t i, Next& c) {           // continuation i, false: there is none
-        c.beam = i / per;
-        const int32_t j = i - c.beam * per;
-        if (kind[c.beam] != 1) {
-            c.v = offset[c.beam];
-            c.token = done_token;
-            return kind[c.beam] == 2 && j == 0;
+    uint64_t held[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) held[h] = tid + h * kThreads < total ? k0[tid + h * kThreads] : 0;       // (of beams without any: not looked at)
+    if (tid == 0) count = 0;
+    for (int32_t b = tid / G; b < sh.beams; b += kThreads / G) {
+        const float2* part = sums + (row0 + b) * parts;
+        const float s = score[row0 + b];
+        const bool logits = looked_at(s, done, row0 + b);
+        float2 v = tid % G < parts ? part[tid % G] : make_float2(-INFINITY, 0.f);        // (perhaps never written)
+        double l = 0.;
+        if (logits) {
+            float m = v.x;
+            for (int32_t i = tid % G + G; i < parts; i += G) m = fmaxf(m, part[i].x);
+#pragma unroll
+            for (int x = 1; x < G; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+            double sum = 0.;
+            for (int32_t i = tid % G; i < parts; i += G) {
+                if (i >= G) v = part[i];
+                sum += v.y > 0.f ? double(v.y) * exp(double(v.x) - double(m)) : double(v.y);        // (NaN stays NaN)
+            }
+#pragma unroll
+            for (int x = 1; x < G; x <<= 1) sum += __shfl_xor(sum, x);
+            l = double(m) + log(sum);
         }
-        const uint64_t key = k0[i];
-        c.v = offset[c.beam] + double(key_value(key));
-        c.token = key_index(key);
-        return key != 0;
-    };
-    // (as in a part: values by their order in fp32, rounded down, so that none is above what it stands for)
-    auto order = [](double v) { return float_order(__double2float_rd(v)); };
-    uint32_t best = 0;
-    for (int32_t i = tid; i < total; i += kThreads) {
-        Next c;
-        if (value(i, c)) best = max(best, order(c.v));
+        if (tid % G == 0) {
+            kind[b] = logits ? (l > -INFINITY && l < INFINITY ? 1 : 0) : s > -INFINITY ? 2 : 0;
+            offset[b] = double(s) - l;
+        }
     }
+    __syncthreads();
+    auto value = [&](int32_t i, uint64_t key) {      // continuation i; order 0: there is none
+        const int32_t beam = i / per, k = kind[beam];
+        const double o = offset[beam];
+        if (k == 1 && key != 0) return Next{double_order(o + double(key_value(key))), uint64_t(beam) << 32 | uint32_t(key_index(key))};
+        if (k == 2 && i == beam * per) return Next{double_order(o), uint64_t(beam) << 32 | uint32_t(done_token)};
+        return Next{0, 0};
+    };
+    Next mine[H];
+    uint32_t best = 0;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        const int32_t i = tid + h * kThreads;
+        mine[h] = i < total ? value(i, held[h]) : Next{0, 0};
+        best = max(best, uint32_t(mine[h].order >> 32));
+    }
+    for (int32_t i = tid + H * kThreads; i < total; i += kThreads) best = max(best, uint32_t(value(i, k0[i]).order >> 32));
     uint32_t g = best;
 #pragma unroll
     for (int x = 1; x < kThreads / 64; x <<= 1) g = max(g, uint32_t(__shfl_xor(int(g), x)));
     if (tid % (kThreads / 64) == 0) group_max[tid / (kThreads / 64)] = g;
     __syncthreads();
     const uint32_t tau = reached_by(group_max[lane], n);
-    if (best >= tau && best > 0)
-        for (int32_t i = tid; i < total; i += kThreads) {
-            Next c;
-            if (value(i, c) && order(c.v) >= tau) {
-                const int32_t o = atomicAdd(&count, 1);
-                if (o < kList) list[o] = c;
-            }
-        }
+    auto consider = [&](const Next& c) {
+        if (c.order == 0 || uint32_t(c.order >> 32) < tau) return;
+        const int32_t o = atomicAdd(&count, 1);
+        if (o < kList) list[o] = c;
+    };
+#pragma unroll
+    for (int h = 0; h < H; ++h) consider(mine[h]);
+    for (int32_t i = tid + H * kThreads; i < total; i += kThreads) consider(value(i, k0[i]));
     __syncthreads();
     const int32_t found = count;
     auto write = [&](int32_t place, const Next& c) {
         const size_t o = size_t(blockIdx.x) * n + place;
-        out_score[o] = float(c.v);
-        out_beam[o] = c.beam;
-        out_token[o] = c.token;
+        out_score[o] = c.order ? float(order_value(c.order)) : -INFINITY;
+        out_beam[o] = c.order ? int32_t(c.place >> 32) : -1;
+        out_token[o] = c.order ? int32_t(uint32_t(c.place)) : -1;
     };
-    const Next nobody{-INFINITY, -1, -1};
     if (found <= kList) {
         for (int32_t c = tid; c < found; c += kThreads) {
-            const Next mine = list[c];
+            const Next x = list[c];
             int32_t place = 0;
-            for (int32_t o = 0; o < found; ++o) place += in_front(list[o], mine) ? 1 : 0;
-            if (place < n) write(place, mine);
+#pragma unroll 8
+            for (int32_t o = 0; o < found; ++o) place += list[o] > x ? 1 : 0;
+            if (place < n) write(place, x);
         }
-        if (tid >= found && tid < n) write(tid, nobody);
+        if (tid >= found && tid < n) write(tid, Next{0, 0});
         return;
     }
-    // more of equal value than the list holds: the best n times over
-    Next last{INFINITY, -1, -1};
+    // more of nearly the same value than the list holds: the best n times over
+    Next last{~uint64_t(0), 0};
     for (int32_t r = 0; r < n; ++r) {
-        Next top = nobody;
+        Next top{0, 0};
         for (int32_t i = tid; i < total; i += kThreads) {
-            Next c;
-            if (value(i, c) && in_front(last, c) && (top.beam < 0 || in_front(c, top))) top = c;
+            const Next c = value(i, k0[i]);
+            if (c.order && last > c && c > top) top = c;
         }
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) {
-            const Next o{__shfl_xor(top.v, x), __shfl_xor(top.beam, x), __shfl_xor(top.token, x)};
-            if (o.beam >= 0 && (top.beam < 0 || in_front(o, top))) top = o;
+            const Next o{uint64_t(__shfl_xor((unsigned long long)top.order, x)), uint64_t(__shfl_xor((unsigned long long)top.place, x))};
+            if (o > top) top = o;
         }
         __syncthreads();
-        if (lane == 0) list[wave] = top;
+        if (lane == 0) list[tid / 64] = top;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < W; ++w)
-            if (list[w].beam >= 0 && (top.beam < 0 || in_front(list[w], top))) top = list[w];
+            if (list[w] > top) top = list[w];
         if (tid == 0) write(r, top);
         last = top;
     }
@@ -318,10 +332,11 @@ struct StateTable {
 };
 static_assert(sizeof(StateTable) + 64 <= 4096, "the arguments of a launch");
 
-// Units of type U; blockIdx = (columns of a row, request, tensor).  B: at least the beams.
-template <typename U, int B>
+// Units of type U; blockIdx = (256 units of a row, request, tensor).  B: at least the beams.  IN_PLACE: a thread has read all rows before it writes one;
+// else four at a time.
+template <typename U, int B, bool IN_PLACE>
 __global__ __launch_bounds__(256)
-void beam_reorder_kernel(StateTable tab, int32_t first_req, int32_t beams, const int32_t* __restrict__ parent, int64_t parent_ld,
+void beam_reorder_kernel(StateTable tab, int64_t first_block, int32_t first_req, int32_t beams, const int32_t* __restrict__ parent, int64_t parent_ld,
                          const int32_t* __restrict__ used)
 {
     const int32_t s = blockIdx.z;
@@ -332,42 +347,61 @@ void beam_reorder_kernel(StateTable tab, int32_t first_req, int32_t beams, const
         const int64_t most = tab.unit[s] > 0 ? row / tab.unit[s] : 0;
         bytes = u < 0 ? 0 : u >= most ? row : u * tab.unit[s];
     }
+    const int64_t base = (first_block + blockIdx.x) * 256 * int64_t(sizeof(U)), left = bytes - base;
+    if (left <= 0) return;
     const int32_t* const from = parent + req * parent_ld;
-    int32_t of[B];
+    const char* const src = tab.src[s] + req * beams * row + base;
+    char* const dst = tab.dst[s] + req * beams * row + base;
+    // n bytes from `off` on, of every beam
+    auto move = [&](auto unit, uint32_t off) __attribute__((always_inline)) {
+        typedef decltype(unit) T;
+        if constexpr (IN_PLACE) {
+            T v[B];
 #pragma unroll
-    for (int i = 0; i < B; ++i) of[i] = i < beams ? from[i] : -1;
-    const bool in_place = tab.src[s] == tab.dst[s];
-    const char* const src = tab.src[s] + req * beams * row;
-    char* const dst = tab.dst[s] + req * beams * row;
-    for (int64_t at = (int64_t(blockIdx.x) * 256 + threadIdx.x) * int64_t(sizeof(U)); at < bytes; at += int64_t(gridDim.x) * 256 * int64_t(sizeof(U))) {
-        U v[B];
+            for (int i = 0; i < B; ++i) {
+                const int32_t of = i < beams ? from[i] : -1;
+                if (of >= 0 && of < beams && of != i) v[i] = *reinterpret_cast<const T*>(src + of * row + off);
+            }
 #pragma unroll
-        for (int i = 0; i < B; ++i)
-            if (of[i] >= 0 && of[i] < beams && !(in_place && of[i] == i)) v[i] = *reinterpret_cast<const U*>(src + of[i] * row + at);
+            for (int i = 0; i < B; ++i) {
+                const int32_t of = i < beams ? from[i] : -1;
+                if (of >= 0 && of < beams && of != i) *reinterpret_cast<T*>(dst + i * row + off) = v[i];
+            }
+        } else {
+            for (int32_t i0 = 0; i0 < beams; i0 += 4) {
+                T v[4];
 #pragma unroll
-        for (int i = 0; i < B; ++i) {
-            if (of[i] < 0 || of[i] >= beams || (in_place && of[i] == i)) continue;
-            if (sizeof(U) == 1 || at + int64_t(sizeof(U)) <= bytes) {
-                *reinterpret_cast<U*>(dst + i * row + at) = v[i];
-            } else {                                 // the end of what is used lies within the unit (a row itself is whole units)
-                const unsigned char* b = reinterpret_cast<const unsigned char*>(&v[i]);
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t of = i0 + i < beams ? from[i0 + i] : -1;
+                    if (of >= 0 && of < beams) v[i] = *reinterpret_cast<const T*>(src + of * row + off);
+                }
 #pragma unroll
-                for (int e = 0; e < int(sizeof(U)); ++e)
-                    if (at + e < bytes) dst[i * row + at + e] = char(b[e]);
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t of = i0 + i < beams ? from[i0 + i] : -1;
+                    if (of >= 0 && of < beams) *reinterpret_cast<T*>(dst + (i0 + i) * row + off) = v[i];
+                }
             }
         }
+    };
+    const uint32_t mine = threadIdx.x * uint32_t(sizeof(U));
+    if (int64_t(mine) + int64_t(sizeof(U)) <= left) {
+        move(U{}, mine);
+    } else if (sizeof(U) > 1 && mine < left) {       // the end of what is used lies within the unit (a row itself is whole ones)
+#pragma unroll 1
+        for (uint32_t e = mine; e < left; ++e) move(uint8_t{}, e);
     }
 }
 
-template <typename U>
-hipError_t launch_reorder(const StateTable& tab, dim3 grid, int32_t first_req, int32_t beams, const int32_t* parent, int64_t parent_ld, const int32_t* used,
-                          hipStream_t st)
+template <typename U, bool IN_PLACE>
+hipError_t launch_reorder(const StateTable& tab, dim3 grid, int64_t first_block, int32_t first_req, int32_t beams, const int32_t* parent,
+                          int64_t parent_ld, const int32_t* used, hipStream_t st)
 {
-    if (beams <= 2) beam_reorder_kernel<U, 2><<<grid, 256, 0, st>>>(tab, first_req, beams, parent, parent_ld, used);
-    else if (beams <= 4) beam_reorder_kernel<U, 4><<<grid, 256, 0, st>>>(tab, first_req, beams, parent, parent_ld, used);
-    else if (beams <= 8) beam_reorder_kernel<U, 8><<<grid, 256, 0, st>>>(tab, first_req, beams, parent, parent_ld, used);
-    else if (beams <= 16) beam_reorder_kernel<U, 16><<<grid, 256, 0, st>>>(tab, first_req, beams, parent, parent_ld, used);
-    else beam_reorder_kernel<U, 32><<<grid, 256, 0, st>>>(tab, first_req, beams, parent, parent_ld, used);
+#define LOBRA_REORDER(B) beam_reorder_kernel<U, B, IN_PLACE><<<grid, 256, 0, st>>>(tab, first_block, first_req, beams, parent, parent_ld, used)
+    if (!IN_PLACE || beams <= 4) LOBRA_REORDER(4);
+    else if (beams <= 8) LOBRA_REORDER(IN_PLACE ? 8 : 4);
+    else if (beams <= 16) LOBRA_REORDER(IN_PLACE ? 16 : 4);
+    else LOBRA_REORDER(IN_PLACE ? 32 : 4);
+#undef LOBRA_REORDER
     return hipGetLastError();
 }
 
@@ -380,10 +414,11 @@ hipError_t beam_select(const BeamShape& s, const void* logits, const float* scor
 {
     const int32_t parts = beam_parts(s.V);
     const dim3 grid(uint32_t(s.n_req) * uint32_t(s.beams) * uint32_t(parts));
+    const bool at_once = grid.x <= 1024;
     if (s.dtype == LOBRA_F32)
-        beam_part_kernel<float><<<grid, kThreads, 0, st>>>(s, static_cast<const float*>(logits), score, done, parts, keys, reinterpret_cast<float2*>(sums));
+        beam_part_kernel<float><<<grid, kThreads, 0, st>>>(s, static_cast<const float*>(logits), score, done, parts, at_once, keys, reinterpret_cast<float2*>(sums));
     else
-        beam_part_kernel<uint16_t><<<grid, kThreads, 0, st>>>(s, static_cast<const uint16_t*>(logits), score, done, parts, keys, reinterpret_cast<float2*>(sums));
+        beam_part_kernel<uint16_t><<<grid, kThreads, 0, st>>>(s, static_cast<const uint16_t*>(logits), score, done, parts, at_once, keys, reinterpret_cast<float2*>(sums));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     beam_merge_kernel<<<dim3(uint32_t(s.n_req)), kThreads, 0, st>>>(s, score, done, done_token, parts, keys, reinterpret_cast<const float2*>(sums), out_score,
@@ -395,18 +430,20 @@ hipError_t beam_reorder(const lobra_beam_state* states, int32_t n_states, int32_
                         const int32_t* used, hipStream_t st)
 {
     for (int32_t i0 = 0; i0 < n_states;) {
-        // runs of tensors whose rows are whole units of the same size
+        // runs of tensors whose rows are whole units of the same size, all in place or none
         StateTable tab;
         int32_t n = 0;
         int64_t most = 0;
         uint64_t unit = 0;
+        bool in_place = false;
         for (; i0 < n_states && n < kStates; ++i0) {
             const lobra_beam_state& a = states[i0];
             const uint64_t bits = reinterpret_cast<uintptr_t>(a.src) | reinterpret_cast<uintptr_t>(a.dst) | uint64_t(a.row_bytes);
-            const uint64_t own = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
+            const uint64_t own = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : bits % 2 == 0 ? 2 : 1;
             if (a.row_bytes == 0) continue;
-            if (n > 0 && own != unit) break;
+            if (n > 0 && (own != unit || in_place != (a.src == a.dst))) break;
             unit = own;
+            in_place = a.src == a.dst;
             tab.src[n] = static_cast<const char*>(a.src);
             tab.dst[n] = static_cast<char*>(a.dst);
             tab.row_bytes[n] = a.row_bytes;
@@ -415,17 +452,21 @@ hipError_t beam_reorder(const lobra_beam_state* states, int32_t n_states, int32_
             ++n;
         }
         if (n == 0) break;
-        const int64_t units = most / int64_t(unit);
-        constexpr int32_t kRequests = 32768;         // of a launch
-        for (int32_t r = 0; r < n_req; r += kRequests) {
-            const uint32_t reqs = uint32_t(n_req - r < kRequests ? n_req - r : kRequests);
-            // some 16 workgroups per compute unit and no more: what is left of a row they take in strides
-            const int64_t all = (units + 255) / 256, wanted = int64_t(4096) / (int64_t(reqs) * n) + 1;
-            const dim3 grid(uint32_t(all < wanted ? all : wanted), reqs, uint32_t(n));
-            const hipError_t e = unit == 16 ? launch_reorder<u32x4>(tab, grid, r, beams, parent, parent_ld, used, st)
-                                 : unit == 4 ? launch_reorder<uint32_t>(tab, grid, r, beams, parent, parent_ld, used, st)
-                                             : launch_reorder<uint8_t>(tab, grid, r, beams, parent, parent_ld, used, st);
-            if (e != hipSuccess) return e;
+        // (a launch holds less than 2^32 threads)
+        const int64_t all = (most / int64_t(unit) + 255) / 256;
+        constexpr int64_t kBlocks = 1 << 17, kWorkgroups = 1 << 23;
+        for (int64_t b = 0; b < all; b += kBlocks) {
+            const int64_t blocks = all - b < kBlocks ? all - b : kBlocks, fit = kWorkgroups / (blocks * n), step = fit < 1 ? 1 : fit < 32768 ? fit : 32768;
+            for (int64_t r = 0; r < n_req; r += step) {
+                const dim3 grid(uint32_t(blocks), uint32_t(n_req - r < step ? n_req - r : step), uint32_t(n));
+                const auto go = [&](auto u) {
+                    typedef decltype(u) U;
+                    return in_place ? launch_reorder<U, true>(tab, grid, b, int32_t(r), beams, parent, parent_ld, used, st)
+                                    : launch_reorder<U, false>(tab, grid, b, int32_t(r), beams, parent, parent_ld, used, st);
+                };
+                const hipError_t e = unit == 16 ? go(u32x4{}) : unit == 4 ? go(uint32_t{}) : unit == 2 ? go(uint16_t{}) : go(uint8_t{});
+                if (e != hipSuccess) return e;
+            }
         }
     }
     return hipSuccess;
