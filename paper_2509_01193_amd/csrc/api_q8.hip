@@ -24,6 +24,7 @@ lobra_status q8_plan(const Plan& p)
 struct Q8Product {
     int32_t K, N, launches, proj;        // K in pairs; the first projection, or -1: all
     GemmChoice choice;
+    bool beside = false;                 // the projection of x runs in the product's launch
 };
 Q8Product q8_product(const Plan& p)
 {
@@ -34,6 +35,11 @@ Q8Product q8_product(const Plan& p)
     if (p.n_proj > 1) {
         const Q8Product each{K, p.dg, p.n_proj, 0, choose(p.dg, 0)};
         if (one.choice.tile < 0 || float(p.n_proj) * (each.choice.cost + 3.f) < one.choice.cost) return each;
+    } else if (adapters) {
+        int32_t halves = 1;
+        for (const TokenBlock& b : p.tb) halves = std::max(halves, (b.nrows + 15) / 16);
+        const GemmChoice c = choose_q8_beside(p.desc.T, K, p.desc.d_out, nseg, p.r_max, int64_t(p.tb.size()), halves, p.desc.d_in);
+        if (c.tile >= 0) one.choice = c, one.beside = true;
     }
     return one;
 }
@@ -47,7 +53,7 @@ Q8Layout q8_layout(const Plan& p, const Q8Product& g, bool h_saved)
     Q8Layout l;
     l.scale = align256(size_t(p.desc.T) * size_t(q8_pitch(p.desc.d_in)));
     l.part = l.scale + align256(size_t(p.desc.T) * sizeof(float));
-    l.h = l.part + (g.choice.splits > 1 ? align256(size_t(g.choice.splits + 1) * size_t(p.desc.T) * size_t(g.N) * sizeof(float)) : 0);
+    l.h = l.part + (g.choice.splits > 1 || g.beside ? align256(size_t(g.choice.splits + 1) * size_t(p.desc.T) * size_t(g.N) * sizeof(float)) : 0);
     l.total = l.h + (h_saved || p.tb.empty() ? 0 : p.p_layout.total);
     return l;
 }
@@ -104,6 +110,12 @@ lobra_status lobra_mlora_quant_fwd(const lobra_mlora_plan* plan, const void* x, 
     float* const part = reinterpret_cast<float*>(wsb + l.part);
     char* const hb = h_save ? static_cast<char*>(h_save) : wsb + l.h;
     LOBRA_LAUNCH(p, st, LOBRA_K_QUANT, q8_rows(p.desc.T, pd.d_in, x, wsb, x_scale, st));
+    if (g.beside) {
+        LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK_GEMM,
+                     gemm_tile_q8_beside(pd, g.choice, wsb, x_scale, Wq, w_scale, x, A, s, hb + p.p_layout.p_tok, hb + p.p_layout.p_blk, B, y, g.K, g.N,
+                                         p.has_row_table(), st, part));
+        return LOBRA_OK;
+    }
     if (adapters)
         LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK, shrink_mfma(pd, x, A, s, hb + p.p_layout.p_tok, hb + p.p_layout.p_blk, pd.d_in, pd.d_in, 1, 0, st));
     const char* const P = adapters ? hb + p.p_layout.p_tok : nullptr;

@@ -361,6 +361,8 @@ void beam_reorder_kernel(StateTable tab, int64_t first_block, int32_t first_req,
             for (int i = 0; i < B; ++i) {
                 const int32_t of = i < beams ? from[i] : -1;
                 if (of >= 0 && of < beams && of != i) v[i] = *reinterpret_cast<const T*>(src + of * row + off);
+                // (a join the optimiser cannot see through: it made a path of its own of every combination of rows that move, 222 registers for eight)
+                if constexpr (sizeof(T) >= 4) asm volatile("" : "+v"(v[i]));
             }
 #pragma unroll
             for (int i = 0; i < B; ++i) {

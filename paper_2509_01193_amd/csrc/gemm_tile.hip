@@ -48,6 +48,7 @@ using namespace gemm;
 #ifndef LOBRA_GT_Q8
 #define LOBRA_GT_Q8 0
 #define LOBRA_GT_KERNEL gemm_tile_kernel
+#define LOBRA_GT_BESIDE gemm_tile_beside_kernel
 #endif
 
 static_assert(kGemmKTile == BK && kGemmTiles[0].tm == BM && kGemmTiles[0].tn == BN, "the plan's choice is about these kernels");
@@ -626,8 +627,6 @@ void LOBRA_GT_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
     );
 }
 
-#if !LOBRA_GT_Q8
-
 // A split product and the rank-r projection of the same Z in one launch: the first pwgs workgroups (a multiple of eight, so that the
 // others keep their XCDs) project, rparts * 2 columns of items as in shrink_ring_kernel<1, 1, 1, 256>, the others multiply.
 // Neither needs the other; gemm_add_up_kernel brings them together.  Small batches are bound by launches and memory round trips: 40
@@ -636,22 +635,35 @@ void LOBRA_GT_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
 constexpr int kBesideLds = 80 * 1024;
 template <bool W_KN, int TM, int TN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(256, 2)
-void gemm_tile_beside_kernel(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t* __restrict__ W, int32_t K, int32_t N,
+void LOBRA_GT_BESIDE(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t* __restrict__ W, int32_t K, int32_t N,
                              int32_t ldw, int32_t tiles_m, int32_t tiles_n, int32_t GM, int32_t splits, float* __restrict__ part,
                              const uint16_t* __restrict__ D, const float* __restrict__ s, uint16_t* __restrict__ P_tok,
-                             uint16_t* __restrict__ P_blk, int32_t rparts, int32_t pwgs)
+                             uint16_t* __restrict__ P_blk, int32_t rparts, int32_t pwgs
+#if LOBRA_GT_Q8
+                             , const float* __restrict__ z_scale, const float* __restrict__ w_scale, const uint16_t* __restrict__ x, int32_t d_in
+#endif
+)
 {
+#if !LOBRA_GT_Q8
+    const uint16_t* const x = Z;
+    const int32_t d_in = K;
+#endif
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int32_t wg = int32_t(blockIdx.x);
     if (wg < pwgs) {
         if (wg < pd.ntb * 2 * rparts)
-            ring_item<1, 1, 1, 256, kBesideLds>(pd, Z, D, s, P_tok, P_blk, K, K, 1, 0, rparts, wg % pd.ntb, wg / pd.ntb, lds);
+            ring_item<1, 1, 1, 256, kBesideLds>(pd, x, D, s, P_tok, P_blk, d_in, d_in, 1, 0, rparts, wg % pd.ntb, wg / pd.ntb, lds);
         return;
     }
     tile_body<W_KN, TM, TN, WM, WN, STAGES, 0>(pd, Z, W, nullptr, nullptr, nullptr, K, N, ldw, N, 1, 0, tiles_m, tiles_n, GM, splits, part,
-                                            wg - pwgs, lds);
+                                            wg - pwgs, lds
+#if LOBRA_GT_Q8
+                                            , z_scale, w_scale
+#endif
+    );
 }
 
+#if !LOBRA_GT_Q8
 // C = the splits' partial products, in split order, plus the adapter term P M_t, rounded once.  A wave has 256 columns of a row, so the
 // row's task and its projected activations are the same for all lanes; the rank rows go straight from memory into fp32 products, 16 of
 // them in flight.  (S splits as a template argument: under a condition of its own every load waited for the one before.)  What bounds it:
@@ -791,6 +803,55 @@ static hipError_t launch_tile(const PlanDev& pd, const void* Z, const void* W, c
     return hipGetLastError();
 }
 
+#if !LOBRA_GT_Q8
+hipError_t gemm_add_up(const PlanDev& pd, int32_t splits, const float* part, const void* P_tok, const void* M, void* C, int32_t N, bool row_table, hipStream_t st)
+{
+    with_splits<1, kMaxSplits>(splits, [&](auto s_c) {
+        const dim3 grid(uint32_t((pd.T + 3) / 4), uint32_t((N + 255) / 256));
+        (row_table ? gemm_add_up_kernel<decltype(s_c)::value, true> : gemm_add_up_kernel<decltype(s_c)::value, false>)<<<grid, 256, 0, st>>>(
+            pd, part, (const uint16_t*)P_tok, (const uint16_t*)M, (uint16_t*)C, N);
+    });
+    return hipGetLastError();
+}
+
+#endif
+
+template <bool W_KN, int TM, int TN, int WM, int WN, int STAGES>
+static hipError_t launch_beside(const PlanDev& pd, const void* Z, const void* W, const void* D, const float* s, void* P_tok, void* P_blk,
+                                const void* M, void* C, int32_t K, int32_t N, int32_t ldw, hipStream_t st, int32_t splits, float* part,
+                                [[maybe_unused]] const float* z_scale = nullptr, [[maybe_unused]] const float* w_scale = nullptr,
+                                [[maybe_unused]] const void* x = nullptr, [[maybe_unused]] bool row_table = true)
+{
+#if !LOBRA_GT_Q8
+    row_table = pd.T <= kRowTableTokens;             // (the plan has chosen this, and made the table)
+#endif
+    static_assert(WM * WN == 4 && ring_bytes<TM, TN, WN, STAGES>() + int(sizeof(TileTable<TM>)) <= kBesideLds, "two workgroups per compute unit");
+    // the kernel needs more dynamic LDS than the default limit: raise it once per device
+    static std::atomic<uint64_t> raised{0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = uint64_t(1) << (dev & 63);
+    if (!(raised.load(std::memory_order_acquire) & bit)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&LOBRA_GT_BESIDE<W_KN, TM, TN, WM, WN, STAGES>),
+                                hipFuncAttributeMaxDynamicSharedMemorySize, kBesideLds);
+        if (e != hipSuccess) return e;
+        raised.fetch_or(bit, std::memory_order_release);
+    }
+    const int32_t tiles_m = (pd.T + TM - 1) / TM, tiles_n = (N + TN - 1) / TN, rparts = (pd.r_max + 15) / 16;
+    const int32_t pwgs = (pd.ntb * 2 * rparts + 7) / 8 * 8;
+    LOBRA_GT_BESIDE<W_KN, TM, TN, WM, WN, STAGES><<<dim3(uint32_t(pwgs + tiles_m * tiles_n * splits)), 256, kBesideLds, st>>>(
+        pd, (const uint16_t*)Z, (const uint16_t*)W, K, N, ldw, tiles_m, tiles_n, 1024 / TM, splits, part, (const uint16_t*)D, s,
+        (uint16_t*)P_tok, (uint16_t*)P_blk, rparts, pwgs
+#if LOBRA_GT_Q8
+        , z_scale, w_scale, (const uint16_t*)x, pd.d_in
+#endif
+    );
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return gemm_add_up(pd, splits, part, P_tok, M, C, N, row_table, st);
+}
+
 #if LOBRA_GT_Q8
 hipError_t gemm_tile_q8(const PlanDev& pd, const GemmChoice& choice, const void* Z, const float* z_scale, const void* W, const float* w_scale, const void* P,
                         const void* M, void* C, int32_t K, int32_t N, int32_t ldc, int32_t nproj, int32_t proj, hipStream_t st, float* part)
@@ -808,39 +869,17 @@ hipError_t gemm_tile_q8(const PlanDev& pd, const GemmChoice& choice, const void*
     }
 #undef LOBRA_TILE
 }
-#else
-template <bool W_KN, int TM, int TN, int WM, int WN, int STAGES>
-static hipError_t launch_beside(const PlanDev& pd, const void* Z, const void* W, const void* D, const float* s, void* P_tok, void* P_blk,
-                                const void* M, void* C, int32_t K, int32_t N, int32_t ldw, hipStream_t st, int32_t splits, float* part)
-{
-    static_assert(WM * WN == 4 && ring_bytes<TM, TN, WN, STAGES>() + int(sizeof(TileTable<TM>)) <= kBesideLds, "two workgroups per compute unit");
-    // the kernel needs more dynamic LDS than the default limit: raise it once per device
-    static std::atomic<uint64_t> raised{0};
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    const uint64_t bit = uint64_t(1) << (dev & 63);
-    if (!(raised.load(std::memory_order_acquire) & bit)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_tile_beside_kernel<W_KN, TM, TN, WM, WN, STAGES>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, kBesideLds);
-        if (e != hipSuccess) return e;
-        raised.fetch_or(bit, std::memory_order_release);
-    }
-    const int32_t tiles_m = (pd.T + TM - 1) / TM, tiles_n = (N + TN - 1) / TN, rparts = (pd.r_max + 15) / 16;
-    const int32_t pwgs = (pd.ntb * 2 * rparts + 7) / 8 * 8;
-    gemm_tile_beside_kernel<W_KN, TM, TN, WM, WN, STAGES><<<dim3(uint32_t(pwgs + tiles_m * tiles_n * splits)), 256, kBesideLds, st>>>(
-        pd, (const uint16_t*)Z, (const uint16_t*)W, K, N, ldw, tiles_m, tiles_n, 1024 / TM, splits, part, (const uint16_t*)D, s,
-        (uint16_t*)P_tok, (uint16_t*)P_blk, rparts, pwgs);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    with_splits<1, kMaxSplits>(splits, [&](auto s_c) {
-        const dim3 grid(uint32_t((pd.T + 3) / 4), uint32_t((N + 255) / 256));
-        (pd.T <= kRowTableTokens ? gemm_add_up_kernel<decltype(s_c)::value, true> : gemm_add_up_kernel<decltype(s_c)::value, false>)<<<grid, 256, 0, st>>>(
-            pd, part, (const uint16_t*)P_tok, (const uint16_t*)M, (uint16_t*)C, N);
-    });
-    return hipGetLastError();
-}
 
+hipError_t gemm_tile_q8_beside(const PlanDev& pd, const GemmChoice& choice, const void* Z, const float* z_scale, const void* W, const float* w_scale,
+                               const void* x, const void* A, const float* s, void* P_tok, void* P_blk, const void* M, void* C, int32_t K, int32_t N,
+                               bool row_table, hipStream_t st, float* part)
+{
+    if (choice.tile < 0 || pd.T == 0 || pd.n_proj != 1 || !part) return hipErrorInvalidValue;
+#define LOBRA_BESIDE(...) launch_beside<false, __VA_ARGS__>(pd, Z, W, A, s, P_tok, P_blk, M, C, K, N, K, st, choice.splits, part, z_scale, w_scale, x, row_table)
+    return choice.tile == 3 ? LOBRA_BESIDE(128, 64, 2, 2, 3) : LOBRA_BESIDE(64, 64, 2, 2, 4);
+#undef LOBRA_BESIDE
+}
+#else
 hipError_t gemm_mfma_beside(const PlanDev& pd, const GemmChoice& choice, bool transW, const void* Z, const void* W, const void* D,
                             const float* s, void* P_tok, void* P_blk, const void* M, void* C, int32_t K, int32_t N, int32_t ldw,
                             hipStream_t st, float* part, size_t part_bytes)

@@ -79,6 +79,9 @@ hipError_t gemm_mfma(const PlanDev& pd, bool transW, const void* Z, const void* 
 hipError_t gemm_mfma_beside(const PlanDev& pd, const GemmChoice& choice, bool transW, const void* Z, const void* W, const void* D,
                             const float* s, void* P_tok, void* P_blk, const void* M, void* C, int32_t K, int32_t N, int32_t ldw,
                             hipStream_t st, float* part, size_t part_bytes);
+// What ends it: C = the sum of the splits' products in part, plus the adapter term P_tok M_t.  row_table: the plan has a table of rows (Plan::has_row_table).
+hipError_t gemm_add_up(const PlanDev& pd, int32_t splits, const float* part, const void* P_tok, const void* M, void* C, int32_t N, bool row_table,
+                       hipStream_t st);
 // The persistent direct-to-LDS kernel behind gemm_mfma for many output tiles (gemm_persistent.hip; T >= 256, N >= 256, K a
 // multiple of 128, or any multiple of 8 from kPersistentMinKTail on);
 // gm = tile rows per sweep of the tile order.  Everything else runs on the tiled kernels of gemm_tile.hip and the
@@ -109,6 +112,10 @@ hipError_t gemm_persistent_q8(const PlanDev& pd, const void* Z, const float* z_s
                               void* C, int32_t K, int32_t N, int32_t ldc, int32_t nproj, int32_t proj, hipStream_t st);
 hipError_t gemm_tile_q8(const PlanDev& pd, const GemmChoice& choice, const void* Z, const float* z_scale, const void* W, const float* w_scale,
                         const void* P, const void* M, void* C, int32_t K, int32_t N, int32_t ldc, int32_t nproj, int32_t proj, hipStream_t st, float* part);
+// With the projection of x [T][d_in] by A in the product's launch, as gemm_mfma_beside.
+hipError_t gemm_tile_q8_beside(const PlanDev& pd, const GemmChoice& choice, const void* Z, const float* z_scale, const void* W, const float* w_scale,
+                               const void* x, const void* A, const float* s, void* P_tok, void* P_blk, const void* M, void* C, int32_t K, int32_t N,
+                               bool row_table, hipStream_t st, float* part);
 bool gemm_mfma_shape_ok(int64_t T, int32_t K, int32_t N, int32_t ldw);
 // P = s_t Z M_t^T in bf16, written token-major [T][r_pad] and block-transposed [ntb][r_pad][32].
 // (ldz: row pitch of Z; nproj > 1: projection `proj` of a fused call - rank window, see the kernel; proj < 0: all of

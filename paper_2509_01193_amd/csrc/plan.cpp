@@ -491,8 +491,31 @@ GemmChoice choose_q8(int64_t T, int32_t K, int32_t N, int32_t group, int32_t nse
             const int64_t bytes = int64_t(s + 1) * T * N * 4;      // (one more for the adapter term)
             if (s > 1 && (i == kPersistentTile || kt < 4 * s || tiles * s > slots || uint64_t(bytes) > part_bytes)) break;
             float cost = rounds_cost(t, tiles * s, (kt + s - 1) / s, fixed) + t.once;
-            if (s > 1) cost += 3.f + float(bytes) / 3e6f;
+            // (the adapter term's workgroups take their time whatever the others do)
+            if (s > 1) cost = std::max(cost, nseg > 0 ? 7.5f : 0.f) + 3.f + float(s - 1) + float(bytes) / 3e6f;
             if (least < 0.f || cost < least) best = GemmChoice{i, s, cost}, least = cost;
+        }
+    }
+    return best;
+}
+
+GemmChoice choose_q8_beside(int64_t T, int32_t K, int32_t N, int32_t nseg, int32_t rank, int64_t ntb, int32_t halves, int32_t d_in)
+{
+    GemmChoice best;
+    const int64_t items = ntb * ((rank + 15) / 16);
+    if (ntb == 0 || items > kMaxBesideItems || T * N * rank > kMaxBesideRankRows) return best;
+    const int32_t kt = K / kGemmKTile;
+    float least = choose_q8(T, K, N, 0, nseg, kMaxPartBytes).cost + beside_gain(d_in);
+    for (int32_t i = 3; i <= 4; ++i) {
+        const GemmTile& t = kQ8Tiles[i];
+        const int64_t tiles = (T + t.tm - 1) / t.tm * ((N + t.tn - 1) / t.tn);
+        for (int32_t s = 1; s <= kMaxSplits; ++s) {
+            const int64_t bytes = int64_t(s) * T * N * 4;
+            if (tiles * s + items * halves > cus * t.per_cu || uint64_t(bytes) > kMaxPartBytes || (s > 1 && kt < 4 * s)) break;
+            // (the launch takes as long as its projection, and what a further split saves the sum behind it takes back in part)
+            const float product = rounds_cost(t, tiles * s + items, (kt + s - 1) / s, t.fixed), projection = 3.8f + 0.9f * float(d_in) / 1024.f;
+            const float cost = std::max(product, projection) + 3.f + 1.7f * float(s - 1) + float(bytes) / 3e6f;
+            if (cost < least) best = GemmChoice{i, s, cost}, least = cost;
         }
     }
     return best;
@@ -597,7 +620,7 @@ std::vector<int32_t> product_tables(const Plan& p)
         list[at + nseg + k] = p.rank_off[t + 1] - p.rank_off[t];
     }
     // and, where the sum of a split product adds the adapter term, the same for every row (see row_rank)
-    if ((p.beside_fwd.tile >= 0 || p.beside_bwd.tile >= 0) && p.desc.T <= kRowTableTokens)
+    if (p.has_row_table())
         for (size_t k = 0; k < nseg; ++k)
             for (int32_t i = p.cseg_off[k]; i < p.cseg_off[k + 1]; ++i) list.insert(list.end(), {list[at + k], list[at + nseg + k]});
     return list;

@@ -122,15 +122,32 @@ struct GemmChoice { int32_t tile = -1, splits = 1; float cost = -1.f; };    // t
 // The choice for C [T, N] = Z [T, K] op(W) given part_bytes of scratch.  group > 0: no tile may straddle a multiple of
 // `group` columns (a multiple of 64).  nseg: segments of the batch (0: no adapter); rank: the widest rank window.
 GemmChoice choose_gemm(int64_t T, int32_t K, int32_t N, int32_t group, int32_t nseg, int32_t rank, size_t part_bytes);
-// The same for a base in 8-bit integers, K in units of two of them (a multiple of 128): what a K tile costs there (gemm_persistent_q8.hip, gemm_tile_q8.hip).
+// The same for a base in 8-bit integers, K in units of two of them (a multiple of 128): what a K tile, 128 of them, costs there (gemm_persistent_q8.hip,
+// gemm_tile_q8.hip).  Measured, us, four tasks of rank 16 in segments of 400:
+//     T x K x N             256 x 256   128 x 256   128 x 128   128 x 64   64 x 64
+//     200 x 4096 x 4096                 28.2        21.4        17.5       14.1
+//     500 x 4096 x 4096     45.1        28.9        22.4        19.3       19.5
+//     1000 x 4096 x 4096    45.2        29.9        24.2        26.6       32.1
+//     2000 x 4096 x 4096    46.5        35.1        42.8        45.6       57.0
+//     4096 x 4096 x 4096    56.7        64.4        79.3        83.5       107
+//     777 x 4096 x 11008    50.6        58.3        58.8        54.3       61.5
+//     2999 x 1376 x 4096    28.0        32.3        37.4        34.5       47.0
+//     3000 x 11008 x 4096   111         131         129         157        221
+//     16384 x 1024 x 1024   27.5        30.3        44.8        38.8       54.5
+//     600 x 512 x 8192      18.0        13.4        20.5        16.5       19.8
+// and 40 one-token segments x 4096 x 4096, 64 x 64: one split 15.2, two 12.6, four 13.9, eight 17.7.
 constexpr GemmTile kQ8Tiles[] = {
-    {256, 256, 1, 1.35f, 0.f, 5.f, 7.f},
-    {128, 256, 1, 0.86f, 0.f, 6.5f, 0.f},
-    {128, 128, 1, 0.48f, 0.f, 7.f, 0.f},
-    {128, 64, 2, 0.36f, 0.59f, 7.f, 0.f},
-    {64, 64, 2, 0.23f, 0.39f, 6.f, 0.f},
+    {256, 256, 1, 1.13f, 0.f, 15.f, 0.f},
+    {128, 256, 1, 0.70f, 0.f, 10.f, 0.f},
+    {128, 128, 1, 0.43f, 0.f, 7.5f, 0.f},
+    {128, 64, 2, 0.36f, 0.53f, 5.5f, 0.f},
+    {64, 64, 2, 0.31f, 0.38f, 4.f, 0.f},
 };
 GemmChoice choose_q8(int64_t T, int32_t K, int32_t N, int32_t group, int32_t nseg, size_t part_bytes);
+// As choose_beside; d_in: the projection's K.  us, apart / beside with 1, 2, 3, 4, 8 splits of 64 x 64: one token x 4096 x 4096 19.8 / 15.4, 12.8, 13.3, 13.1, 13.5; 40
+// of them 28.3 / 16.6, 14.6, 15.7, 15.9, 17.2; 100 32.3 / 18.9, 17.3, 18.3, 20.6; 8 x 1376 x 4096 17.2 / 11.5, 10.6, 10.6, 10.7, 11.5; 8 x 8192 x 1024 at rank 64 27.9 /
+// 25.5, 21.4, 21.5, 21.6, 21.5; 40 x 4096 x 11008 28.4 / 19.6, 20.5, 22.9, 22.6.
+GemmChoice choose_q8_beside(int64_t T, int32_t K, int32_t N, int32_t nseg, int32_t rank, int64_t ntb, int32_t halves, int32_t d_in);
 // The same where the projection runs in the product's launch and the adapter term comes with the sum of the splits, of which there may
 // be one (gemm_mfma_beside; ntb: token blocks; halves: 2 if one has more than 16 tokens, else 1): tile -1 where a projection of its own is better.  Given kMaxPartBytes of scratch.
 // Forward passes, a projection of its own / beside the product, us (K x N, rank, n one-token requests or tokens of segments of m):
@@ -177,6 +194,8 @@ struct Plan {
     lobra_mlora_desc desc{};            // table pointers point into the vectors below
     uint32_t flags = 0;
     bool mfma = false;                  // bf16 storage and MFMA kernels
+    // whether the device image has the table of rows (row_rank in device_common.h)
+    bool has_row_table() const { return (beside_fwd.tile >= 0 || beside_bwd.tile >= 0) && desc.T <= kRowTableTokens; }
     int32_t r_max = 0, r_pad = 0, R_tot = 0;
     int32_t n_proj = 1;                 // shared-input projections fused into the call
     int32_t dg = 0;                     // d_out / n_proj: width of B and dB

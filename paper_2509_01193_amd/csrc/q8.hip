@@ -24,115 +24,129 @@ __device__ __forceinline__ Quantiser quantiser(float amax)       // amax: finite
     return z;
 }
 
-// q of N values at a time, as floats
-template <int N> __device__ __forceinline__ void quantise(const Quantiser& z, const float (&v)[N], float (&q)[N])
+// q of N values at a time, as bytes.  A product plus 1.5 x 2^23 is the nearest whole number (halves to the even one) in the lowest bits of a float.
+template <int N> __device__ __forceinline__ void quantise(const Quantiser& z, const float (&v)[N], uint32_t (&b)[N / 4])
 {
-    float far = 0.f;
+    constexpr float kWhole = 12582912.f;
+    float t[N], far = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float t = v[i] * z.inv;
-        q[i] = rintf(t);
-        far = fmaxf(far, fabsf(t - q[i]));
+        t[i] = fmaf(v[i], z.inv, kWhole);
+        far = fmaxf(far, fabsf(fmaf(v[i], z.inv, kWhole - t[i])));
     }
     if (far > 0.4999f) {                             // (a packet in some hundreds)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float r = fmaf(-q[i], z.scale, v[i]), over = fabsf(r) - 0.5f * z.scale;
-            if (over > 0.f || (over == 0.f && (int32_t(q[i]) & 1))) q[i] += copysignf(1.f, r);
+            const float q = t[i] - kWhole, r = fmaf(-q, z.scale, v[i]), over = fabsf(r) - 0.5f * z.scale;
+            if (over > 0.f || (over == 0.f && (int32_t(q) & 1))) t[i] += copysignf(1.f, r);
         }
     }
-}
-
-template <int N> __device__ __forceinline__ void to_bytes(const float (&q)[N], uint32_t (&b)[N / 4])
-{
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-        b[i] = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) b[i] |= (uint32_t(int32_t(q[4 * i + e])) & 255u) << (8 * e);
+        const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(t[4 * i + 1]), __float_as_uint(t[4 * i]), 0x0c0c0400u),
+                       hi = __builtin_amdgcn_perm(__float_as_uint(t[4 * i + 3]), __float_as_uint(t[4 * i + 2]), 0x04000c0cu);
+        b[i] = lo | hi;
     }
 }
 
-constexpr int kHeld = 16;                            // packets a lane keeps of its row: 8192 elements
-
-// The largest magnitude of eight bf16, as bits (NaN and infinity: 0x7f80 and above), joined with m.
-__device__ __forceinline__ uint32_t amax_bits(u32x4 p, uint32_t m)
+// The largest magnitude of eight bf16 as bits, two in a word (NaN and infinity: 0x7f80 and above), joined with m.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 amax_bits(u32x4 p, u16x2 m)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m = max(m, max(p[i] & 0x7fffu, p[i] >> 16 & 0x7fffu));
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, p[i] & 0x7fff7fffu));
     return m;
+}
+// (NaN counts as infinity: a maximum would drop it)
+__device__ __forceinline__ float amax_value(u16x2 m)
+{
+    const uint32_t b = max(uint32_t(m[0]), uint32_t(m[1])) << 16;
+    return __uint_as_float(b > 0x7f800000u ? 0x7f800000u : b);
 }
 
 __device__ __forceinline__ void store_packet(const Quantiser& z, u32x4 p, bool finite, uint8_t* out)
 {
-    float v[8], q[8];
+    float v[8];
     uint32_t b[2] = {0u, 0u};
     if (finite) {
         Packet<uint16_t>::widen(p, v);
-        quantise<8>(z, v, q);
-        to_bytes<8>(q, b);
+        quantise<8>(z, v, b);
     }
     *reinterpret_cast<uint64_t*>(out) = uint64_t(b[1]) << 32 | b[0];
 }
 
-// A wave per row, whose packets stay in registers between the maximum and the quotients (rows beyond 8192 elements: what does not fit is
-// read again).  Bound: memory.
+// W waves per row, whose packets stay in registers between the maximum and the quotients, H a lane (what does not fit is read again).  Bound: memory,
+// and some six VALU instructions an element next to it; few rows: the round trip.
+template <int W, int H>
 __global__ __launch_bounds__(256) void q8_rows_kernel(int32_t T, int32_t d, int32_t pitch, const uint16_t* __restrict__ x, uint8_t* __restrict__ q,
                                                       float* __restrict__ scale)
 {
-    const int32_t row = int32_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(int32_t(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    if (row >= T) return;
+    __shared__ float part[4];
+    const int32_t wave = __builtin_amdgcn_readfirstlane(int32_t(threadIdx.x >> 6)), row = int32_t(blockIdx.x) * (4 / W) + wave / W;
+    if (W == 1 && row >= T) return;
+    constexpr int32_t step = 64 * W;
+    const int32_t t = int32_t(threadIdx.x) % step;
     const u32x4* p = reinterpret_cast<const u32x4*>(x + size_t(row) * d);
     uint8_t* out = q + size_t(row) * pitch;
     const int32_t packets = d / 8, all = pitch / 8;
     const u32x4 none = {0u, 0u, 0u, 0u};
-    u32x4 held[kHeld];
+    u32x4 held[H];
 #pragma unroll
-    for (int c = 0; c < kHeld; ++c) held[c] = lane + 64 * c < packets ? p[lane + 64 * c] : none;
-    uint32_t m = 0;
+    for (int c = 0; c < H; ++c) held[c] = t + step * c < packets ? p[t + step * c] : none;
+    u16x2 m = {0, 0};
 #pragma unroll
-    for (int c = 0; c < kHeld; ++c) m = amax_bits(held[c], m);
-    for (int32_t i = lane + 64 * kHeld; i < packets; i += 64) m = amax_bits(p[i], m);
-    const float amax = wave_max(__uint_as_float(m << 16 > 0x7f800000u ? 0x7f800000u : m << 16));       // (NaN counts as infinity: a maximum would drop it)
+    for (int c = 0; c < H; ++c) m = amax_bits(held[c], m);
+    for (int32_t i = t + step * H; i < packets; i += step) m = amax_bits(p[i], m);
+    float amax = wave_max(amax_value(m));
+    if constexpr (W > 1) {
+        static_assert(W == 4, "a row per workgroup");
+        if ((threadIdx.x & 63) == 0) part[wave] = amax;
+        __syncthreads();
+        amax = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+    }
     const bool finite = amax < INFINITY;
     const Quantiser z = quantiser(finite ? amax : 0.f);
 #pragma unroll
-    for (int c = 0; c < kHeld; ++c)
-        if (lane + 64 * c < all) store_packet(z, held[c], finite, out + 8 * (lane + 64 * c));
-    for (int32_t i = lane + 64 * kHeld; i < all; i += 64) store_packet(z, i < packets ? p[i] : none, finite, out + 8 * i);
-    if (lane == 0) scale[row] = finite ? z.scale : NAN;
+    for (int c = 0; c < H; ++c)
+        if (t + step * c < all) store_packet(z, held[c], finite, out + 8 * (t + step * c));
+    for (int32_t i = t + step * H; i < all; i += step) store_packet(z, i < packets ? p[i] : none, finite, out + 8 * i);
+    if (t == 0) scale[row] = finite ? z.scale : NAN;
 }
 
-// 64 columns per workgroup, a lane each; every wave has a quarter of each 64 rows, so that a lane's 16 values are 16 neighbouring bytes of its
-// column's row of q.  Done once per weight.
+// 64 columns per workgroup, a lane each; its 16 waves share the rows, 16 neighbouring ones at a time, so that a lane's 16 values are 16 neighbouring
+// bytes of its column's row of q.  Done once per weight.
+constexpr int kWeightWaves = 16;
 template <typename E>
-__global__ __launch_bounds__(256) void q8_weight_kernel(int32_t d_in, int32_t d_out, int32_t pitch, int64_t ldw, const E* __restrict__ W,
-                                                        uint8_t* __restrict__ q, float* __restrict__ scale)
+__global__ __launch_bounds__(64 * kWeightWaves) void q8_weight_kernel(int32_t d_in, int32_t d_out, int32_t pitch, int64_t ldw, const E* __restrict__ W,
+                                                                     uint8_t* __restrict__ q, float* __restrict__ scale)
 {
-    __shared__ float part[4][64];
+    __shared__ float part[kWeightWaves][64];
     const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t col = int64_t(blockIdx.x) * 64 + lane;
     const bool in = col < d_out;
     float m = 0.f;
-    if (in)
-        for (int32_t k = wave; k < d_in; k += 4) {
-            const float v = fabsf(Elem<E>::load(W, size_t(k) * ldw + col));
-            m = v < INFINITY ? fmaxf(m, v) : INFINITY;
-        }
+    auto rows = [&](int32_t k0, float (&v)[16]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = in && k0 + i < d_in ? Elem<E>::load(W, size_t(k0 + i) * ldw + col) : 0.f;
+    };
+    for (int32_t k0 = 16 * wave; k0 < d_in; k0 += 16 * kWeightWaves) {
+        float v[16];
+        rows(k0, v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m = fabsf(v[i]) < INFINITY ? fmaxf(m, fabsf(v[i])) : INFINITY;
+    }
     part[wave][lane] = m;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, part[w][lane]);
+    for (int w = 0; w < kWeightWaves; ++w) m = fmaxf(m, part[w][lane]);
     if (!in) return;
     const bool finite = m < INFINITY;
     const Quantiser z = quantiser(finite ? m : 0.f);
-    for (int32_t k0 = 16 * wave; k0 < pitch; k0 += 64) {
-        float v[16], r[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = finite && k0 + i < d_in ? Elem<E>::load(W, size_t(k0 + i) * ldw + col) : 0.f;
-        quantise<16>(z, v, r);
-        uint32_t b[4];
-        to_bytes<16>(r, b);
+    for (int32_t k0 = 16 * wave; k0 < pitch; k0 += 16 * kWeightWaves) {
+        float v[16];
+        uint32_t b[4] = {0u, 0u, 0u, 0u};
+        rows(k0, v);
+        if (finite) quantise<16>(z, v, b);
         *reinterpret_cast<u32x4*>(q + size_t(col) * pitch + k0) = u32x4{b[0], b[1], b[2], b[3]};
     }
     if (wave == 0) scale[col] = finite ? z.scale : NAN;
@@ -170,8 +184,14 @@ __global__ __launch_bounds__(256) void q8_dequantise_kernel(int32_t d_in, int32_
 
 hipError_t q8_rows(int64_t T, int32_t d, const void* x, void* q, float* scale, hipStream_t st)
 {
-    q8_rows_kernel<<<dim3(uint32_t((T + 3) / 4)), 256, 0, st>>>(int32_t(T), d, int32_t(q8_pitch(d)), static_cast<const uint16_t*>(x),
-                                                               static_cast<uint8_t*>(q), scale);
+    const int32_t pitch = int32_t(q8_pitch(d));
+    const auto go = [&](auto kernel, int32_t rows) {
+        kernel<<<dim3(uint32_t((T + rows - 1) / rows)), 256, 0, st>>>(int32_t(T), d, pitch, static_cast<const uint16_t*>(x), static_cast<uint8_t*>(q), scale);
+    };
+    // a wave per row where a workgroup has less than two packets a thread and there are enough rows (us, a row per wave / workgroup: 16384 x 256 12.6 /
+    // 20.6, x 1024 17.0 / 23.1, x 2048 22.3 / 28.0, x 4096 37.9 / 36.0, 8190 x 4096 23.4 / 21.8, 40 x 2048 6.9 / 6.1)
+    if (d <= 2048 && T > 1024) go(q8_rows_kernel<1, 8>, 4);
+    else d <= 8192 ? go(q8_rows_kernel<4, 4>, 1) : go(q8_rows_kernel<4, 8>, 1);
     return hipGetLastError();
 }
 
@@ -180,9 +200,9 @@ hipError_t q8_weight(int dtype, int32_t d_in, int32_t d_out, int64_t ldw, const 
     const dim3 grid(uint32_t((int64_t(d_out) + 63) / 64));
     const int32_t pitch = int32_t(q8_pitch(d_in));
     if (dtype == LOBRA_F32)
-        q8_weight_kernel<float><<<grid, 256, 0, st>>>(d_in, d_out, pitch, ldw, static_cast<const float*>(W), static_cast<uint8_t*>(q), scale);
+        q8_weight_kernel<float><<<grid, 64 * kWeightWaves, 0, st>>>(d_in, d_out, pitch, ldw, static_cast<const float*>(W), static_cast<uint8_t*>(q), scale);
     else
-        q8_weight_kernel<uint16_t><<<grid, 256, 0, st>>>(d_in, d_out, pitch, ldw, static_cast<const uint16_t*>(W), static_cast<uint8_t*>(q), scale);
+        q8_weight_kernel<uint16_t><<<grid, 64 * kWeightWaves, 0, st>>>(d_in, d_out, pitch, ldw, static_cast<const uint16_t*>(W), static_cast<uint8_t*>(q), scale);
     return hipGetLastError();
 }
 
