@@ -7,7 +7,11 @@ Embedding, base weights, head and the norms' gains are frozen; every task trains
 norm, so that no task's spike touches another's step.  A block's second norm, its gate, the residual and the next block's first norm are
 one call.  Attention is not part of it: the next token is learnt from the token alone.
 
+The base of the down projections and the head can be put into 8-bit integers (quantise_base); adapters on it learn from the likeliest tokens of
+another model, the one before for instance (teacher = ...), and prompts are continued by beam search (search).
+
     python -m paper_2509_01193_amd.joint_step --steps 30          # trains, then continues a prompt of every task token by token
+    python -m paper_2509_01193_amd.joint_step --steps 30 --distill-steps 10 --beams 4       # then an 8-bit base, distillation, beam search
 """
 import argparse
 import math
@@ -61,20 +65,58 @@ class JointStep:
             blk["dgate"] = torch.zeros(self.n_tasks, d, device=self.dev)
             grads.append((blk["dgate"], None, list(range(self.n_tasks + 1))))     # one row a task, as of rank 1
             self.blocks.append(blk)
+        self.head8 = None
         self.grads = lobra.GradSet(grads, self.n_tasks)
         self.norm, self.clip_scale = (torch.empty(self.n_tasks, device=self.dev) for _ in range(2))
         self.step_now = torch.empty_like(self.steps)
         self.batch(seg_off, seg_task)
 
+    def quantise_base(self):
+        """The frozen weights of the down projections and the head in 8-bit integers from here on; the others are not kept."""
+        def quantised(W):
+            d_in, d_out = W.shape
+            q = torch.empty(d_out, lobra.lobra_quant_pitch(d_in), dtype=torch.int8, device=self.dev), torch.empty(d_out, device=self.dev)
+            lobra.lobra_quantise_weight(W, *q)
+            return q
+
+        for blk in self.blocks:
+            blk["W_down8"] = quantised(blk.pop("W_down"))
+        self.head8, self.head = quantised(self.head), None
+        self.batch(*self.packing)
+
+    def restart(self):
+        """Adapters that add nothing yet, and gates, as at the beginning (the down factors stay)."""
+        for blk in self.blocks:
+            for k in ("A_gu", "B_gu", "A_down", "B_down"):
+                for what in ("m_", "v_") + (("master_", "") if k[0] == "B" else ()):
+                    blk[what + k].zero_()
+            blk["gate32"].fill_(0.5)
+            blk["gate"].copy_(blk["gate32"])
+        self.steps.zero_()
+
+    def _fwd(self, plan, x, W, W8, A, B, s, y, h_save):
+        if W8 is None:
+            lobra.lobra_mlora_plan_fwd(plan, x, W, A, B, s, y, h_save, self.ws)
+        else:
+            lobra.lobra_mlora_quant_fwd(plan, x, *W8, A, B, s, y, h_save, self.ws)
+
+    def _bwd(self, plan, x, W, W8, A, B, s, dy, h_saved, dx, dA, dB):
+        if W8 is None:
+            lobra.lobra_mlora_plan_bwd(plan, x, W, A, B, s, dy, h_saved, dx, dA, dB, 0, self.ws)
+        else:
+            lobra.lobra_mlora_quant_bwd(plan, x, *W8, A, B, s, dy, h_saved, dx, dA, dB, 0, self.ws)
+
     def batch(self, seg_off, seg_task, train=True):
         """Plans and buffers for another packing (train=False: of a serving step, which keeps nothing for backward)."""
         T, d, f, dev, edt = int(seg_off[-1]), self.d, self.f, self.dev, self.edt
-        self.T, self.train = T, train
+        self.T, self.train, self.packing = T, train, (seg_off, seg_task, train)
         self.p_gu = lobra.Plan(self.dtype, T, d, 2 * f, self.rank_off2, seg_off, seg_task, n_proj=2)
         self.p_down = lobra.Plan(self.dtype, T, f, d, self.rank_off, seg_off, seg_task)
         self.p_head = lobra.Plan(self.dtype, T, d, self.vocab, None, [0, T], [-1])
         plans = (self.p_gu, self.p_down, self.p_head)
         need = [p.fwd_ws_bytes for p in plans] + [lobra.lobra_mlora_gated_workspace_bytes(self.p_gu, train), 16]
+        if self.head8 is not None:
+            need += [n[k] for n in (lobra.lobra_mlora_quant_workspace_bytes(p) for p in (self.p_down, self.p_head)) for k in ((0, 1) if train else (0,))]
         if train:
             need += [p.bwd_ws_bytes for p in plans] + [self.grads.ws_bytes, lobra.lobra_mlora_block_norm_workspace_bytes(self.p_gu)]
         self.ws = torch.empty(max(need), dtype=torch.uint8, device=dev)
@@ -92,11 +134,24 @@ class JointStep:
         self.x_out = buf(T, d)
         self.logits = buf(T, self.vocab)
         self.logp, self.lse, self.lse_rest, self.entropy = (buf(T, dtype=torch.float32) for _ in range(4))
+        self.loss, self.stat = buf(T, dtype=torch.float32), buf(T, 4, dtype=torch.float32)
         if train:
             self.dr, self.dx, self.dh = buf(T, d), buf(T, d), buf(T, f)
 
-    def forward(self, tokens, target=None, top=None):
-        """logp [T] of target (int32 [T]; outside the vocabulary: not counted).  top = (logp [T, k], id [T, k]): receives the likeliest."""
+    def forward(self, tokens, target=None, top=None, teacher=None):
+        """logp [T] of target (int32 [T]; outside the vocabulary: not counted).  top = (logp [T, k], id [T, k]): receives the likeliest.
+        teacher = (logp [T, k], id [T, k]), another model's likeliest: the loss [T] against them instead, what they leave out as one more token."""
+        self.logits_of(tokens)
+        lo = lobra
+        if teacher is not None:
+            desc = lo.make_distill_desc(self.dtype, self.T, self.vocab, teacher[0].shape[1], tail=True)
+            lo.lobra_token_distill_fwd(desc, self.logits, *teacher, self.loss, self.stat)
+            return self.loss
+        desc = lo.make_logprob_desc(self.dtype, self.T, self.vocab, top_k=0 if top is None else top[0].shape[1])
+        lo.lobra_token_logprob_fwd(desc, self.logits, target, self.logp, self.lse, self.lse_rest, self.entropy, *(top or (None, None)))
+        return self.logp
+
+    def logits_of(self, tokens):
         lo = lobra
         r = self.embedding.index_select(0, tokens)
         for l, blk in enumerate(self.blocks):
@@ -105,21 +160,23 @@ class JointStep:
                 lo.lobra_mlora_block_norm_fwd(self.p_gu, self.cfg, r, None, None, None, self.gain, None, a["x"])
             x_next = self.x_out if l + 1 == self.layers else self.act[l + 1 if self.train else 0]["x"]
             lo.lobra_mlora_gated_fwd(self.p_gu, lo.ACT_SILU, a["x"], blk["W_gu"], blk["A_gu"], blk["B_gu"], self.s, a["gu"], a["h"], a["h_gu"], self.ws)
-            lo.lobra_mlora_plan_fwd(self.p_down, a["h"], blk["W_down"], blk["A_down"], blk["B_down"], self.s, a["b"], a["h_down"], self.ws)
+            self._fwd(self.p_down, a["h"], blk.get("W_down"), blk.get("W_down8"), blk["A_down"], blk["B_down"], self.s, a["b"], a["h_down"])
             lo.lobra_mlora_block_norm_fwd(self.p_gu, self.cfg, r, a["b"], self.gain, blk["gate"], self.gain, a["r"], x_next,
                                           a["rstd_post"], a["rstd_pre"])
             r = a["r"]
-        lo.lobra_mlora_plan_fwd(self.p_head, self.x_out, self.head, None, None, None, self.logits, None, self.ws)
-        desc = lo.make_logprob_desc(self.dtype, self.T, self.vocab, top_k=0 if top is None else top[0].shape[1])
-        lo.lobra_token_logprob_fwd(desc, self.logits, target, self.logp, self.lse, self.lse_rest, self.entropy, *(top or (None, None)))
-        return self.logp
+        self._fwd(self.p_head, self.x_out, self.head, self.head8, None, None, None, self.logits, None)
 
-    def backward(self, target, dlogp):
-        """Gradients of sum(dlogp * logp) into every block's dA_*, dB_*, dgate.  The logits' gradient takes the logits' place."""
+    def backward(self, target, dlogp, teacher=None):
+        """Gradients of sum(dlogp * logp), or with the teacher that forward had of sum(dlogp * loss), into every block's dA_*, dB_*, dgate.  The logits'
+        gradient takes the logits' place."""
         lo = lobra
-        desc = lo.make_logprob_desc(self.dtype, self.T, self.vocab)
-        lo.lobra_token_logprob_bwd(desc, self.logits, target, self.lse, self.lse_rest, None, dlogp, None, self.logits)
-        lo.lobra_mlora_plan_bwd(self.p_head, self.x_out, self.head, None, None, None, self.logits, None, self.dx, None, None, 0, self.ws)
+        if teacher is not None:
+            desc = lo.make_distill_desc(self.dtype, self.T, self.vocab, teacher[0].shape[1], tail=True)
+            lo.lobra_token_distill_bwd(desc, self.logits, *teacher, self.stat, dlogp, self.logits)
+        else:
+            desc = lo.make_logprob_desc(self.dtype, self.T, self.vocab)
+            lo.lobra_token_logprob_bwd(desc, self.logits, target, self.lse, self.lse_rest, None, dlogp, None, self.logits)
+        self._bwd(self.p_head, self.x_out, self.head, self.head8, None, None, None, self.logits, None, self.dx, None, None)
         dr = None
         for l in reversed(range(self.layers)):
             blk, a = self.blocks[l], self.act[l]
@@ -127,8 +184,8 @@ class JointStep:
             lo.lobra_mlora_block_norm_bwd(self.p_gu, self.cfg, a["r"], a["b"], self.gain, blk["gate"], self.gain, a["rstd_post"], a["rstd_pre"],
                                           dr, self.dx, self.dr, db, blk["dgate"], None, None, 0, self.ws)
             dr = self.dr
-            lo.lobra_mlora_plan_bwd(self.p_down, a["h"], blk["W_down"], blk["A_down"], blk["B_down"], self.s, db, a["h_down"], self.dh,
-                                    blk["dA_down"], blk["dB_down"], 0, self.ws)
+            self._bwd(self.p_down, a["h"], blk.get("W_down"), blk.get("W_down8"), blk["A_down"], blk["B_down"], self.s, db, a["h_down"], self.dh,
+                      blk["dA_down"], blk["dB_down"])
             lo.lobra_mlora_gated_bwd(self.p_gu, lo.ACT_SILU, a["x"], blk["W_gu"], blk["A_gu"], blk["B_gu"], self.s, a["gu"], self.dh, a["h_gu"],
                                      a["gu"], self.dx if l else None, blk["dA_gu"], blk["dB_gu"], 0 if l else lo.FLAG_NO_DX, self.ws)
 
@@ -149,6 +206,29 @@ class JointStep:
             blk["gate"].copy_(blk["gate32"])
 
 
+    def search(self, tokens, tasks, beams, new_tokens, end=-1):
+        """Beam search from one token per request: (scores [n, beams], tokens [n, beams, new_tokens]), the best first.  A beam that has come to the token
+        `end` is finished; what follows it is `end` again.  The batch is a serving one from here on."""
+        n, lo = len(tasks), lobra
+        self.batch([beams * i for i in range(n + 1)], tasks, train=False)
+        desc = lo.make_beam_desc(self.dtype, n, beams, self.vocab)
+        ws = torch.empty(lo.lobra_beam_workspace_bytes(desc), dtype=torch.uint8, device=self.dev)
+        score = torch.full((n, beams), -math.inf, device=self.dev)
+        score[:, 0] = 0.0                             # one beam to begin with
+        parent, token = (torch.empty(n, beams, dtype=torch.int32, device=self.dev) for _ in range(2))
+        seen = torch.zeros(n * beams, new_tokens, dtype=torch.int32, device=self.dev)
+        done = torch.zeros(n * beams, 1, dtype=torch.int32, device=self.dev)
+        now = tokens.repeat_interleave(beams)
+        for k in range(new_tokens):
+            self.logits_of(now)
+            lo.lobra_beam_select(desc, self.logits, score, done.view(n, beams), end, score, parent, token, ws)
+            lo.lobra_beam_reorder([(seen, seen), (done, done)], n, beams, parent)
+            seen[:, k] = token.view(-1)
+            done |= token.view(-1, 1) == end
+            now = token.view(-1).long().clamp(min=0)
+        return score, seen.view(n, beams, new_tokens)
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--dtype", choices=("bf16", "f32"), default="bf16")
@@ -160,6 +240,8 @@ def main(argv=None):
     ap.add_argument("--tokens", type=int, default=600, help="per task")
     ap.add_argument("--ranks", type=int, nargs="+", default=[8, 16, 8])
     ap.add_argument("--new-tokens", type=int, default=5)
+    ap.add_argument("--distill-steps", type=int, default=0, help="steps of new adapters on an 8-bit base, against the trained model's likeliest tokens")
+    ap.add_argument("--beams", type=int, default=0, help="continue the prompts by beam search")
     args = ap.parse_args(argv)
     n, T = len(args.ranks), len(args.ranks) * args.tokens
     gen = torch.Generator().manual_seed(1)
@@ -181,6 +263,24 @@ def main(argv=None):
         losses.append((-logp.view(n, args.tokens).mean(dim=1)).tolist())
         if k % 5 == 0 or k + 1 == args.steps:
             print("step %3d  losses %s  gradient norms %s" % (k, ["%.3f" % v for v in losses[-1]], ["%.3f" % v for v in step.norm.tolist()]), flush=True)
+    if args.distill_steps:
+        # what the model thinks likeliest, as the teacher of new adapters on an 8-bit base
+        teacher = torch.empty(T, 16, device=step.dev), torch.empty(T, 16, dtype=torch.int32, device=step.dev)
+        step.forward(tokens, target, teacher)
+        step.quantise_base()
+        step.restart()
+        weight = torch.full((T,), 1.0 / args.tokens, device=step.dev)
+        for k in range(args.distill_steps):
+            loss = step.forward(tokens, teacher=teacher)
+            step.backward(None, weight, teacher)
+            step.update()
+            if k % 5 == 0 or k + 1 == args.distill_steps:
+                print("8-bit base, step %3d  losses %s" % (k, ["%.5f" % v for v in loss.view(n, args.tokens).mean(dim=1).tolist()]), flush=True)
+    if args.beams:
+        score, seen = step.search((torch.arange(n) % occur).to(step.dev), list(range(n)), args.beams, args.new_tokens)
+        for t in range(n):
+            for b in range(args.beams):
+                print("task %d: %4d -> %s (%.2f)" % (t, t % occur, " ".join("%4d" % v for v in seen[t, b].tolist()), float(score[t, b])), flush=True)
     # one token per task at a time, all tasks in one call
     step.batch(list(range(n + 1)), list(range(n)), train=False)
     tokens = (torch.arange(n) % occur).to(step.dev)
