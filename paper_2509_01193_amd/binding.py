@@ -163,7 +163,7 @@ def lib():
         L.lobra_token_distill_bwd.argtypes = [ctypes.POINTER(DistillDesc)] + [vp] * 6 + [u32, vp]
         L.lobra_beam_workspace_bytes.argtypes = [ctypes.POINTER(BeamDesc), szp]
         L.lobra_beam_select.argtypes = [ctypes.POINTER(BeamDesc)] + [vp] * 3 + [i32] + [vp] * 4 + [sz, vp]
-        L.lobra_beam_reorder.argtypes = [ctypes.POINTER(BeamState), i32, i32, i32, vp, i64, vp, vp]
+        L.lobra_beam_reorder.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp]
         L.lobra_status_string.restype = ctypes.c_char_p
         L.lobra_status_string.argtypes = [ctypes.c_int]
         L.lobra_version.restype = ctypes.c_int
@@ -687,7 +687,7 @@ def lobra_beam_reorder(states, n_req, beams, parent, used=None, stream=None, che
             assert len(shape) >= 2, "a state without positions"
             unit = row // (shape[1] or 1)
         vals += (src.data_ptr(), dst.data_ptr(), row, unit)
-    arr = ctypes.cast((ctypes.c_int64 * max(len(vals), 4))(*vals), ctypes.POINTER(BeamState))
+    arr = (ctypes.c_int64 * max(len(vals), 4))(*vals)          # (as BeamState has them)
     assert parent.dtype is _torch_types["int32"] and parent.dim() == 2 and parent.shape[0] == n_req and parent.shape[1] >= beams, \
         "parents other than int32 [n_req, beams]"
     assert parent.shape[1] <= 1 or parent.stride(1) == 1, "rows of parents must be contiguous"

@@ -544,7 +544,7 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
                     constexpr int nb = decltype(nb_c)::value;
                     static_for<0, 4>([&](auto v_c) {
                         constexpr int v = decltype(v_c)::value, reg = acc_reg(mb, nb) + v;
-                        acc_write<reg>(float(__float_as_int(acc_read<reg>())) * zs[mb] * ws[nb][v]);
+                        acc_write<reg>(float(__float_as_int(acc_read<reg>())) * ws[nb][v] * zs[mb]);
                     });
                 });
             });

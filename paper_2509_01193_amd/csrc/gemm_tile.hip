@@ -494,7 +494,7 @@ void tile_body(const PlanDev& pd, const uint16_t* __restrict__ Z, const uint16_t
             for (int nb = 0; nb < NB; ++nb) {
                 const i32x4 sum = __builtin_bit_cast(i32x4, acc[mb][nb]);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[mb][nb][v] = float(sum[v]) * zs * ws[nb][v];
+                for (int v = 0; v < 4; ++v) acc[mb][nb][v] = float(sum[v]) * ws[nb][v] * zs;
             }
         }
     }

@@ -180,19 +180,28 @@ __global__ __launch_bounds__(256) void q8_dequantise_kernel(int32_t d_in, int32_
     }
 }
 
+// (a launch holds less than 2^32 threads)
+constexpr int64_t kRowsPerLaunch = 1 << 22;
+
 }  // namespace
 
 hipError_t q8_rows(int64_t T, int32_t d, const void* x, void* q, float* scale, hipStream_t st)
 {
     const int32_t pitch = int32_t(q8_pitch(d));
-    const auto go = [&](auto kernel, int32_t rows) {
-        kernel<<<dim3(uint32_t((T + rows - 1) / rows)), 256, 0, st>>>(int32_t(T), d, pitch, static_cast<const uint16_t*>(x), static_cast<uint8_t*>(q), scale);
-    };
-    // a wave per row where a workgroup has less than two packets a thread and there are enough rows (us, a row per wave / workgroup: 16384 x 256 12.6 /
-    // 20.6, x 1024 17.0 / 23.1, x 2048 22.3 / 28.0, x 4096 37.9 / 36.0, 8190 x 4096 23.4 / 21.8, 40 x 2048 6.9 / 6.1)
-    if (d <= 2048 && T > 1024) go(q8_rows_kernel<1, 8>, 4);
-    else d <= 8192 ? go(q8_rows_kernel<4, 4>, 1) : go(q8_rows_kernel<4, 8>, 1);
-    return hipGetLastError();
+    for (int64_t r = 0; r < T; r += kRowsPerLaunch) {
+        const int32_t n = int32_t(T - r < kRowsPerLaunch ? T - r : kRowsPerLaunch);
+        const auto go = [&](auto kernel, int32_t rows) {
+            kernel<<<dim3(uint32_t((n + rows - 1) / rows)), 256, 0, st>>>(n, d, pitch, static_cast<const uint16_t*>(x) + r * d, static_cast<uint8_t*>(q) + r * pitch,
+                                                                         scale + r);
+        };
+        // a wave per row where a workgroup has less than two packets a thread and there are enough rows (us, a row per wave / workgroup: 16384 x 256
+        // 12.6 / 20.6, x 1024 17.0 / 23.1, x 2048 22.3 / 28.0, x 4096 37.9 / 36.0, 8190 x 4096 23.4 / 21.8, 40 x 2048 6.9 / 6.1)
+        if (d <= 2048 && n > 1024) go(q8_rows_kernel<1, 8>, 4);
+        else d <= 8192 ? go(q8_rows_kernel<4, 4>, 1) : go(q8_rows_kernel<4, 8>, 1);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t q8_weight(int dtype, int32_t d_in, int32_t d_out, int64_t ldw, const void* W, void* q, float* scale, hipStream_t st)

@@ -380,3 +380,38 @@ def test_refusals():
     off16 = torch.empty(max(fwd, bwd) + 16, dtype=torch.uint8, device=DEV)[8:]
     assert F(ws=off16) == -8 and B(ws=off16) == -8
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_launch_holds():
+    """Rows behind the first 2^22, which is where a second launch quantises them."""
+    T, d, f = (1 << 22) + 5, 8, 8
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(T, d, device=DEV, generator=g).bfloat16()
+    W = torch.randn(d, f, device=DEV, generator=g).bfloat16()
+    wq, ws = weight(None, W, d, f)
+    plan = bd.Plan("bf16", T, d, f, None, [0, T], [-1])
+    y = torch.empty(T, f, dtype=torch.bfloat16, device=DEV)
+    wsb = torch.empty(bd.lobra_mlora_quant_workspace_bytes(plan)[0], dtype=torch.uint8, device=DEV)
+    bd.lobra_mlora_quant_fwd(plan, x, wq, ws, None, None, None, y, None, wsb)
+    rows = torch.cat([torch.arange(100), torch.arange((1 << 22) - 50, T)])
+    v = dict(x=x.cpu()[rows], W=W.cpu(), A=torch.zeros(0, d), B=torch.zeros(0, f), s=torch.ones(1), dy=torch.zeros(len(rows), f))
+    ref, off, _, _ = reference(v, [0, len(rows)], [-1], [0], 1)
+    within(y.cpu()[rows], ref["y"], off["y"], True, "y")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,std_x,std_w", [(40, 1e30, 1e-30), (700, 1e33, 1e-30), (700, 1e-30, 1e4)])
+def test_scales_far_apart(T, std_x, std_w):
+    """Tokens and channels whose scales only together are of ordinary size."""
+    d, f = 512, 264
+    v, off, task, rank_off = make(T, d, f, [], "one")
+    v["x"], v["W"] = (v["x"].double() * std_x).bfloat16(), (v["W"].double() * std_w).bfloat16()
+    ref, off_by, _, _ = reference(v, off, task, rank_off, 1)
+    dv = on_device(v)
+    wq, ws = weight(None, dv["W"], d, f)
+    plan = bd.Plan("bf16", T, d, f, None, off, task)
+    y = torch.empty(T, f, dtype=torch.bfloat16, device=DEV)
+    wsb = torch.empty(bd.lobra_mlora_quant_workspace_bytes(plan)[0], dtype=torch.uint8, device=DEV)
+    bd.lobra_mlora_quant_fwd(plan, dv["x"], wq, ws, None, None, None, y, None, wsb)
+    within(y, ref["y"], off_by["y"], True, "y")
