@@ -44,6 +44,9 @@ Q8Product q8_product(const Plan& p)
     return one;
 }
 
+// Few tokens have kernels of their own, which keep no projected activations (which are better: q8_few.hip).
+bool q8_is_few(const Plan& p) { return p.desc.T > 0 && p.desc.T <= kQ8FewTokens && p.desc.d_out <= kQ8FewColumns && p.r_max <= kQ8FewRank; }
+
 // The forward workspace: quantised tokens, their scales, a split product's sums, projected activations.
 struct Q8Layout {
     size_t scale, part, h, total;
@@ -51,11 +54,17 @@ struct Q8Layout {
 Q8Layout q8_layout(const Plan& p, const Q8Product& g, bool h_saved)
 {
     Q8Layout l;
-    l.scale = align256(size_t(p.desc.T) * size_t(q8_pitch(p.desc.d_in)));
+    // (few tokens: in blocks of 16)
+    l.scale = align256(size_t(q8_is_few(p) ? (p.desc.T + 15) / 16 * 16 : p.desc.T) * size_t(q8_pitch(p.desc.d_in)));
     l.part = l.scale + align256(size_t(p.desc.T) * sizeof(float));
     l.h = l.part + (g.choice.splits > 1 || g.beside ? align256(size_t(g.choice.splits + 1) * size_t(p.desc.T) * size_t(g.N) * sizeof(float)) : 0);
     l.total = l.h + (h_saved || p.tb.empty() ? 0 : p.p_layout.total);
     return l;
+}
+
+size_t q8_fwd_bytes(const Plan& p, const Q8Layout& l, bool h_saved)
+{
+    return h_saved || !q8_is_few(p) || p.tb.empty() ? l.total : std::max(l.total, l.part + q8_few_bytes(p.desc.T, p.r_max));
 }
 
 size_t q8_weight_bytes(const Plan& p) { return align256(size_t(p.desc.d_in) * size_t(p.desc.d_out) * 2); }
@@ -83,7 +92,7 @@ lobra_status lobra_mlora_quant_workspace_bytes(const lobra_mlora_plan* plan, siz
     if (!plan) return LOBRA_ERR_PLAN;
     const lobra_status rs = q8_plan(*plan);
     if (rs != LOBRA_OK) return rs;
-    if (fwd_bytes) *fwd_bytes = plan->desc.T == 0 ? 0 : q8_layout(*plan, q8_product(*plan), false).total;
+    if (fwd_bytes) *fwd_bytes = plan->desc.T == 0 ? 0 : q8_fwd_bytes(*plan, q8_layout(*plan, q8_product(*plan), false), false);
     if (bwd_bytes) *bwd_bytes = q8_weight_bytes(*plan) + plan->bwd_ws_bytes;
     return LOBRA_OK;
 }
@@ -101,7 +110,8 @@ lobra_status lobra_mlora_quant_fwd(const lobra_mlora_plan* plan, const void* x, 
     const Q8Layout l = q8_layout(p, g, h_save != nullptr);
     if ((rs = plan_fwd_check(p, x, Wq, A, B, s, y, h_save, ws, ws_bytes)) != LOBRA_OK) return rs;
     if (!aligned16(w_scale)) return LOBRA_ERR_ALIGN;
-    if (!ws || ws_bytes < l.total) return LOBRA_ERR_WORKSPACE;
+    const bool few = q8_is_few(p) && !h_save;
+    if (!ws || ws_bytes < q8_fwd_bytes(p, l, h_save != nullptr)) return LOBRA_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const PlanDev pd = device_view(p);
     const bool adapters = !p.tb.empty();
@@ -109,6 +119,12 @@ lobra_status lobra_mlora_quant_fwd(const lobra_mlora_plan* plan, const void* x, 
     float* const x_scale = reinterpret_cast<float*>(wsb + l.scale);
     float* const part = reinterpret_cast<float*>(wsb + l.part);
     char* const hb = h_save ? static_cast<char*>(h_save) : wsb + l.h;
+    if (few) {
+        float* const P = adapters ? part : nullptr;
+        LOBRA_LAUNCH(p, st, adapters ? LOBRA_K_SHRINK : LOBRA_K_QUANT, q8_few_rows(pd, x, A, s, wsb, x_scale, P, st));
+        LOBRA_LAUNCH(p, st, LOBRA_K_GEMM, q8_few(pd, wsb, x_scale, Wq, w_scale, P, B, y, st));
+        return LOBRA_OK;
+    }
     LOBRA_LAUNCH(p, st, LOBRA_K_QUANT, q8_rows(p.desc.T, pd.d_in, x, wsb, x_scale, st));
     if (g.beside) {
         LOBRA_LAUNCH(p, st, LOBRA_K_SHRINK_GEMM,

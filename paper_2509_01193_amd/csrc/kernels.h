@@ -103,6 +103,13 @@ constexpr int64_t q8_pitch(int64_t d) { return (d + kQ8Pad - 1) / kQ8Pad * kQ8Pa
 // q [T][q8_pitch(d)] and scale [T] of x [T][d]: scale = max |x| / 127, q = x / scale to the nearest, halves to the even one.  A row of zeros has
 // the scale 0, one with NaN or infinity the scale NaN and q = 0.
 hipError_t q8_rows(int64_t T, int32_t d, const void* x, void* q, float* scale, hipStream_t st);
+// Up to kQ8FewTokens tokens (q8_few.hip): q (whole blocks of 16 tokens) and scale, with P the projections of x (q8_few_bytes; or NULL), then y.
+constexpr int64_t kQ8FewTokens = 48;
+constexpr int32_t kQ8FewColumns = 4096, kQ8FewRank = 32;
+size_t q8_few_bytes(int64_t T, int32_t r_max);
+hipError_t q8_few_rows(const PlanDev& pd, const void* x, const void* A, const float* s, void* q, float* scale, float* P, hipStream_t st);
+hipError_t q8_few(const PlanDev& pd, const void* Z, const float* z_scale, const void* W, const float* w_scale, const float* P, const void* B, void* y,
+                  hipStream_t st);
 // The same of the columns of W [d_in][ldw], transposed: q [d_out][q8_pitch(d_in)], scale [d_out]; and W [d_in][d_out] in bf16 from them.
 hipError_t q8_weight(int dtype, int32_t d_in, int32_t d_out, int64_t ldw, const void* W, void* q, float* scale, hipStream_t st);
 hipError_t q8_dequantise(int32_t d_in, int32_t d_out, const void* q, const float* scale, void* W, hipStream_t st);

@@ -68,7 +68,7 @@ def test_only_the_named_statements_touch_agprs(q8_kernels):
         assert code[last:first].count("s_nop 15") == 2, code[last:first]
 
 
-@pytest.mark.parametrize("source", ["gemm_persistent_q8.hip", "gemm_tile_q8.hip", "q8.hip", "distill.hip", "beam.hip"])
+@pytest.mark.parametrize("source", ["gemm_persistent_q8.hip", "gemm_tile_q8.hip", "q8.hip", "q8_few.hip", "distill.hip", "beam.hip"])
 def test_lds_writes_are_waited_for(tmp_path, source):
     parts = re.split(r"^(_ZN5lobra\w+):", assembly(tmp_path, source), flags=re.M)
     barriers = 0
@@ -82,6 +82,6 @@ def test_lds_writes_are_waited_for(tmp_path, source):
     assert barriers >= 1, source
 
 
-@pytest.mark.parametrize("source,least", [("gemm_persistent_q8.hip", 1), ("gemm_tile_q8.hip", 6), ("q8.hip", 5), ("distill.hip", 20), ("beam.hip", 10)])
+@pytest.mark.parametrize("source,least", [("gemm_persistent_q8.hip", 1), ("gemm_tile_q8.hip", 6), ("q8.hip", 5), ("q8_few.hip", 5), ("distill.hip", 20), ("beam.hip", 10)])
 def test_no_scratch_memory(tmp_path, source, least):
     SCRATCH(tmp_path, source, least)
