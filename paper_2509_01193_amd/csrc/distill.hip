@@ -63,6 +63,19 @@ template <typename E> struct NoneListed {
     template <int N> __device__ __forceinline__ void operator()(float (&)[N], int32_t, int = 0) const {}
 };
 
+// How often a token stands in the list (kMost ids, -1 in empty places), read four ids at a time: nearly always once.  219 x 1408 with 128 places, forward
+// and backward, us: place by place 27.8, so 12.5.
+__device__ __forceinline__ int32_t times_listed(const int32_t* ids, int32_t k, int32_t id)
+{
+    int32_t n = 0;
+#pragma unroll 4
+    for (int32_t i = 0; i < k; i += 4) {
+        const int4 v = *reinterpret_cast<const int4*>(ids + i);
+        n += int32_t(v.x == id) + int32_t(v.y == id) + int32_t(v.z == id) + int32_t(v.w == id);
+    }
+    return n;
+}
+
 // Elements listed in a row, as bits.  Bit 0 of a packet's is bit 0 of a group of N (the elements in front of the first packet end a group of their own).
 template <typename E, int NT> struct ListedBits {
     static constexpr int N = Packet<E>::N;
@@ -112,7 +125,7 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
     static_assert(NT >= kMost, "a thread per place of the list");
     extern __shared__ __attribute__((aligned(16))) uint32_t table[];
     __shared__ Stat part[W];
-    __shared__ int32_t ids[kMost];                   // -1: an empty place
+    __shared__ __attribute__((aligned(16))) int32_t ids[kMost];      // -1: an empty place
     __shared__ double join[3][kMost / 64];
     __shared__ float top[2][kMost / 64];
     __shared__ bool any[kMost / 64];
@@ -159,7 +172,8 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
         const float zm = fmaxf(top[1][0], top[1][1]);
         M = fmax(rest_m, double(zm));
         bool first = id >= 0;
-        for (int32_t i = 0; i < k; ++i) first = first && !(i < tid && ids[i] == id);
+        if (first && times_listed(ids, k, id) > 1)
+            for (int32_t i = 0; i < tid; ++i) first = first && ids[i] != id;
         if (first) ex = M == -INFINITY ? 0. : exp((double(zj) - M) * cd);
         own = id >= 0 ? exp(ln_q) : 0.;
     } else {
@@ -229,9 +243,9 @@ void distill_bwd_kernel(const E* logits, int64_t ld, int32_t V, int32_t k, float
 {
     constexpr int N = Packet<E>::N;
     static_assert(NT >= kMost, "a thread per place of the list");
-    __shared__ int32_t ids[kMost];
+    __shared__ __attribute__((aligned(16))) int32_t ids[kMost];      // -1: an empty place
     __shared__ float qs[kMost];
-        const size_t r = size_t(xcd_contiguous(int32_t(gridDim.x - 1 - blockIdx.x), int32_t(gridDim.x)));
+    const size_t r = size_t(xcd_contiguous(int32_t(gridDim.x - 1 - blockIdx.x), int32_t(gridDim.x)));
     const E* row = logits + r * size_t(ld);
     E* out = dlogits + r * size_t(ld);
     const RowShape sh = row_shape(row, V);            // (logits and dlogits are aligned alike: both bases to 16 bytes)
@@ -263,9 +277,9 @@ void distill_bwd_kernel(const E* logits, int64_t ld, int32_t V, int32_t k, float
                 if (ADD) had = Elem<E>::load(out, size_t(id));
             }
         }
-        ids[t] = id;
         qs[t] = l == INFINITY ? NAN : TAIL ? float(exp(double(l))) : float(exp((double(l) - double(st.z) - double(st.w)) * double(c)));
     }
+    if (t < kMost) ids[t] = id;
     const float rest = -scale * st.y;
     const float sum_q = TAIL ? (st.z == INFINITY ? st.w : 1.f) : st.z == st.z ? 1.f : NAN;        // (a teacher of NaN)
     // the tail as a multiple of p, where that is not near the ends of fp32's range (else an exponential of its own)
@@ -281,11 +295,14 @@ void distill_bwd_kernel(const E* logits, int64_t ld, int32_t V, int32_t k, float
     __syncthreads();
     float gj = 0.f;
     if (mine) {
-        float q = 0.f;
-        for (int32_t i = 0; i < k; ++i) {
-            const bool same = ids[i] == id;
-            if (same && i < t) mine = false;         // an earlier place writes it
-            q += same ? qs[i] : 0.f;
+        float q = qs[t];
+        if (times_listed(ids, k, id) > 1) {
+            q = 0.f;
+            for (int32_t i = 0; i < k; ++i) {
+                const bool same = ids[i] == id;
+                if (same && i < t) mine = false;     // an earlier place writes it
+                q += same ? qs[i] : 0.f;
+            }
         }
         gj = had + w * (sum_q * exp2_fast(fmaf(zj - st.x, scale, rest)) - q);
     }
