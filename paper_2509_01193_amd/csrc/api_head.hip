@@ -36,15 +36,15 @@ lobra_status beam_shape(const lobra_beam_desc* d, BeamShape* s)
         d->n_out > LOBRA_MAX_TOP)
         return LOBRA_ERR_SHAPE;
     const int64_t rows = int64_t(d->n_req) * d->beams;
-    if (rows >= int64_t(1) << 24 || rows * beam_parts(d->V) >= int64_t(1) << 24) return LOBRA_ERR_SHAPE;     // (a launch holds less than 2^32 threads)
+    if (rows >= int64_t(1) << 24 || rows * beam_parts(d->dtype, d->V) >= int64_t(1) << 24) return LOBRA_ERR_SHAPE;     // (a launch holds less than 2^32 threads)
     if (rows > 0 && ld >= (int64_t(1) << 60) / rows) return LOBRA_ERR_SHAPE;
     *s = BeamShape{d->dtype, d->V, ld, d->n_req, d->beams, d->n_out};
     return LOBRA_OK;
 }
 
 // Every part's largest logits, then its sums.
-size_t beam_key_bytes(const BeamShape& s) { return size_t(s.n_req) * s.beams * beam_parts(s.V) * s.n_out * sizeof(uint64_t); }
-size_t beam_ws_bytes(const BeamShape& s) { return beam_key_bytes(s) + size_t(s.n_req) * s.beams * beam_parts(s.V) * 2 * sizeof(float); }
+size_t beam_key_bytes(const BeamShape& s) { return size_t(s.n_req) * s.beams * beam_parts(s.dtype, s.V) * s.n_out * sizeof(uint64_t); }
+size_t beam_ws_bytes(const BeamShape& s) { return beam_key_bytes(s) + size_t(s.n_req) * s.beams * beam_parts(s.dtype, s.V) * 2 * sizeof(float); }
 
 }  // namespace
 

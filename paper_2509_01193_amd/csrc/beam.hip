@@ -3,7 +3,7 @@
 //
 // Selection.  Beam b of score s continued by token j has the value (s - lse_b) + z_j, lse_b = ln sum exp(z_b).  A beam's own best continuations
 // are its largest logits, so a part of a row hands on its n largest logits, the lowest index first among equals, and its sum; a workgroup per
-// request then makes lse and values, in fp64, and orders what is left.  A logit is read once: a part's 8192 stay in registers from the sum to
+// request then makes lse and values, in fp64, and orders what is left.  A logit is read once: a part's 16 KB stay in registers from the sum to
 // the choice.  Rows are cut into parts by index, wherever they begin in memory, so that beams of equal logits have equal sums bit for bit, and
 // what is equal in the formula is equal here.
 // Reordering.  A thread has the same 16 bytes of all rows of a request: it has read every row it needs before it writes one, which is all
@@ -19,7 +19,10 @@ using namespace rows;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPart = 8192;               // elements of a row that a workgroup works on at a time
+// Bytes of a row that a workgroup works on at a time.  64 x 8 x 128000, the choice of a step, us: bf16 with 8 KB 51, 16 KB 43, 32 KB 53 (512 threads 46);
+// fp32 8 KB 79, 16 KB 59, 32 KB 70, 64 KB 58; 5 x 5 x 50257 fp32 with its states 13.3, 14.3, 15.4.
+constexpr int kPartBytes = 16384;
+template <typename E> constexpr int kPart = kPartBytes / int(sizeof(E));
 constexpr int kPackets = 128;             // 16 bytes each of a part's logits that may hold one of the best
 constexpr int kList = 512;                // of a part's logits, or a request's continuations, that may be among the best
 
@@ -63,19 +66,19 @@ __global__ __launch_bounds__(kThreads)
 void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* __restrict__ score, const int32_t* __restrict__ done, int32_t parts,
                       bool at_once, uint64_t* __restrict__ keys, float2* __restrict__ sums)
 {
-    constexpr int N = Packet<E>::N, U = kPart / (kThreads * N), W = kThreads / 64;
+    constexpr int N = Packet<E>::N, U = kPart<E> / (kThreads * N), W = kThreads / 64;
     __shared__ uint64_t list[kList];
     __shared__ float group_max[64];
     __shared__ Stat stat[W];
     __shared__ u32x4 packet[kPackets];
     __shared__ int32_t packet_at[kPackets], packets, count;
     const int32_t tid = threadIdx.x, lane = tid & 63, n = sh.n_out;
-    const int32_t row = int32_t(blockIdx.x) / parts, base = (int32_t(blockIdx.x) - row * parts) * kPart, len = min(kPart, sh.V - base);
+    const int32_t row = int32_t(blockIdx.x) / parts, base = (int32_t(blockIdx.x) - row * parts) * kPart<E>, len = min(kPart<E>, sh.V - base);
     // (at_once: the logits are fetched before it is known whether they are looked at, a round trip less; many parts find out first)
     if (!at_once && !looked_at(score[row], done, size_t(row))) return;
     const E* p = logits + size_t(row) * size_t(sh.ld) + base;
     u32x4 q[U];
-    if (len == kPart) {                              // (uniform)
+    if (len == kPart<E>) {                            // (uniform)
 #pragma unroll
         for (int c = 0; c < U; ++c) q[c] = *reinterpret_cast<const typename Loose<E>::type*>(p + (c * kThreads + tid) * N);
     } else
@@ -409,12 +412,16 @@ hipError_t launch_reorder(const StateTable& tab, dim3 grid, int64_t first_block,
 
 }  // namespace
 
-int32_t beam_parts(int32_t V) { return (V + kPart - 1) / kPart; }
+int32_t beam_parts(int32_t dtype, int32_t V)
+{
+    const int32_t part = dtype == LOBRA_F32 ? kPart<float> : kPart<uint16_t>;
+    return (V - 1) / part + 1;
+}
 
 hipError_t beam_select(const BeamShape& s, const void* logits, const float* score, const int32_t* done, int32_t done_token, float* out_score,
                        int32_t* out_beam, int32_t* out_token, uint64_t* keys, float* sums, hipStream_t st)
 {
-    const int32_t parts = beam_parts(s.V);
+    const int32_t parts = beam_parts(s.dtype, s.V);
     const dim3 grid(uint32_t(s.n_req) * uint32_t(s.beams) * uint32_t(parts));
     const bool at_once = grid.x <= 1024;
     if (s.dtype == LOBRA_F32)

@@ -184,14 +184,14 @@ hipError_t distill_fwd(const DistillShape& s, const void* logits, const float* t
 hipError_t distill_bwd(const DistillShape& s, const void* logits, const float* teacher_logp, const int32_t* teacher_id, const float* stat,
                        const float* dloss, void* dlogits, bool accumulate, hipStream_t st);
 
-// Beam search (beam.hip): lobra_beam_select with checked arguments (n_req > 0, n_req beams beam_parts(V) < 2^24).  keys [n_req beams parts][n_out], sums
+// Beam search (beam.hip): lobra_beam_select with checked arguments (n_req > 0, n_req beams beam_parts < 2^24).  keys [n_req beams parts][n_out], sums
 // [n_req beams parts][2].  lobra_beam_reorder likewise.
 struct BeamShape {
     int32_t dtype, V;
     int64_t ld;
     int32_t n_req, beams, n_out;
 };
-int32_t beam_parts(int32_t V);
+int32_t beam_parts(int32_t dtype, int32_t V);
 hipError_t beam_select(const BeamShape& s, const void* logits, const float* score, const int32_t* done, int32_t done_token, float* out_score,
                        int32_t* out_beam, int32_t* out_token, uint64_t* keys, float* sums, hipStream_t st);
 hipError_t beam_reorder(const lobra_beam_state* states, int32_t n_states, int32_t n_req, int32_t beams, const int32_t* parent, int64_t parent_ld,
