@@ -246,6 +246,23 @@ def _typed(t, kind, least=0):
     return t.data_ptr()
 
 
+_current_device = None
+
+
+def _here(t):
+    """t, which has to lie on the device that the call is launched on: the current one."""
+    global _current_device
+    if t is not None and not isinstance(t, int):
+        device = t.get_device()
+        assert device >= 0, "a host tensor where the library reads or writes device memory"
+        if _current_device is None:
+            import torch
+            torch.cuda.current_device()           # (initialises, or says why it can't)
+            _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        assert device == _current_device(), "a tensor of another device than the current one"
+    return t
+
+
 _current_stream = None
 
 
@@ -287,6 +304,7 @@ class Plan:
         self.T, self.d_in, self.d_out = int(T), int(d_in), int(d_out)
         self.n_tasks, self.kind = self.desc.n_tasks, _KINDS[self.desc.dtype]
         self.R_tot = int(np.asarray(rank_off)[-1]) if self.n_tasks > 0 else 0
+        self.host_only = bool(int(flags) & PLAN_HOST_ONLY)
 
     @classmethod
     def for_problem(cls, p, flags=0):
@@ -580,7 +598,7 @@ def lobra_quantise_weight(W, Wq, w_scale, stream=None, check=True):
     assert kind is not None, "a weight of another type than fp32 and bf16"
     assert d_out <= 1 or W.stride(1) == 1, "rows of a weight must be contiguous"
     assert Wq.shape == (d_out, lobra_quant_pitch(d_in)), "Wq of another shape than [d_out, lobra_quant_pitch(d_in)]"
-    st = lib().lobra_quantise_weight(kind, d_in, d_out, W.stride(0) if d_in > 1 else 0, W.data_ptr(), _typed(Wq, "int8"),
+    st = lib().lobra_quantise_weight(kind, d_in, d_out, W.stride(0) if d_in > 1 else 0, _here(W).data_ptr(), _typed(Wq, "int8"),
                                         _typed(w_scale, "fp32", d_out), _stream(stream))
     if check:
         _check(st, "lobra_quantise_weight")
@@ -594,15 +612,22 @@ def lobra_mlora_quant_workspace_bytes(plan: Plan):
     return a.value, b.value
 
 
-def _quant_weight(plan: Plan, Wq, w_scale):
-    return _typed(Wq, "int8", plan.d_out * lobra_quant_pitch(plan.d_in)), _typed(w_scale, "fp32", plan.d_out)
+def _quant_operands(plan: Plan, x, Wq, w_scale, A, B, s):
+    R = plan.R_tot
+    return (_typed(x if plan.host_only else _here(x), plan.kind, plan.T * plan.d_in), _typed(Wq, "int8", plan.d_out * lobra_quant_pitch(plan.d_in)),
+            _typed(w_scale, "fp32", plan.d_out), _typed(A, plan.kind, R * plan.d_in), _typed(B, plan.kind, R * (plan.d_out // plan.desc.n_proj)),
+            _typed(s, "fp32", plan.n_tasks))
+
+
+def _saved(plan: Plan, h):
+    assert h is None or isinstance(h, int) or _nbytes(h) >= plan.h_save_bytes, "fewer bytes than plan.h_save_bytes"
+    return _ptr(h)
 
 
 def lobra_mlora_quant_fwd(plan: Plan, x, Wq, w_scale, A, B, s, y, h_save=None, ws=None, stream=None, check=True):
     """y = x W + s_t (A_t x) B_t with W and x in 8-bit integers in the first product.  Returns the status."""
-    e, T = plan.kind, plan.T
-    st = lib().lobra_mlora_quant_fwd(plan.handle, _typed(x, e, T * plan.d_in), *_quant_weight(plan, Wq, w_scale), _typed(A, e), _typed(B, e), _typed(s, "fp32"),
-                                  _typed(y, e, T * plan.d_out), _ptr(h_save), _ptr(ws), _nbytes(ws), _stream(stream))
+    st = lib().lobra_mlora_quant_fwd(plan.handle, *_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(y, plan.kind, plan.T * plan.d_out),
+                                  _saved(plan, h_save), _ptr(ws), _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_mlora_quant_fwd")
     return st
@@ -610,9 +635,9 @@ def lobra_mlora_quant_fwd(plan: Plan, x, Wq, w_scale, A, B, s, y, h_save=None, w
 
 def lobra_mlora_quant_bwd(plan: Plan, x, Wq, w_scale, A, B, s, dy, h_saved, dx, dA, dB, flags=0, ws=None, stream=None, check=True):
     """dx, dA, dB of the layer on an 8-bit base.  Returns the status."""
-    e, T = plan.kind, plan.T
-    st = lib().lobra_mlora_quant_bwd(plan.handle, _typed(x, e, T * plan.d_in), *_quant_weight(plan, Wq, w_scale), _typed(A, e), _typed(B, e), _typed(s, "fp32"),
-                                  _typed(dy, e, T * plan.d_out), _ptr(h_saved), _typed(dx, e, T * plan.d_in), _typed(dA, "fp32"), _typed(dB, "fp32"),
+    e, T, R = plan.kind, plan.T, plan.R_tot
+    st = lib().lobra_mlora_quant_bwd(plan.handle, *_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(dy, e, T * plan.d_out), _saved(plan, h_saved),
+                                  _typed(dx, e, T * plan.d_in), _typed(dA, "fp32", R * plan.d_in), _typed(dB, "fp32", R * (plan.d_out // plan.desc.n_proj)),
                                   int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_mlora_quant_bwd")
@@ -633,7 +658,7 @@ def _teacher(desc: DistillDesc, teacher_logp, teacher_id):
 def lobra_token_distill_fwd(desc: DistillDesc, logits, teacher_logp, teacher_id, loss, stat=None, stream=None, check=True):
     """loss [T] of every row against the teacher's tokens [T, top_k]; stat (fp32 [T, 4]) for backward.  Returns the status."""
     T = desc.T
-    st = lib().lobra_token_distill_fwd(ctypes.byref(desc), _rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id), _typed(loss, "fp32", T),
+    st = lib().lobra_token_distill_fwd(ctypes.byref(desc), _rows_ptr(_here(logits), desc), *_teacher(desc, teacher_logp, teacher_id), _typed(loss, "fp32", T),
                                        _typed(stat, "fp32", 4 * T), _stream(stream))
     if check:
         _check(st, "lobra_token_distill_fwd")
@@ -643,7 +668,7 @@ def lobra_token_distill_fwd(desc: DistillDesc, logits, teacher_logp, teacher_id,
 def lobra_token_distill_bwd(desc: DistillDesc, logits, teacher_logp, teacher_id, stat, dloss, dlogits, flags=0, stream=None, check=True):
     """dlogits (may be logits) from dloss [T].  Returns the status."""
     T = desc.T
-    st = lib().lobra_token_distill_bwd(ctypes.byref(desc), _rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id),
+    st = lib().lobra_token_distill_bwd(ctypes.byref(desc), _rows_ptr(_here(logits), desc), *_teacher(desc, teacher_logp, teacher_id),
                                        _typed(stat, "fp32", 4 * T), _typed(dloss, "fp32", T), _rows_ptr(dlogits, desc), int(flags), _stream(stream))
     if check:
         _check(st, "lobra_token_distill_bwd")
@@ -664,7 +689,7 @@ def lobra_beam_workspace_bytes(desc: BeamDesc) -> int:
 def lobra_beam_select(desc: BeamDesc, logits, score, done, done_token, out_score, out_beam, out_token, ws, stream=None, check=True):
     """The n_out best continuations of every request: scores, beams within the request, tokens.  Returns the status."""
     rows, n = desc.n_req * desc.beams, desc.n_req * desc.n_out
-    st = lib().lobra_beam_select(ctypes.byref(desc), _rows_ptr(logits, desc, rows), _typed(score, "fp32", rows), _typed(done, "int32", rows),
+    st = lib().lobra_beam_select(ctypes.byref(desc), _rows_ptr(_here(logits), desc, rows), _typed(score, "fp32", rows), _typed(done, "int32", rows),
                                  int(done_token), _typed(out_score, "fp32", n), _typed(out_beam, "int32", n), _typed(out_token, "int32", n), _ptr(ws),
                                  _nbytes(ws), _stream(stream))
     if check:
@@ -691,7 +716,7 @@ def lobra_beam_reorder(states, n_req, beams, parent, used=None, stream=None, che
     assert parent.dtype is _torch_types["int32"] and parent.dim() == 2 and parent.shape[0] == n_req and parent.shape[1] >= beams, \
         "parents other than int32 [n_req, beams]"
     assert parent.shape[1] <= 1 or parent.stride(1) == 1, "rows of parents must be contiguous"
-    st = lib().lobra_beam_reorder(arr, len(states), int(n_req), int(beams), parent.data_ptr(), parent.stride(0) if n_req > 1 else int(beams),
+    st = lib().lobra_beam_reorder(arr, len(states), int(n_req), int(beams), _here(parent).data_ptr(), parent.stride(0) if n_req > 1 else int(beams),
                                   _typed(used, "int32", n_req), _stream(stream))
     if check:
         _check(st, "lobra_beam_reorder")

@@ -474,3 +474,16 @@ def test_on_another_stream_and_in_a_graph():
         go(eager)
         torch.cuda.synchronize()
         assert all(torch.equal(eager[i], graphed[i]) for i in eager), r
+
+
+def test_host_tensors():
+    """What lies in host memory is refused before anything is launched."""
+    z, f, i = torch.zeros(3, 100).bfloat16(), torch.zeros(3, 5), torch.zeros(3, 5, dtype=torch.int32)
+    dd, bm = bd.make_distill_desc("bf16", 3, 100, 5), bd.make_beam_desc("bf16", 1, 3, 100)
+    one, par, ws = torch.zeros(1, 3), torch.zeros(1, 3, dtype=torch.int32), torch.zeros(4096, dtype=torch.uint8)
+    for call in (lambda: bd.lobra_token_distill_fwd(dd, z, f, i, torch.zeros(3), torch.zeros(3, 4), stream=0),
+                 lambda: bd.lobra_token_distill_bwd(dd, z, f, i, torch.zeros(3, 4), torch.zeros(3), z, stream=0),
+                 lambda: bd.lobra_beam_select(bm, z, one, None, 2, one, par, par.clone(), ws, stream=0),
+                 lambda: bd.lobra_beam_reorder([(z, z)], 1, 3, par, stream=0)):
+        with pytest.raises(AssertionError, match="host tensor"):
+            call()

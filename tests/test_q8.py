@@ -426,3 +426,20 @@ def test_scales_far_apart(T, std_x, std_w):
 def test_few_tokens(T, d_in, d_out, ranks, batch, n_proj):
     """On both sides of what the kernels for few tokens take; forward with and without what backward starts from."""
     test_layer(T, d_in, d_out, ranks, batch, n_proj)
+
+
+def test_host_tensors_and_short_ones():
+    with pytest.raises(AssertionError, match="host tensor"):
+        bd.lobra_quantise_weight(torch.zeros(8, 16), torch.zeros(16, 256, dtype=torch.int8), torch.zeros(16), stream=0)
+    plan = bd.Plan("bf16", 8, 64, 64, [0, 8, 24], [0, 4, 8], [0, 1], flags=bd.PLAN_HOST_ONLY)
+    x, a, q, s, f = torch.zeros(8, 64).bfloat16(), torch.zeros(24, 64).bfloat16(), torch.zeros(64, 256, dtype=torch.int8), torch.zeros(64), torch.zeros(24, 64)
+    fwd = dict(x=x, Wq=q, w_scale=s, A=a, B=a, s=s[:2], y=x, stream=0, check=False)
+    bwd = dict(x=x, Wq=q, w_scale=s, A=a, B=a, s=s[:2], dy=x, h_saved=None, dx=x, dA=f, dB=f, stream=0, check=False)
+    assert bd.lobra_mlora_quant_fwd(plan, **fwd) == -10 and bd.lobra_mlora_quant_bwd(plan, **bwd) == -10
+    short = torch.zeros(plan.h_save_bytes - 1, dtype=torch.uint8)
+    for bad in (dict(A=a[:23]), dict(B=a[:23]), dict(s=s[:1]), dict(h_save=short)):
+        with pytest.raises(AssertionError):
+            bd.lobra_mlora_quant_fwd(plan, **{**fwd, **bad})
+    for bad in (dict(dA=f[:23]), dict(dB=f[:23]), dict(A=a[:23]), dict(s=s[:1]), dict(h_saved=short)):
+        with pytest.raises(AssertionError):
+            bd.lobra_mlora_quant_bwd(plan, **{**bwd, **bad})
