@@ -483,7 +483,7 @@ typedef struct {
     int32_t dtype;           /* lobra_dtype of the logits */
     int32_t V;               /* 1 .. LOBRA_MAX_VOCAB */
     int64_t ld;              /* row pitch in elements, >= V (0: V), n_req beams ld < 2^60 */
-    int32_t n_req;           /* 0 <= n_req, n_req beams < 2^24 */
+    int32_t n_req;           /* 0 <= n_req; n_req beams, each counted once for every 16 KB of its row, < 2^24 */
     int32_t beams;           /* 1 .. LOBRA_MAX_TOP */
     int32_t n_out;           /* 1 .. LOBRA_MAX_TOP */
 } lobra_beam_desc;

@@ -8,7 +8,8 @@
 // them at the end: p_r as a difference would lose all its digits where the student is sure of the list.  A table of bits in LDS says which
 // elements are listed, a byte (bf16) to a packet.  The list itself, up to 128 tokens, is a thread's business each, in fp64: it costs a row next to nothing.
 // Backward writes every element as if it were not listed, and then the listed ones.
-// Bound: memory.
+// Bound: memory.  Forward / backward, us: 8190 x 32000 bf16, 20 listed, 119 / 156 (backward leaves the rows without a teacher unread), 4096 x 128000 with a tail and 64 listed
+// 193 / 415 (5.4 and 5.0 TB/s), 1000 x 50257 fp32 with a tail 54 / 72; 48 x 32000 6.0 / 4.7, where a row is three rounds to memory and the list in fp64.
 #include "kernels.h"
 #include "row_common.h"
 #include "row_logits.h"

@@ -18,7 +18,7 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(int32_t T, int32_t d, int3
 }
 
 // 64 columns per workgroup, a lane each; its 16 waves share the rows, 16 neighbouring ones at a time, so that a lane's 16 values are 16 neighbouring
-// bytes of its column's row of q.  Done once per weight.
+// bytes of its column's row of q.  Done once per weight: 4096 x 11008 bf16 180 us (with four waves a workgroup 617).
 constexpr int kWeightWaves = 16;
 template <typename E>
 __global__ __launch_bounds__(64 * kWeightWaves) void q8_weight_kernel(int32_t d_in, int32_t d_out, int32_t pitch, int64_t ldw, const E* __restrict__ W,
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * kWeightWaves) void q8_weight_kernel(int32_t d_
 }
 
 // W [d_in][d_out] = q scale, rounded once to bf16 (backward multiplies in bf16).  A block of 64 x 64 through LDS: 64 bytes of each row of q are
-// read, whole 128-byte lines of W written.
+// read, whole 128-byte lines of W written.  Bound: memory, 4096 x 4096 13 us (3.9 TB/s).
 __global__ __launch_bounds__(256) void q8_dequantise_kernel(int32_t d_in, int32_t d_out, int32_t pitch, const uint8_t* __restrict__ q,
                                                             const float* __restrict__ scale, uint16_t* __restrict__ W)
 {
