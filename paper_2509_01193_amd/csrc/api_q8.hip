@@ -45,7 +45,10 @@ Q8Product q8_product(const Plan& p)
 }
 
 // Few tokens have kernels of their own, which keep no projected activations (which are better: q8_few.hip).
-bool q8_is_few(const Plan& p) { return p.desc.T > 0 && p.desc.T <= kQ8FewTokens && p.desc.d_out <= kQ8FewColumns && p.r_max <= kQ8FewRank; }
+bool q8_is_few(const Plan& p)
+{
+    return p.desc.T > 0 && p.desc.T <= kQ8FewTokens && p.desc.d_out <= kQ8FewColumns * (p.desc.T <= 16 ? 2 : 1) && p.r_max <= kQ8FewRank;
+}
 
 // The forward workspace: quantised tokens, their scales, a split product's sums, projected activations.
 struct Q8Layout {

@@ -104,8 +104,8 @@ constexpr int64_t q8_pitch(int64_t d) { return (d + kQ8Pad - 1) / kQ8Pad * kQ8Pa
 // the scale 0, one with NaN or infinity the scale NaN and q = 0.
 hipError_t q8_rows(int64_t T, int32_t d, const void* x, void* q, float* scale, hipStream_t st);
 // Up to kQ8FewTokens tokens (q8_few.hip): q (whole blocks of 16 tokens) and scale, with P the projections of x (q8_few_bytes; or NULL), then y.
-constexpr int64_t kQ8FewTokens = 48;
-constexpr int32_t kQ8FewColumns = 4096, kQ8FewRank = 32;
+constexpr int64_t kQ8FewTokens = 64;
+constexpr int32_t kQ8FewColumns = 4096, kQ8FewRank = 32;          // (up to 16 tokens: twice the columns)
 size_t q8_few_bytes(int64_t T, int32_t r_max);
 hipError_t q8_few_rows(const PlanDev& pd, const void* x, const void* A, const float* s, void* q, float* scale, float* P, hipStream_t st);
 hipError_t q8_few(const PlanDev& pd, const void* Z, const float* z_scale, const void* W, const float* w_scale, const float* P, const void* B, void* y,

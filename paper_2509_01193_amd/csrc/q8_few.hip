@@ -2,15 +2,18 @@
 // adapter term and writes y.
 //
 // The product reads W once and does next to nothing with it, so what counts is that all of W is on its way at once and that no sum goes
-// through memory.  A workgroup has 16 columns, its eight waves share K: a lane's 16 bytes of W go straight from memory into the matrix instruction, eight
-// of them in flight, and the waves' whole sums meet in LDS.  The tokens (a few hundred KB) come from the L2 in the same form.
+// through memory.  A workgroup has 16 columns, its eight waves share K in pieces of 256, two of them on their way, and the waves' whole sums meet in LDS.  A lane of
+// the matrix instruction holds 16 k of a column of its own; read like that, each load touches 64 bytes of 16 lines, so four whole lines of each of four columns are read
+// instead and turned in LDS (40 x 4096 x 4096 15.7 -> 13.2, 40 x 11008 x 4096 29.9 -> 23.3, as for a W that lies in memory the way the instruction takes it: 14.2, 26.3 with
+// one piece on its way).  The tokens (a few hundred KB) come from the L2, in that form.
 // The projection of a token has a workgroup per quarter of K, since one alone streams the 128 KiB of a rank-16 adapter at K = 4096 for longer than the
 // product takes; the quarters' fp32 sums are added where they are used.
-// Tokens x K x N, one-token segments, us, with the tiled product (q8.hip, gemm_tile_q8.hip) / these: rank 16, 1 x 4096 x 4096 13.6 / 11.0, 16 of them 15.3 / 11.9, 40
-// 15.4 / 15.0, 64 16.6 / 17.5; 8 x 1376 x 4096 11.7 / 9.3, 20 x 512 x 512 10.4 / 7.9, 32 x 2048 x 2048 12.3 / 9.3, 40 x 11008 x 4096 32.4 / 30.8.  Not where the
-// columns are more than a workgroup's for every compute unit, whose tokens come from the L2 once more for each (1 x 4096 x 11008 20.6 / 21.1, 40 25.8 / 30.5), nor
-// for wide adapters, whose ranks are added one by one (8 x 8192 x 1024 at rank 64 22.3 / 23.7, 64 x 256 x 256 at rank 128 25.7 / 39).  With the tokens row by row
-// instead of as the matrix instruction takes them 40 x 4096 x 4096 16.4, with 32 columns a workgroup 20.5, with eight steps in flight 16.8.
+// Tokens x K x N, one-token segments, us, with the tiled product (q8.hip, gemm_tile_q8.hip) / these: rank 16, 1 x 4096 x 4096 13.6 / 9.6, 16 of them 15.3 / 10.9, 40
+// 15.4 / 13.3, 64 16.6 / 15.5; 64 x 1376 x 4096 14.0 / 10.5, 64 x 512 x 512 10.9 / 9.3, 32 x 2048 x 2048 12.3 / 9.0, 64 x 11008 x 4096 29.7 / 26.4; 1 x 4096 x 8192 15.9 / 12.4, 16 18.3 / 14.9,
+// 40 18.9 / 20.8.  Not where the columns are more than two workgroups' for every compute unit, each of which takes the tokens from the L2 once more (1 x 4096 x 11008 16.7 / 16.7, 16
+// 18.8 / 19.8, 40 20.2 / 27.3), nor for wide adapters, whose ranks are added one by one (rank 64, 1 x 4096 x 4096 16.9 / 14.3, 8 18.3 / 18.6, 40 19.5 / 22.6; rank 128, 8 x 1024 x 1024
+// 15.8 / 19.4).  Three pieces of W on their way instead of two 13.8 (40 x 4096 x 4096), tokens row by row instead of as the matrix instruction takes them 0.7 more, 32 columns a
+// workgroup half as much again.
 #include "gemm_common.h"
 #include "kernels.h"
 #include "q8_rows.h"
@@ -81,13 +84,15 @@ __global__ __launch_bounds__(64 * kWaves)
 void q8_few_kernel(PlanDev pd, const uint8_t* __restrict__ Z, const float* __restrict__ z_scale, const uint8_t* __restrict__ W,
                    const float* __restrict__ w_scale, const float* __restrict__ P, const uint16_t* __restrict__ B, uint16_t* __restrict__ y, int32_t pitch)
 {
-    constexpr int U = 4;                             // steps of 64 k whose operands are in flight
-    static_assert(NBT <= kWaves, "a wave ends a block of tokens");
-    __shared__ i32x4 red[kWaves][NBT][64];
+    constexpr int U = kQ8Pad / 64;                   // steps of 64 k to a piece of K
+    static_assert(NBT <= kWaves && NBT <= 4, "a wave ends a block of tokens, and its sums lie where it has turned W");
+    __shared__ i32x4 own[kWaves][256];               // a wave's: 256 k of 16 columns, chunk c of column r at 16 r + (c ^ r); then its sums [block][lane]
     const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int32_t(threadIdx.x >> 6));
     const int32_t j = lane & 15, kg = lane >> 4, T = pd.T, N = pd.d_out, col0 = int32_t(blockIdx.x) * 16;
-    const int32_t steps = pitch / 64, first = steps * wave / kWaves, last = steps * (wave + 1) / kWaves;
-    const uint8_t* const wp = W + size_t(min(col0 + j, N - 1)) * pitch + 16 * kg;
+    const int32_t pieces = pitch / kQ8Pad, first = pieces * wave / kWaves, last = pieces * (wave + 1) / kWaves;
+    const uint8_t* wp[U];                            // four columns a load, whole lines of each
+#pragma unroll
+    for (int i = 0; i < U; ++i) wp[i] = W + size_t(min(col0 + 4 * i + (lane >> 4), N - 1)) * pitch + 16 * j;
     const uint8_t* zp[NBT];
 #pragma unroll
     for (int b = 0; b < NBT; ++b) zp[b] = Z + size_t(b) * 16 * pitch + 16 * lane;        // (rows beyond T: whatever is there, which goes nowhere)
@@ -103,24 +108,38 @@ void q8_few_kernel(PlanDev pd, const uint8_t* __restrict__ Z, const float* __res
         seg_r0 = cseg_rank(pd)[lane];
         seg_r = cseg_rank(pd)[pd.nseg + lane];
     }
-    // (steps beyond the last repeat it, with W taken as 0)
-    for (int32_t k = first; k < last; k += U) {
-        i32x4 w[U], z[U][NBT];
+    i32x4 w[U], z[U][NBT], wn[U], zn[U][NBT];
+    auto load = [&](int32_t g, i32x4 (&wv)[U], i32x4 (&zv)[U][NBT]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wp + min(k + u, last - 1) * 64));
+        for (int i = 0; i < U; ++i) wv[i] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wp[i] + g * kQ8Pad));
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int b = 0; b < NBT; ++b) z[u][b] = *reinterpret_cast<const i32x4*>(zp[b] + min(k + u, last - 1) * 1024);
+            for (int b = 0; b < NBT; ++b) zv[u][b] = *reinterpret_cast<const i32x4*>(zp[b] + (g * U + u) * 1024);
+    };
+    if (first < last) load(first, w, z);
+    for (int32_t g = first; g < last; ++g) {
+        if (g + 1 < last) load(g + 1, wn, zn);
+        // (the wave's own part of LDS, whose operations are carried out in order)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (k + u >= last) w[u] = i32x4{0, 0, 0, 0};
+        for (int i = 0; i < U; ++i) own[wave][16 * (4 * i + (lane >> 4)) + (j ^ (4 * i + (lane >> 4)))] = w[i];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = own[wave][16 * j + ((4 * u + kg) ^ j)];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int b = 0; b < NBT; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], z[u][b], acc[b], 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            w[u] = wn[u];
+#pragma unroll
+            for (int b = 0; b < NBT; ++b) z[u][b] = zn[u][b];
         }
     }
 #pragma unroll
-    for (int b = 0; b < NBT; ++b) red[wave][b][lane] = acc[b];
+    for (int b = 0; b < NBT; ++b) own[wave][64 * b + lane] = acc[b];
     // the adapter term of the wave's block, while the others arrive
     const int32_t row = 16 * wave + j, col = col0 + 4 * kg;
     float up[4] = {0.f, 0.f, 0.f, 0.f};
@@ -167,9 +186,9 @@ void q8_few_kernel(PlanDev pd, const uint8_t* __restrict__ Z, const float* __res
     }
     __syncthreads();
     if (!mine) return;
-    i32x4 sum = red[0][wave][lane];
+    i32x4 sum = own[0][64 * wave + lane];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) sum = sum + red[w][wave][lane];
+    for (int w = 1; w < kWaves; ++w) sum = sum + own[w][64 * wave + lane];
     const float zs = z_scale[row];
     const f32x4 ws = *reinterpret_cast<const f32x4*>(w_scale + col);
     bf16x4 o;
@@ -197,6 +216,7 @@ hipError_t q8_few_rows(const PlanDev& pd, const void* x, const void* A, const fl
 hipError_t q8_few(const PlanDev& pd, const void* Z, const float* z_scale, const void* W, const float* w_scale, const float* P, const void* B, void* y,
                   hipStream_t st)
 {
+    static_assert(kQ8FewTokens <= 64, "four blocks of 16 tokens");
     if (pd.T < 1 || pd.T > kQ8FewTokens || pd.nseg > 64) return hipErrorInvalidValue;
     const dim3 grid(uint32_t((pd.d_out + 15) / 16));
 #define LOBRA_FEW(NBT) \
@@ -204,7 +224,8 @@ hipError_t q8_few(const PlanDev& pd, const void* Z, const float* z_scale, const 
                                                     static_cast<const uint16_t*>(B), static_cast<uint16_t*>(y), int32_t(q8_pitch(pd.d_in)))
     if (pd.T <= 16) LOBRA_FEW(1);
     else if (pd.T <= 32) LOBRA_FEW(2);
-    else LOBRA_FEW(3);
+    else if (pd.T <= 48) LOBRA_FEW(3);
+    else LOBRA_FEW(4);
 #undef LOBRA_FEW
     return hipGetLastError();
 }

@@ -421,6 +421,8 @@ def test_scales_far_apart(T, std_x, std_w):
 @pytest.mark.parametrize("T,d_in,d_out,ranks,batch,n_proj", [
     (1, 264, 8, [4], "one", 1), (16, 520, 1032, [16, 8, 3], "tokens", 1), (17, 9000, 264, [16, 8], "tokens", 1), (31, 1376, 4096, [32, 5], "mixed", 1),
     (48, 4096, 72, [8, 16, 1, 32], "tokens", 1), (48, 256, 4096, [16], "bare", 1), (33, 768, 1536, [8], "tokens", 3), (48, 512, 2064, [16, 8], "mixed", 2),
+    (64, 512, 264, [16, 8], "tokens", 1), (65, 512, 264, [16, 8], "tokens", 1), (64, 1024, 4096, [16], "bare", 1), (16, 512, 8192, [16, 8], "tokens", 1),
+    (17, 512, 4104, [16, 8], "tokens", 1), (16, 264, 8200, [16, 8], "tokens", 1), (15, 2304, 6144, [8], "tokens", 3), (50, 264, 1032, [32, 8], "tokens", 1),
     (49, 512, 264, [16, 8], "tokens", 1), (48, 512, 4104, [16, 8], "tokens", 1), (48, 512, 264, [33, 8], "tokens", 1), (40, 512, 520, [], "tokens", 1),
 ])
 def test_few_tokens(T, d_in, d_out, ranks, batch, n_proj):
