@@ -126,6 +126,13 @@ lobra_status lobra_beam_reorder(const lobra_beam_state* states, int32_t n_states
         if (!t.src || !t.dst) return LOBRA_ERR_NULL;
         const uintptr_t a = reinterpret_cast<uintptr_t>(t.src), b = reinterpret_cast<uintptr_t>(t.dst);
         if (a != b && (a < b ? b - a : a - b) < uintptr_t(bytes)) return LOBRA_ERR_SHAPE;
+        // nothing that one tensor writes is another's (they run side by side)
+        for (int32_t j = 0; j < i; ++j) {
+            const uintptr_t c = reinterpret_cast<uintptr_t>(states[j].src), d = reinterpret_cast<uintptr_t>(states[j].dst);
+            const uintptr_t own = uintptr_t(bytes), other = uintptr_t(states[j].row_bytes) * uintptr_t(rows);
+            const auto meet = [&](uintptr_t p, uintptr_t q) { return p < q + other && q < p + own; };
+            if (other > 0 && (meet(b, d) || meet(b, c) || meet(a, d))) return LOBRA_ERR_SHAPE;
+        }
     }
     if (!any) return LOBRA_OK;
     if (!parent) return LOBRA_ERR_NULL;

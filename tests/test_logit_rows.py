@@ -476,6 +476,21 @@ def test_on_another_stream_and_in_a_graph():
         assert all(torch.equal(eager[i], graphed[i]) for i in eager), r
 
 
+def test_reorder_of_tensors_that_meet():
+    """Two tensors of a list where one writes what is the other's too; six rows of 64 bytes."""
+    L, p = bd.lib(), 1 << 20
+
+    def R(*pairs):
+        t = (bd.BeamState * len(pairs))(*(bd.BeamState(a, b, 64, 8) for a, b in pairs))
+        return L.lobra_beam_reorder(t, len(pairs), 2, 3, None, 3, None, None)
+
+    for pairs in (((p, p), (p, p)), ((p, p), (p + 383, p + 383)), ((p, p + 4096), (p + 8192, p + 4096)), ((p, p + 4096), (p + 4096 + 64, p + 8192)),
+                  ((p, p), (p + 4096, p + 4096), (p, p + 8192)), ((p + 4096, p + 8192), (p, p + 4096 + 383))):
+        assert R(*pairs) == -2, pairs
+    # (as far as the missing parents)
+    assert R((p, p), (p + 384, p + 384)) == -1 and R((p, p + 4096), (p, p + 8192)) == -1 and R((p, p + 384), (p + 768, p + 1152)) == -1
+
+
 def test_host_tensors():
     """What lies in host memory is refused before anything is launched."""
     z, f, i = torch.zeros(3, 100).bfloat16(), torch.zeros(3, 5), torch.zeros(3, 5, dtype=torch.int32)

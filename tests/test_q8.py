@@ -445,3 +445,20 @@ def test_host_tensors_and_short_ones():
     for bad in (dict(dA=f[:23]), dict(dB=f[:23]), dict(A=a[:23]), dict(s=s[:1]), dict(h_saved=short)):
         with pytest.raises(AssertionError):
             bd.lobra_mlora_quant_bwd(plan, **{**bwd, **bad})
+
+
+@pytest.mark.gpu
+def test_no_tokens():
+    """Nothing is read; the gradients are those of nothing."""
+    plan = bd.Plan("bf16", 0, 64, 72, [0, 8], [0], [])
+    fwd, bwd = bd.lobra_mlora_quant_workspace_bytes(plan)
+    assert fwd == 0
+    dA, dB = torch.full((8, 64), 7.0, device=DEV), torch.full((8, 72), 7.0, device=DEV)
+    W = torch.randn(64, 72, device=DEV).bfloat16()
+    wq, ws = weight(None, W, 64, 72)
+    A, B, s = torch.ones(8, 64, device=DEV).bfloat16(), torch.ones(8, 72, device=DEV).bfloat16(), torch.ones(1, device=DEV)
+    e = torch.empty(0, 64, device=DEV).bfloat16()
+    bd.lobra_mlora_quant_fwd(plan, e, wq, ws, A, B, s, torch.empty(0, 72, device=DEV).bfloat16())
+    bd.lobra_mlora_quant_bwd(plan, e, wq, ws, A, B, s, torch.empty(0, 72, device=DEV).bfloat16(), None, e, dA, dB, 0, torch.empty(max(bwd, 16), dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    assert bool((dA == 0).all()) and bool((dB == 0).all())
