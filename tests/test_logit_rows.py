@@ -279,7 +279,8 @@ def ref_select(z, score, done, done_token, k):
     (1, 1, 1, 1, "plain", 0), (2, 3, 2, 8, "plain", 0), (1, 4, 32000, 4, "plain", 0), (3, 5, 4099, 10, "plain", 3), (40, 2, 8192, 4, "plain", 0), (2, 4, 8193, 8, "plain", 1),
     (3, 8, 20001, 16, "offset", 0), (2, 16, 1000, 32, "plain", 0), (2, 32, 30, 32, "plain", 2), (2, 4, 5000, 32, "masked", 0), (2, 3, 9000, 8, "lowest", 0),
     (2, 4, 20000, 32, "equal", 0), (2, 2, 40960, 32, "constant", 0), (3, 4, 3001, 8, "twins", 0), (2, 4, 3000, 4, "nan", 0), (5, 4, 50257, 8, "first", 0),
-    (7, 4, 500, 4, "done", 0), (2, 3, 70, 8, "none", 0), (1, 2, 300000, 32, "one_stride", 0),
+    (7, 4, 500, 4, "done", 0), (2, 3, 70, 8, "none", 0), (1, 2, 300000, 32, "one_stride", 0), (2, 16, 70000, 32, "plain", 0), (1, 32, 40000, 32, "ahead", 1),
+    (1, 16, 90000, 17, "ahead", 0), (1, 16, 70000, 32, "equal", 0),
 ])
 def test_beam_select(dtype, n, b, V, k, kind, pad):
     z = logits_of(kind if kind in ("offset", "masked", "lowest", "equal", "nan", "one_stride") else "plain", n * b, V, dtype, n + b + V)
@@ -294,6 +295,8 @@ def test_beam_select(dtype, n, b, V, k, kind, pad):
         score[:] = score[:, :1]
     elif kind == "first":
         score[:, 1:] = -math.inf
+    elif kind == "ahead":                            # one beam far in front of the others
+        score -= 30 * (torch.arange(b) != b // 2)
     elif kind == "done":
         done = (torch.rand(n, b, generator=g) < 0.6).int()
         done[0] = 1
