@@ -505,3 +505,35 @@ def test_host_tensors():
                  lambda: bd.lobra_beam_reorder([(z, z)], 1, 3, par, stream=0)):
         with pytest.raises(AssertionError, match="host tensor"):
             call()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("noise", [0.05, 0.7])
+@pytest.mark.parametrize("T,V,k,temperature", [(60, 16064, 4, 2.0), (9, 20099, 32, 2.0), (30, 70528, 1, 2.0), (3, 108864, 1, 2.0), (50, 3001, 64, 0.7), (40, 2048, 10, 1.0)])
+def test_distill_of_nearly_the_same_model(dtype, noise, T, V, k, temperature):
+    """A loss far below 1, terms near 1 that cancel, with a tail.  Only the sum over what is not listed is in fp32.  A relative error e of it moves
+    ln S by p_r e and ln p_r by (1 - p_r) e, so the loss by (sum q p_r - q_r (1 - p_r)) e = (p_r - q_r) e; the loss itself is rounded once more, by 2^-24.  e, in units of 2^-24: 4 for
+    each unit of the exponents, weighted as the sum weighs them (difference, scale's own two roundings, product), 2 for the exponential, one an addition (up to 64 or V / 512 in a
+    thread, 14 behind it), 24 for rescaling on the way."""
+    g = torch.Generator().manual_seed(V)
+    z = (torch.randn(T, V, generator=g) * 2.5).to(DT[dtype])
+    z[torch.arange(T), torch.randint(0, V, (T,), generator=g)] += (torch.rand(T, generator=g) * 16).to(DT[dtype])
+    teacher = (z.double() + noise * torch.randn(T, V, generator=g)) / temperature
+    tl, ids = torch.log_softmax(teacher, dim=1).topk(k, dim=1)
+    tl, ids = tl.float(), ids.int()
+    held = float(np.float32(temperature))            # (what the descriptor holds)
+    want, _, _ = ref_distill(z, tl, ids, True, held)
+    x = z.double() / held * math.log2(math.e)
+    x = x - x.max(dim=1, keepdim=True).values
+    e = torch.exp2(x)
+    rest = e.scatter(1, ids.long(), 0.0)
+    p_r, q_r = rest.sum(dim=1) / e.sum(dim=1), 1 - tl.double().exp().sum(dim=1)
+    size = (rest * x.abs()).sum(dim=1) / rest.sum(dim=1)
+    off = 2.0 ** -24 * (want.abs() + (4 * size + 2 + max(64, V / 512) + 14 + 24) * (p_r - q_r).abs()) + 4e-13          # (in 64 bits: some hundred terms of up to 30)
+    loss = torch.empty(T, device=DEV)
+    bd.lobra_token_distill_fwd(bd.make_distill_desc(dtype, T, V, k, tail=True, temperature=temperature), z.to(DEV), tl.to(DEV), ids.to(DEV), loss)
+    got = loss.double().cpu()
+    print("%s V %d noise %g: losses of %.1e, off by %.1e of themselves, allowed %.1e" % (
+        dtype, V, noise, float(want.abs().median()), float((got - want).norm() / want.norm()), float(off.norm() / want.norm())))
+    assert bool(((got - want).abs() <= off).all()), ((got - want).abs() / off).max()
