@@ -249,18 +249,23 @@ def _typed(t, kind, least=0):
 _current_device = None
 
 
-def _here(t):
-    """t, which has to lie on the device that the call is launched on: the current one."""
+def _here(*tensors):
+    """All tensors of a call have to lie on the device that it is launched on: the current one."""
     global _current_device
-    if t is not None and not isinstance(t, int):
-        device = t.get_device()
-        assert device >= 0, "a host tensor where the library reads or writes device memory"
+    device = None
+    for t in tensors:
+        if t is not None and t.__class__ is not int:
+            d = t.get_device()
+            if d != device:
+                assert d >= 0, "a host tensor where the library reads or writes device memory"
+                assert device is None, "tensors of different devices"
+                device = d
+    if device is not None:
         if _current_device is None:
             import torch
             torch.cuda.current_device()           # (initialises, or says why it can't)
             _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         assert device == _current_device(), "a tensor of another device than the current one"
-    return t
 
 
 _current_stream = None
@@ -598,8 +603,9 @@ def lobra_quantise_weight(W, Wq, w_scale, stream=None, check=True):
     assert kind is not None, "a weight of another type than fp32 and bf16"
     assert d_out <= 1 or W.stride(1) == 1, "rows of a weight must be contiguous"
     assert Wq.shape == (d_out, lobra_quant_pitch(d_in)), "Wq of another shape than [d_out, lobra_quant_pitch(d_in)]"
-    st = lib().lobra_quantise_weight(kind, d_in, d_out, W.stride(0) if d_in > 1 else 0, _here(W).data_ptr(), _typed(Wq, "int8"),
-                                        _typed(w_scale, "fp32", d_out), _stream(stream))
+    args = W.data_ptr(), _typed(Wq, "int8"), _typed(w_scale, "fp32", d_out)
+    _here(W, Wq, w_scale)
+    st = lib().lobra_quantise_weight(kind, d_in, d_out, W.stride(0) if d_in > 1 else 0, *args, _stream(stream))
     if check:
         _check(st, "lobra_quantise_weight")
     return st
@@ -614,7 +620,7 @@ def lobra_mlora_quant_workspace_bytes(plan: Plan):
 
 def _quant_operands(plan: Plan, x, Wq, w_scale, A, B, s):
     R = plan.R_tot
-    return (_typed(x if plan.host_only else _here(x), plan.kind, plan.T * plan.d_in), _typed(Wq, "int8", plan.d_out * lobra_quant_pitch(plan.d_in)),
+    return (_typed(x, plan.kind, plan.T * plan.d_in), _typed(Wq, "int8", plan.d_out * lobra_quant_pitch(plan.d_in)),
             _typed(w_scale, "fp32", plan.d_out), _typed(A, plan.kind, R * plan.d_in), _typed(B, plan.kind, R * (plan.d_out // plan.desc.n_proj)),
             _typed(s, "fp32", plan.n_tasks))
 
@@ -626,8 +632,10 @@ def _saved(plan: Plan, h):
 
 def lobra_mlora_quant_fwd(plan: Plan, x, Wq, w_scale, A, B, s, y, h_save=None, ws=None, stream=None, check=True):
     """y = x W + s_t (A_t x) B_t with W and x in 8-bit integers in the first product.  Returns the status."""
-    st = lib().lobra_mlora_quant_fwd(plan.handle, *_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(y, plan.kind, plan.T * plan.d_out),
-                                  _saved(plan, h_save), _ptr(ws), _nbytes(ws), _stream(stream))
+    args = (*_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(y, plan.kind, plan.T * plan.d_out), _saved(plan, h_save), _ptr(ws))
+    if not plan.host_only:
+        _here(x, Wq, w_scale, A, B, s, y, h_save, ws)
+    st = lib().lobra_mlora_quant_fwd(plan.handle, *args, _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_mlora_quant_fwd")
     return st
@@ -636,9 +644,11 @@ def lobra_mlora_quant_fwd(plan: Plan, x, Wq, w_scale, A, B, s, y, h_save=None, w
 def lobra_mlora_quant_bwd(plan: Plan, x, Wq, w_scale, A, B, s, dy, h_saved, dx, dA, dB, flags=0, ws=None, stream=None, check=True):
     """dx, dA, dB of the layer on an 8-bit base.  Returns the status."""
     e, T, R = plan.kind, plan.T, plan.R_tot
-    st = lib().lobra_mlora_quant_bwd(plan.handle, *_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(dy, e, T * plan.d_out), _saved(plan, h_saved),
-                                  _typed(dx, e, T * plan.d_in), _typed(dA, "fp32", R * plan.d_in), _typed(dB, "fp32", R * (plan.d_out // plan.desc.n_proj)),
-                                  int(flags), _ptr(ws), _nbytes(ws), _stream(stream))
+    args = (*_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(dy, e, T * plan.d_out), _saved(plan, h_saved), _typed(dx, e, T * plan.d_in),
+            _typed(dA, "fp32", R * plan.d_in), _typed(dB, "fp32", R * (plan.d_out // plan.desc.n_proj)), int(flags), _ptr(ws))
+    if not plan.host_only:
+        _here(x, Wq, w_scale, A, B, s, dy, h_saved, dx, dA, dB, ws)
+    st = lib().lobra_mlora_quant_bwd(plan.handle, *args, _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_mlora_quant_bwd")
     return st
@@ -658,8 +668,9 @@ def _teacher(desc: DistillDesc, teacher_logp, teacher_id):
 def lobra_token_distill_fwd(desc: DistillDesc, logits, teacher_logp, teacher_id, loss, stat=None, stream=None, check=True):
     """loss [T] of every row against the teacher's tokens [T, top_k]; stat (fp32 [T, 4]) for backward.  Returns the status."""
     T = desc.T
-    st = lib().lobra_token_distill_fwd(ctypes.byref(desc), _rows_ptr(_here(logits), desc), *_teacher(desc, teacher_logp, teacher_id), _typed(loss, "fp32", T),
-                                       _typed(stat, "fp32", 4 * T), _stream(stream))
+    args = (_rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id), _typed(loss, "fp32", T), _typed(stat, "fp32", 4 * T))
+    _here(logits, teacher_logp, teacher_id, loss, stat)
+    st = lib().lobra_token_distill_fwd(ctypes.byref(desc), *args, _stream(stream))
     if check:
         _check(st, "lobra_token_distill_fwd")
     return st
@@ -668,8 +679,9 @@ def lobra_token_distill_fwd(desc: DistillDesc, logits, teacher_logp, teacher_id,
 def lobra_token_distill_bwd(desc: DistillDesc, logits, teacher_logp, teacher_id, stat, dloss, dlogits, flags=0, stream=None, check=True):
     """dlogits (may be logits) from dloss [T].  Returns the status."""
     T = desc.T
-    st = lib().lobra_token_distill_bwd(ctypes.byref(desc), _rows_ptr(_here(logits), desc), *_teacher(desc, teacher_logp, teacher_id),
-                                       _typed(stat, "fp32", 4 * T), _typed(dloss, "fp32", T), _rows_ptr(dlogits, desc), int(flags), _stream(stream))
+    args = (_rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id), _typed(stat, "fp32", 4 * T), _typed(dloss, "fp32", T), _rows_ptr(dlogits, desc))
+    _here(logits, teacher_logp, teacher_id, stat, dloss, dlogits)
+    st = lib().lobra_token_distill_bwd(ctypes.byref(desc), *args, int(flags), _stream(stream))
     if check:
         _check(st, "lobra_token_distill_bwd")
     return st
@@ -689,9 +701,10 @@ def lobra_beam_workspace_bytes(desc: BeamDesc) -> int:
 def lobra_beam_select(desc: BeamDesc, logits, score, done, done_token, out_score, out_beam, out_token, ws, stream=None, check=True):
     """The n_out best continuations of every request: scores, beams within the request, tokens.  Returns the status."""
     rows, n = desc.n_req * desc.beams, desc.n_req * desc.n_out
-    st = lib().lobra_beam_select(ctypes.byref(desc), _rows_ptr(_here(logits), desc, rows), _typed(score, "fp32", rows), _typed(done, "int32", rows),
-                                 int(done_token), _typed(out_score, "fp32", n), _typed(out_beam, "int32", n), _typed(out_token, "int32", n), _ptr(ws),
-                                 _nbytes(ws), _stream(stream))
+    args = (_rows_ptr(logits, desc, rows), _typed(score, "fp32", rows), _typed(done, "int32", rows), int(done_token), _typed(out_score, "fp32", n),
+            _typed(out_beam, "int32", n), _typed(out_token, "int32", n), _ptr(ws))
+    _here(logits, score, done, out_score, out_beam, out_token, ws)
+    st = lib().lobra_beam_select(ctypes.byref(desc), *args, _nbytes(ws), _stream(stream))
     if check:
         _check(st, "lobra_beam_select")
     return st
@@ -700,24 +713,32 @@ def lobra_beam_select(desc: BeamDesc, logits, score, done, done_token, out_score
 def lobra_beam_reorder(states, n_req, beams, parent, used=None, stream=None, check=True):
     """states: [(src, dst)] of tensors [n_req * beams, ...] of any type, dst may be src; with `used` (int32 [n_req]) only the first used positions
     (dimension 1) of a request's rows move.  parent: int32 [n_req, >= beams], whose rows may lie in wider ones.  Returns the status."""
-    rows, vals = n_req * beams, []
+    rows, vals, where = n_req * beams, [], [parent, used]
     for src, dst in states:
         shape = src.shape
-        assert src.dtype is dst.dtype and shape == dst.shape, "a state that goes to a tensor of another type or shape"
         assert shape[0] == rows, "a state of another number of rows than beams"
-        assert src.is_contiguous() and dst.is_contiguous(), "tensors must be contiguous"
+        assert src.is_contiguous(), "tensors must be contiguous"
+        at = to = src.data_ptr()
+        if dst is not src:
+            assert src.dtype is dst.dtype and shape == dst.shape, "a state that goes to a tensor of another type or shape"
+            assert dst.is_contiguous(), "tensors must be contiguous"
+            to = dst.data_ptr()
+            where.append(dst)
         row = src.nbytes // rows if rows else 0
         unit = 0
         if used is not None:
             assert len(shape) >= 2, "a state without positions"
             unit = row // (shape[1] or 1)
-        vals += (src.data_ptr(), dst.data_ptr(), row, unit)
+        where.append(src)
+        vals += (at, to, row, unit)
     arr = (ctypes.c_int64 * max(len(vals), 4))(*vals)          # (as BeamState has them)
     assert parent.dtype is _torch_types["int32"] and parent.dim() == 2 and parent.shape[0] == n_req and parent.shape[1] >= beams, \
         "parents other than int32 [n_req, beams]"
     assert parent.shape[1] <= 1 or parent.stride(1) == 1, "rows of parents must be contiguous"
-    st = lib().lobra_beam_reorder(arr, len(states), int(n_req), int(beams), _here(parent).data_ptr(), parent.stride(0) if n_req > 1 else int(beams),
-                                  _typed(used, "int32", n_req), _stream(stream))
+    limit = _typed(used, "int32", n_req)
+    _here(*where)
+    st = lib().lobra_beam_reorder(arr, len(states), int(n_req), int(beams), parent.data_ptr(), parent.stride(0) if n_req > 1 else int(beams), limit,
+                                  _stream(stream))
     if check:
         _check(st, "lobra_beam_reorder")
     return st
