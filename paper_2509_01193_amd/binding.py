@@ -602,6 +602,7 @@ def lobra_quantise_weight(W, Wq, w_scale, stream=None, check=True):
     kind = {str(_torch_types["fp32"]): F32, str(_torch_types["bf16"]): BF16}.get(str(W.dtype))
     assert kind is not None, "a weight of another type than fp32 and bf16"
     assert d_out <= 1 or W.stride(1) == 1, "rows of a weight must be contiguous"
+    assert d_in <= 1 or W.stride(0) >= d_out, "rows of a weight that overlap"
     assert Wq.shape == (d_out, lobra_quant_pitch(d_in)), "Wq of another shape than [d_out, lobra_quant_pitch(d_in)]"
     args = W.data_ptr(), _typed(Wq, "int8"), _typed(w_scale, "fp32", d_out)
     _here(W, Wq, w_scale)

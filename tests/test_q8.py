@@ -462,3 +462,13 @@ def test_no_tokens():
     bd.lobra_mlora_quant_bwd(plan, e, wq, ws, A, B, s, torch.empty(0, 72, device=DEV).bfloat16(), None, e, dA, dB, 0, torch.empty(max(bwd, 16), dtype=torch.uint8, device=DEV))
     torch.cuda.synchronize()
     assert bool((dA == 0).all()) and bool((dB == 0).all())
+
+
+def test_weights_whose_rows_overlap_are_refused():
+    """A row pitch below a row's length (a broadcast row has 0, which the library takes for rows back to back) would be read as d_in rows that are not there."""
+    q, s = torch.zeros(16, 256, dtype=torch.int8), torch.zeros(16)
+    for W in (torch.zeros(16).expand(8, 16), torch.zeros(1, 16).bfloat16().expand(8, 16), torch.zeros(64).as_strided((8, 16), (4, 1)), torch.zeros(1).expand(8, 16)):
+        with pytest.raises(AssertionError, match="rows of a weight"):
+            bd.lobra_quantise_weight(W, q, s, stream=0)
+    with pytest.raises(AssertionError, match="host tensor"):          # (a single row has no pitch)
+        bd.lobra_quantise_weight(torch.zeros(16).expand(1, 16), q, s, stream=0)
