@@ -23,6 +23,13 @@ from paper_2509_01193_amd import binding as lobra
 LR_GATE = 0.02
 
 
+def not_8_bits(dtype, d, f):
+    """Why a base of this type and these widths is not put into 8 bits; None if it is."""
+    if dtype != "bf16":
+        return "a base in 8-bit integers is one of bf16 layers"
+    return "layers wider than %d are not put into 8-bit integers" % lobra.MAX_QUANT_IN if max(d, f) > lobra.MAX_QUANT_IN else None
+
+
 class JointStep:
     """Buffers and plans of a batch whose packing stays: seg_off / seg_task as in the plan (-1: tokens without an adapter)."""
 
@@ -72,7 +79,12 @@ class JointStep:
         self.batch(seg_off, seg_task)
 
     def quantise_base(self):
-        """The frozen weights of the down projections and the head in 8-bit integers from here on; the others are not kept."""
+        """The frozen weights of the down projections and the head in 8-bit integers from here on; the others are not kept.  ValueError, and the weights as
+        they are, where that can't be."""
+        why = not_8_bits(self.dtype, self.d, self.f) if self.head8 is None else "the base is in 8-bit integers already"
+        if why:
+            raise ValueError(why)
+
         def quantised(W):
             d_in, d_out = W.shape
             q = torch.empty(d_out, lobra.lobra_quant_pitch(d_in), dtype=torch.int8, device=self.dev), torch.empty(d_out, device=self.dev)
@@ -243,6 +255,11 @@ def main(argv=None):
     ap.add_argument("--distill-steps", type=int, default=0, help="steps of new adapters on an 8-bit base, against the trained model's likeliest tokens")
     ap.add_argument("--beams", type=int, default=0, help="continue the prompts by beam search")
     args = ap.parse_args(argv)
+    why = not_8_bits(args.dtype, args.width, args.ffn) if args.distill_steps else None
+    if why:
+        ap.error("--distill-steps: " + why)
+    if not 0 <= args.beams <= lobra.MAX_TOP:
+        ap.error("--beams: 0 to %d" % lobra.MAX_TOP)
     n, T = len(args.ranks), len(args.ranks) * args.tokens
     gen = torch.Generator().manual_seed(1)
     # every task has a map of its own from a token to the next, over the tokens that occur
