@@ -202,6 +202,12 @@ __device__ __forceinline__ void mfma2_dma16_i8(bf16x8 a0, bf16x8 a1, bf16x8 b, u
                  : LOBRA_MFMA_CLOB_MEM);
 }
 
+// A whole sum times the scale of its channel, then that of its token, which is an ordinary number also where a product on the way is none: sums are below 2^31 and scales
+// 2^-126 at least, so nothing on the way is too small, and only a channel's scale above 2^96 makes it too large.  Such a scale is taken 2^64 times smaller (near_scale), and
+// the product with both made up for it (far_back, else 1: exact, so that all others are what they are without it).
+__device__ __forceinline__ float near_scale(float w_scale) { return w_scale > 0x1p96f ? w_scale * 0x1p-64f : w_scale; }
+__device__ __forceinline__ float far_back(float w_scale) { return w_scale > 0x1p96f ? 0x1p64f : 1.f; }
+
 // One register of an accumulator, written (the MFMAs behind it have to stay the documented wait states away).
 template <int R> __device__ __forceinline__ void acc_write(float v)
 {

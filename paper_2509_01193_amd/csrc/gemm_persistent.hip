@@ -531,20 +531,39 @@ void LOBRA_GP_KERNEL(PlanDev pd, const uint16_t* __restrict__ Z, const uint16_t*
 #if LOBRA_GP_Q8
         // whole sums -> fp32 (rounded once: they have up to 31 bits) times the scales
         {
+            const float* const wsp = w_scale + col0 + wn * TN;
             f32x4 ws[NB];
             float zs[MB];
+            bool far = false;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-                ws[nb] = *reinterpret_cast<const f32x4*>(w_scale + col0 + wn * TN + block_col(nb, 4 * kg));
+            for (int nb = 0; nb < NB; ++nb) {
+                ws[nb] = *reinterpret_cast<const f32x4*>(wsp + block_col(nb, 4 * kg));
+#pragma unroll
+                for (int v = 0; v < 4; ++v) far = far || far_back(ws[nb][v]) != 1.f, ws[nb][v] = near_scale(ws[nb][v]);
+            }
+            far = __any(far);                        // (uniform, and hardly ever: a product for every accumulator took 1 us a tile)
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) zs[mb] = z_scale[wrow0 + 16 * mb + j];
             static_for<0, MB>([&](auto mb_c) {
                 constexpr int mb = decltype(mb_c)::value;
+                float y[NB][4];
                 static_for<0, NB>([&](auto nb_c) {
                     constexpr int nb = decltype(nb_c)::value;
                     static_for<0, 4>([&](auto v_c) {
-                        constexpr int v = decltype(v_c)::value, reg = acc_reg(mb, nb) + v;
-                        acc_write<reg>(float(__float_as_int(acc_read<reg>())) * ws[nb][v] * zs[mb]);
+                        constexpr int v = decltype(v_c)::value;
+                        y[nb][v] = float(__float_as_int(acc_read<acc_reg(mb, nb) + v>())) * ws[nb][v] * zs[mb];
+                    });
+                });
+                if (far)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) y[nb][v] *= far_back(wsp[block_col(nb, 4 * kg) + v]);
+                static_for<0, NB>([&](auto nb_c) {
+                    constexpr int nb = decltype(nb_c)::value;
+                    static_for<0, 4>([&](auto v_c) {
+                        constexpr int v = decltype(v_c)::value;
+                        acc_write<acc_reg(mb, nb) + v>(y[nb][v]);
                     });
                 });
             });

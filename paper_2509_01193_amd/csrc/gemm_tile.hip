@@ -484,9 +484,16 @@ void tile_body(const PlanDev& pd, const uint16_t* __restrict__ Z, const uint16_t
 
 #if LOBRA_GT_Q8
     {
+        const float* const wsp = w_scale + col0 + wn * WTN + 4 * kg;
+        const int32_t last = N - 4 - (col0 + wn * WTN + 4 * kg);
         f32x4 ws[NB];
+        bool far = false;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) ws[nb] = *reinterpret_cast<const f32x4*>(w_scale + min(col0 + wn * WTN + nb * 16 + 4 * kg, N - 4));
+        for (int nb = 0; nb < NB; ++nb) {
+            ws[nb] = *reinterpret_cast<const f32x4*>(wsp + min(nb * 16, last));
+#pragma unroll
+            for (int v = 0; v < 4; ++v) far = far || far_back(ws[nb][v]) != 1.f, ws[nb][v] = near_scale(ws[nb][v]);
+        }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             const float zs = z_scale[min(row0 + wm * WTM + mb * 16 + j, T - 1)];
@@ -497,6 +504,15 @@ void tile_body(const PlanDev& pd, const uint16_t* __restrict__ Z, const uint16_t
                 for (int v = 0; v < 4; ++v) acc[mb][nb][v] = float(sum[v]) * ws[nb][v] * zs;
             }
         }
+        if (__any(far))                              // (uniform, and hardly ever)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const f32x4 w = *reinterpret_cast<const f32x4*>(wsp + min(nb * 16, last));
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[mb][nb][v] *= far_back(w[v]);
+            }
     }
 #endif
 

@@ -193,7 +193,11 @@ void q8_few_kernel(PlanDev pd, const uint8_t* __restrict__ Z, const float* __res
     const f32x4 ws = *reinterpret_cast<const f32x4*>(w_scale + col);
     bf16x4 o;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) o[v] = (__bf16)(float(sum[v]) * ws[v] * zs + up[v]);
+    for (int v = 0; v < 4; ++v) {
+        // (a large scale of a channel last: nothing on the way leaves the range, see near_scale; the sum with the adapter's term is one rounding)
+        const bool far = ws[v] > 0x1p96f;
+        o[v] = (__bf16)(float(sum[v]) * (far ? zs : ws[v]) * (far ? ws[v] : zs) + up[v]);
+    }
     *reinterpret_cast<bf16x4*>(y + size_t(row) * N + col) = o;
 }
 

@@ -472,3 +472,37 @@ def test_weights_whose_rows_overlap_are_refused():
             bd.lobra_quantise_weight(W, q, s, stream=0)
     with pytest.raises(AssertionError, match="host tensor"):          # (a single row has no pitch)
         bd.lobra_quantise_weight(torch.zeros(16).expand(1, 16), q, s, stream=0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,f,ranks,n_proj", [
+    (40, 512, 264, [], 1), (40, 512, 264, [8], 1), (100, 1024, 264, [8], 1), (200, 512, 512, [8], 2), (300, 512, 128, [], 1), (700, 512, 264, [8], 1), (1500, 768, 1032, [], 1),
+    (4500, 512, 1024, [8], 1),
+])
+def test_scales_of_every_size(T, d, f, ranks, n_proj):
+    """Channels and tokens between 1e-34 and 1e37 side by side: where a product of both is an ordinary number it is that number, whatever lies on the way to it."""
+    v, off, task, rank_off = make(T, d, f, ranks, "one", n_proj)
+    tokens, channels = (1e-34, 1.0, 1e30, 1e-20), (1e37, 1.0, 1e-30, 1e33, 1e20)
+    v["x"] = (v["x"].double() * torch.tensor(tokens)[torch.arange(T) % len(tokens)][:, None].double()).bfloat16()
+    v["W"] = (v["W"].double() * torch.tensor(channels)[torch.arange(f) % len(channels)].double()).bfloat16()
+    v["A"].zero_()
+    q, xs = quantised(v["x"])
+    wq, wsc = quantised(v["W"].t())
+    ref = (q @ wq.t()) * xs * wsc[:, 0]
+    dv = on_device(v)
+    Wq, ws = weight(None, dv["W"], d, f)
+    plan = bd.Plan("bf16", T, d, f, rank_off if ranks else None, off, task, n_proj=n_proj)
+    fwd, _ = bd.lobra_mlora_quant_workspace_bytes(plan)
+    wsb, h = torch.empty(fwd, dtype=torch.uint8, device=DEV), torch.empty(max(plan.h_save_bytes, 16), dtype=torch.uint8, device=DEV)
+    top = torch.finfo(torch.bfloat16).max
+    for kept in (None, h):
+        y = torch.empty(T, f, dtype=torch.bfloat16, device=DEV)
+        bd.lobra_mlora_quant_fwd(plan, dv["x"], Wq, ws, *((dv["A"], dv["B"], dv["s"]) if ranks else (None,) * 3), y, kept, wsb)
+        got = y.double().cpu()
+        # whole sums, three roundings of 2^-24 (six where splits of a sum are added), one to bf16; below the normal numbers nothing is promised
+        good = (got - ref).abs() <= HALF * (1 + 2.0 ** -12) * ref.abs() + 2.0 ** -126
+        split = (got - ref).abs() <= HALF * ref.abs() + 2e-6 * ((q.abs() @ wq.abs().t()) * xs * wsc[:, 0]) + 2.0 ** -126
+        large = ref.abs() > top * (1 - HALF)
+        good = torch.where(large, (got * ref.sign() >= top * (1 - HALF)), good | split)
+        assert bool(good.all()), (int((~good).sum()), good.numel(), got[~good][:4].tolist(), ref[~good][:4].tolist())
+        assert int(large.sum()) > 0 and int(((ref.abs() > 1) & ~large).sum()) > T * f // 10
