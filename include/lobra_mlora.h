@@ -470,7 +470,8 @@ LOBRA_API lobra_status lobra_token_distill_bwd(const lobra_distill_desc *desc, c
                                      void *hip_stream);
 
 /* A step of beam search: of every request the n_out best continuations over its beams and the vocabulary.  A beam b of score s continued by
- * token j has s + ln softmax(z_b)_j, in fp64; the largest come first, among equals the lowest beam, then the lowest token.  No continuations:
+ * token j has s + ln softmax(z_b)_j, in fp64; the largest come first, among equals the lowest beam, then the larger logit (a score far larger than
+ * the logits leaves nothing of them in a sum), then the lowest token.  No continuations:
  * logits of -inf; a beam whose score is -inf or NaN (its logits are not looked at); a beam whose logits hold NaN or +inf.
  *   logits      : device, row (request * beams + beam) at logits + row ld elements, 16-byte aligned (ld need not keep the rows aligned)
  *   score       : device fp32 [n_req, beams], the beams' scores so far (-inf: no beam, as all but one at a request's first step)

@@ -24,6 +24,7 @@ constexpr int kThreads = 256;
 constexpr int kPartBytes = 16384;
 template <typename E> constexpr int kPart = kPartBytes / int(sizeof(E));
 constexpr int kPackets = 128;             // 16 bytes each of a part's logits that may hold one of the best
+static_assert(LOBRA_MAX_VOCAB <= 1 << 24 && LOBRA_MAX_TOP <= 256, "a token's and a beam's bits in a continuation's place");
 constexpr int kList = 512;                // of a part's logits, or a request's continuations, that may be among the best
 
 // 16 bytes of a row that may begin at any element.
@@ -193,7 +194,9 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
     }
 }
 
-// A continuation as two numbers: its value's order, and beam and token, the lower the better.
+// A continuation as two numbers: its value's order, and beam, logit and token, the lower the better: 5 bits of beam, the logit's order from the largest down, 24 bits of
+// token (of a beam that is done: of no token).  Within a beam the logits' order is the values', also where those are equal in 64 bits because the score is far larger than
+// a logit, so that what a part hands on is what the request wants of it.
 struct Next {
     uint64_t order, place;
     __device__ __forceinline__ bool operator>(const Next& o) const { return order > o.order || (order == o.order && place < o.place); }
@@ -259,8 +262,9 @@ void beam_merge_kernel(BeamShape sh, const float* score, const int32_t* __restri
     auto value = [&](int32_t i, uint64_t key) {      // continuation i; order 0: there is none
         const int32_t beam = i / per, k = kind[beam];
         const double o = offset[beam];
-        if (k == 1 && key != 0) return Next{double_order(o + double(key_value(key))), uint64_t(beam) << 32 | uint32_t(key_index(key))};
-        if (k == 2 && i == beam * per) return Next{double_order(o), uint64_t(beam) << 32 | uint32_t(done_token)};
+        if (k == 1 && key != 0)
+            return Next{double_order(o + double(key_value(key))), uint64_t(beam) << 56 | uint64_t(~uint32_t(key >> 32)) << 24 | uint32_t(key_index(key))};
+        if (k == 2 && i == beam * per) return Next{double_order(o), uint64_t(beam) << 56};
         return Next{0, 0};
     };
     Next mine[H];
@@ -344,8 +348,9 @@ void beam_merge_kernel(BeamShape sh, const float* score, const int32_t* __restri
     auto write = [&](int32_t place, const Next& c) {
         const size_t o = size_t(blockIdx.x) * n + place;
         out_score[o] = c.order ? float(order_value(c.order)) : -INFINITY;
-        out_beam[o] = c.order ? int32_t(c.place >> 32) : -1;
-        out_token[o] = c.order ? int32_t(uint32_t(c.place)) : -1;
+        const int32_t beam = int32_t(c.place >> 56);
+        out_beam[o] = c.order ? beam : -1;
+        out_token[o] = !c.order ? -1 : kind[beam] == 2 ? done_token : int32_t(c.place & 0xffffff);
     };
     if (found <= kList) {
         for (int32_t c = tid; c < found; c += kThreads) {

@@ -537,3 +537,38 @@ def test_distill_of_nearly_the_same_model(dtype, noise, T, V, k, temperature):
     print("%s V %d noise %g: losses of %.1e, off by %.1e of themselves, allowed %.1e" % (
         dtype, V, noise, float(want.abs().median()), float((got - want).norm() / want.norm()), float(off.norm() / want.norm())))
     assert bool(((got - want).abs() <= off).all()), ((got - want).abs() / off).max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("far", [-1e9, -1e30, "lowest", 1e30, math.inf])
+def test_scores_that_swallow_the_logits(dtype, far):
+    """Scores next to which logits are lost even in 64 bits (the type's lowest value for a beam that is none, for one): a beam's continuations still come by its logits."""
+    n, b, V, k = 2, 4, 20000, 8
+    far = -3.4028234663852886e38 if far == "lowest" else far
+    g = torch.Generator().manual_seed(11)
+    z = (torch.randn(n * b, V, generator=g) * (1e-7 if far == -1e9 else 3)).to(DT[dtype])
+    z[:, 5000:5200] = -math.inf
+    score = torch.tensor([[-1.0, far / 2, far, -math.inf], [far, -math.inf, far, math.nan]])
+    few = [17, 900, 19000]
+    z[0] = -math.inf                                 # the beam of an ordinary score has three continuations
+    z[0, few] = torch.tensor([1.0, 3.0, 2.0]).to(DT[dtype])
+    z[6] = z[4]                                      # equal beams: the lower one's, one of its own behind the other
+    desc = bd.make_beam_desc(dtype, n, b, V, k)
+    f = lambda dt: torch.empty(n, k, dtype=dt, device=DEV)
+    os_, ob, ot = f(torch.float32), f(torch.int32), f(torch.int32)
+    ws = torch.empty(bd.lobra_beam_workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    bd.lobra_beam_select(desc, z.to(DEV), score.to(DEV), None, 2, os_, ob, ot, ws)
+    own = lambda row: torch.sort(z[row].float(), descending=True, stable=True).indices[:k].tolist()
+    first = [(0, t) for t in (900, 19000, 17)]
+    rest = [(1, t) for t in own(1)]
+    # (half of infinity is infinity: the lower beam)
+    want0 = (first + rest)[:k] if far < 0 else rest if far == math.inf else [(2, t) for t in own(2)]
+    got = [list(zip(ob[i].tolist(), ot[i].tolist())) for i in range(n)]
+    assert got[0] == want0, (got[0], want0)
+    if far == -1e9:                                  # (the two beams' continuations of equal value alternate)
+        assert [t for bb, t in got[1] if bb == 0] == own(4)[:sum(bb == 0 for bb, _ in got[1])]
+        assert [t for bb, t in got[1] if bb == 2] == own(4)[:sum(bb == 2 for bb, _ in got[1])]
+    else:
+        assert got[1] == [(0, t) for t in own(4)], (got[1], own(4))
+    assert bool((os_[1] == far).all()) or far == -1e9
