@@ -572,3 +572,46 @@ def test_scores_that_swallow_the_logits(dtype, far):
     else:
         assert got[1] == [(0, t) for t in own(4)], (got[1], own(4))
     assert bool((os_[1] == far).all()) or far == -1e9
+
+
+def peaks(dtype, V, b, k):
+    """Logits [b, V] with one peak in every part of 16 KB, each reaching far over what the k-th largest of a part has elsewhere, and their scores."""
+    part, g = 4096 if dtype == "f32" else 8192, torch.Generator().manual_seed(V)
+    z = torch.randn(b, V, generator=g)
+    at = torch.arange(0, V, part)
+    at = at + torch.randint(0, V - int(at[-1]), (len(at),), generator=g)
+    z[:, at] = 20 + 0.01 * torch.randperm(b * len(at), generator=g).view(b, -1)
+    return z.to(DT[dtype]), -1 - 0.003 * torch.arange(b)[None, :], len(at) * b
+
+
+PARTS = [("f32", 131072, 1024), ("f32", 131073, 1056), ("f32", 151000, 1184), ("bf16", 262144, 1024), ("bf16", 300000, 1184)]
+
+
+def test_peaks_are_far_enough_apart():
+    """Of the inputs below: no two continuations that are wanted, or next to those, lie nearer to each other than the kernel's sums are exact, but those of one beam."""
+    for dtype, V, parts in PARTS:
+        z, score, n = peaks(dtype, V, 32, 32)
+        assert n == parts
+        v, beam, _ = (t[0] for t in ref_select(z, score, None, 2, 40))
+        assert bool(((v[:-1] - v[1:] > 2e-5) | (beam[:-1] == beam[1:])).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["peaks", "constant"])
+@pytest.mark.parametrize("dtype,V,parts", PARTS)
+def test_more_parts_than_the_merge_lists(dtype, V, parts, kind):
+    """32 beams, all of whose parts reach the merge's first threshold, with more candidates than its list holds: up to 1024 parts are listed in their turn, more are looked at
+    as they lie; the counts leave 32 peaks, or all candidates, which are equal."""
+    b = k = 32
+    z, score, _ = peaks(dtype, V, b, k)
+    if kind == "constant":
+        z[:], score[:] = 0.5, -1.0
+    want = ref_select(z, score, None, 2, k)
+    desc = bd.make_beam_desc(dtype, 1, b, V, k)
+    ws, wok = guarded(bd.lobra_beam_workspace_bytes(desc), dtype=torch.uint8)
+    o = [guarded(1, k, dtype=dt) for dt in (torch.float32, torch.int32, torch.int32)]
+    bd.lobra_beam_select(desc, z.to(DEV), score.to(DEV), None, 2, *(t for t, _ in o), ws)
+    torch.cuda.synchronize()
+    assert wok() and all(ok() for _, ok in o)
+    assert bool(((o[0][0].double().cpu() - want[0]).abs() <= 4e-6 + 2.0 ** -23 * want[0].abs()).all())
+    assert torch.equal(o[1][0].cpu().long(), want[1]) and torch.equal(o[2][0].cpu().long(), want[2]), (o[1][0], want[1], o[2][0], want[2])
