@@ -615,3 +615,53 @@ def test_more_parts_than_the_merge_lists(dtype, V, parts, kind):
     assert wok() and all(ok() for _, ok in o)
     assert bool(((o[0][0].double().cpu() - want[0]).abs() <= 4e-6 + 2.0 ** -23 * want[0].abs()).all())
     assert torch.equal(o[1][0].cpu().long(), want[1]) and torch.equal(o[2][0].cpu().long(), want[2]), (o[1][0], want[1], o[2][0], want[2])
+
+
+def meet(pairs, size):
+    """Whether a tensor of the list writes what another one reads or writes, pair by pair; pairs of addresses, sizes of the tensors."""
+    over = lambda p, n, q, m: p < q + m and q < p + n
+    return any(size[i] and size[j] and (over(b, size[i], d, size[j]) or over(b, size[i], c, size[j]) or over(a, size[i], d, size[j]))
+               for i, (a, b) in enumerate(pairs) for j, (c, d) in enumerate(pairs[:i]))
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 7, 40, 255, 256, 257, 300, 700])
+def test_which_lists_of_states_meet(n):
+    """Lists that do and lists that don't, of every length around what is sorted at a time, against pair by pair; six rows a tensor."""
+    L, rng, seen = bd.lib(), np.random.default_rng(n), set()
+    for trial in range(60 if n < 100 else 12):
+        row = rng.choice([0, 16, 32, 48], size=n, p=[0.05, 0.35, 0.3, 0.3])
+        # places of their own, some of which are given up for one that another tensor has, or one next to it
+        place = (1 << 20) + 288 * rng.permutation(2 * n)
+        src, dst = place[:n].copy(), np.where(rng.random(n) < 0.4, place[:n], place[n:])
+        for _ in range(int(rng.integers(0, 3))):
+            i, j, shift = int(rng.integers(n)), int(rng.integers(n)), int(rng.choice([0, 16, 272, -272, 288]))
+            k = rng.integers(4)
+            if k == 0:
+                src[i] = src[j]                      # (read twice)
+            elif k == 1:
+                dst[i] = dst[j] + shift
+            elif k == 2:
+                src[i] = dst[j] + shift
+            else:
+                dst[i] = src[j] + shift
+        pairs, size = list(zip(src.tolist(), dst.tolist())), (6 * row).tolist()
+        own = any(s and a != b and abs(a - b) < s for (a, b), s in zip(pairs, size))
+        want = -2 if own or meet(pairs, size) else 0 if not any(size) else -1        # (-1: as far as the missing parents)
+        t = (bd.BeamState * n)(*(bd.BeamState(a, b, s // 6, 8) for (a, b), s in zip(pairs, size)))
+        assert L.lobra_beam_reorder(t, n, 2, 3, None, 3, None, None) == want, (trial, pairs[:4], size[:4])
+        seen.add(want)
+    assert n == 1 or {-1, -2} <= seen
+
+
+def test_a_long_list_of_states_is_looked_at_quickly():
+    """Keys and values of 80 layers, and of 640: eight times the tensors take less than 24 times as long on the host, where pair by pair it would be 64."""
+    import time
+    L, best = bd.lib(), {}
+    for n in (160, 1280):
+        t = (bd.BeamState * n)(*(bd.BeamState(*((1 << 20) + (i * 7919 % n) * 4096,) * 2, 64, 8) for i in range(n)))
+        best[n] = math.inf
+        for _ in range(30):
+            a = time.perf_counter()
+            assert L.lobra_beam_reorder(t, n, 2, 3, None, 3, None, None) == -1
+            best[n] = min(best[n], time.perf_counter() - a)
+    assert best[1280] < 24 * best[160], best
