@@ -423,7 +423,7 @@ LOBRA_API lobra_status lobra_quantise_weight(int32_t dtype, int32_t d_in, int32_
 /* The layer on such a base, for a bf16 plan of any n_proj (projection j: rows j dg .. of Wq and w_scale).  The arguments are those of
  * lobra_mlora_plan_fwd / _bwd, and h_save is what lobra_mlora_plan_fwd writes.
  *   ws : lobra_mlora_quant_workspace_bytes (either out pointer may be NULL); all of it is needed: the quantised tokens and a split product's
- *        sums, in backward Ŵ in front of the plan's own
+ *        sums, in backward Ŵ in front of the plan's own (with LOBRA_FLAG_NO_DX the plan's own bwd_ws_bytes are enough)
  * LOBRA_ERR_DTYPE for an fp32 plan or one of plain kernels, LOBRA_ERR_SHAPE for d_in above LOBRA_MAX_QUANT_IN. */
 LOBRA_API lobra_status lobra_mlora_quant_workspace_bytes(const lobra_mlora_plan *plan, size_t *fwd_bytes, size_t *bwd_bytes);
 LOBRA_API lobra_status lobra_mlora_quant_fwd(const lobra_mlora_plan *plan, const void *x, const int8_t *Wq, const float *w_scale, const void *A,

@@ -159,17 +159,18 @@ lobra_status lobra_mlora_quant_bwd(const lobra_mlora_plan* plan, const void* x, 
     if (rs != LOBRA_OK) return rs;
     const Plan& p = *plan;
     if ((rs = q8_plan(p)) != LOBRA_OK) return rs;
-    const size_t own = q8_weight_bytes(p);
+    const bool want_dx = !(flags & LOBRA_FLAG_NO_DX);
+    const size_t own = want_dx ? q8_weight_bytes(p) : 0;             // (only dx takes the weight)
     if (p.desc.T > 0 && !w_scale) return LOBRA_ERR_NULL;
     if (!aligned16(w_scale)) return LOBRA_ERR_ALIGN;
     char* const rest = ws ? static_cast<char*>(ws) + own : nullptr;
     const size_t left = ws && ws_bytes > own ? ws_bytes - own : 0;
     if ((rs = plan_bwd_check(p, x, Wq, A, B, s, dy, h_saved, dx, dA, dB, flags, rest, left)) != LOBRA_OK) return rs;
-    if (p.desc.T > 0 && (!ws || ws_bytes < own)) return LOBRA_ERR_WORKSPACE;
+    if (p.desc.T > 0 && own > 0 && (!ws || ws_bytes < own)) return LOBRA_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (p.desc.T > 0 && !(flags & LOBRA_FLAG_NO_DX))
+    if (p.desc.T > 0 && want_dx)
         LOBRA_LAUNCH(p, st, LOBRA_K_QUANT, q8_dequantise(p.desc.d_in, p.desc.d_out, Wq, w_scale, ws, st));
-    return lobra_mlora_plan_bwd(plan, x, ws, A, B, s, dy, h_saved, dx, dA, dB, flags, rest, left, hip_stream);
+    return lobra_mlora_plan_bwd(plan, x, want_dx ? ws : Wq, A, B, s, dy, h_saved, dx, dA, dB, flags, rest, left, hip_stream);
 }
 
 }  // extern "C"

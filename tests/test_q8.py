@@ -506,3 +506,26 @@ def test_scales_of_every_size(T, d, f, ranks, n_proj):
         good = torch.where(large, (got * ref.sign() >= top * (1 - HALF)), good | split)
         assert bool(good.all()), (int((~good).sum()), good.numel(), got[~good][:4].tolist(), ref[~good][:4].tolist())
         assert int(large.sum()) > 0 and int(((ref.abs() > 1) & ~large).sum()) > T * f // 10
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,f,ranks,n_proj", [(40, 512, 264, [8], 1), (300, 640, 768, [16, 8], 2), (2600, 1032, 520, [16, 8], 1), (64, 256, 264, [], 1)])
+def test_backward_without_dx_needs_no_room_for_the_weight(T, d, f, ranks, n_proj):
+    v, off, task, rank_off = make(T, d, f, ranks, "mixed" if ranks else "one", n_proj)
+    dv = on_device(v)
+    wq, ws = weight(None, dv["W"], d, f)
+    plan = bd.Plan("bf16", T, d, f, rank_off if ranks else None, off, task, n_proj=n_proj)
+    ad = (dv["A"], dv["B"], dv["s"]) if ranks else (None,) * 3
+    full = torch.empty(bd.lobra_mlora_quant_workspace_bytes(plan)[1], dtype=torch.uint8, device=DEV)
+    own, ok = guarded(max(plan.bwd_ws_bytes, 16), dtype=torch.uint8)
+    R = sum(ranks) * n_proj
+    G = [[torch.full(s, 5.0, device=DEV) for s in ((R, d), (R, f // n_proj))] if ranks else [None, None] for _ in range(2)]
+    bd.lobra_mlora_quant_bwd(plan, dv["x"], wq, ws, *ad, dv["dy"], None, torch.empty(T, d, device=DEV, dtype=torch.bfloat16), *G[0], 0, full)
+    bd.lobra_mlora_quant_bwd(plan, dv["x"], wq, ws, *ad, dv["dy"], None, None, *G[1], bd.FLAG_NO_DX, own if ranks else None)
+    torch.cuda.synchronize()
+    assert ok()
+    if ranks:
+        for a, b in zip(*G):                         # (with dx the projection of dy may run in the product's launch: another order of sums)
+            assert torch.allclose(a, b, rtol=2 * HALF, atol=2 * HALF * float(a.abs().max()))
+        call = lambda n: bd.lobra_mlora_quant_bwd(plan, dv["x"], wq, ws, *ad, dv["dy"], None, None, *G[1], bd.FLAG_NO_DX, own[:n], check=False)
+        assert call(0) == -7 and bd.lobra_mlora_quant_bwd(plan, dv["x"], None, ws, *ad, dv["dy"], None, None, *G[1], bd.FLAG_NO_DX, own, check=False) == -1
