@@ -495,7 +495,7 @@ LOBRA_API lobra_status lobra_beam_select(const lobra_beam_desc *desc, const void
 /* What is kept per sequence (tokens so far, caches), put in the order of the beams that go on: row (request, i) of dst becomes row
  * (request, parent[request][i]) of src, for every tensor of the list.
  *   states  : HOST array.  src, dst: device, n_req * beams rows of row_bytes, back to back; dst = src reorders in place (a row that stays costs
- *             nothing), else the two do not overlap; nor does what one tensor of the list writes with another (LOBRA_ERR_SHAPE)
+ *             nothing), else the two do not overlap; nor does what one tensor of the list writes with another, with parent or with used (LOBRA_ERR_SHAPE)
  *   parent  : device int32, row of a request every parent_ld numbers (>= beams): out_beam of lobra_beam_select, for one (n_out >= beams).  Outside
  *             [0, beams): row i of dst is left as it is
  *   used    : device int32 [n_req] or NULL: only the first used unit_bytes bytes of a request's rows move, the rest of dst is left as it is

@@ -43,11 +43,17 @@ lobra_status beam_shape(const lobra_beam_desc* d, BeamShape* s)
     return LOBRA_OK;
 }
 
-// Whether a tensor of the list writes what another one reads or writes (they run side by side).  What kAtATime tensors read and write is sorted by address, with the
+// What is read beside the states.
+struct Bytes {
+    const void* at;
+    uintptr_t n;
+};
+
+// Whether a tensor of the list writes what another one reads or writes (they run side by side), or something of `beside`.  What kAtATime tensors read and write is sorted by address, with the
 // furthest end of all that begins no later, and of what is written among it; every tensor behind them is looked up there.  No memory is taken.  (160 tensors, the
 // keys and values of 80 layers, 4 us in place, 7 apart, and pair by pair 21; 1000 of them 43 and 131, and 744.)
 constexpr int32_t kAtATime = 256;
-bool states_meet(const lobra_beam_state* states, int32_t n, int64_t rows)
+template <int N> bool states_meet(const lobra_beam_state* states, int32_t n, int64_t rows, const Bytes (&beside)[N])
 {
     struct Range {
         uintptr_t at, end, written_end;
@@ -73,12 +79,14 @@ bool states_meet(const lobra_beam_state* states, int32_t n, int64_t rows)
             p->end = std::max(p->end, p[-1].end);
             p->written_end = std::max(p->written_end, p[-1].written_end);
         }
+        const auto apart = [&](uintptr_t at, uintptr_t end, bool written) {
+            const Range* const behind = std::lower_bound(r, last, end, [](const Range& x, uintptr_t v) { return x.at < v; });
+            return behind == r || !behind[-1].meets(at, written);
+        };
         for (int32_t i = i1; i < n; ++i)
-            if (!of(i, [&](uintptr_t at, uintptr_t end, bool written) {
-                    const Range* const behind = std::lower_bound(r, last, end, [](const Range& x, uintptr_t v) { return x.at < v; });
-                    return behind == r || !behind[-1].meets(at, written);
-                }))
-                return true;
+            if (!of(i, apart)) return true;
+        for (const Bytes& b : beside)
+            if (const uintptr_t at = reinterpret_cast<uintptr_t>(b.at); at && !apart(at, at + b.n, false)) return true;
     }
     return false;
 }
@@ -169,7 +177,10 @@ lobra_status lobra_beam_reorder(const lobra_beam_state* states, int32_t n_states
         if (a != b && (a < b ? b - a : a - b) < uintptr_t(bytes)) return LOBRA_ERR_SHAPE;
     }
     if (!any) return LOBRA_OK;
-    if (states_meet(states, n_states, rows)) return LOBRA_ERR_SHAPE;
+    const bool given = parent && aligned4(parent) && aligned4(used);          // (else refused below)
+    const Bytes parents{given ? parent : nullptr, uintptr_t((n_req - 1) * parent_ld + beams) * sizeof(int32_t)},
+        lengths{given ? used : nullptr, uintptr_t(n_req) * sizeof(int32_t)};
+    if (states_meet(states, n_states, rows, {parents, lengths})) return LOBRA_ERR_SHAPE;
     if (!parent) return LOBRA_ERR_NULL;
     if (!aligned4(parent) || !aligned4(used)) return LOBRA_ERR_ALIGN;
     LOBRA_HIP(beam_reorder(states, n_states, n_req, beams, parent, parent_ld, used, static_cast<hipStream_t>(hip_stream)));

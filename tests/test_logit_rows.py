@@ -665,3 +665,32 @@ def test_a_long_list_of_states_is_looked_at_quickly():
             assert L.lobra_beam_reorder(t, n, 2, 3, None, 3, None, None) == -1
             best[n] = min(best[n], time.perf_counter() - a)
     assert best[1280] < 24 * best[160], best
+
+
+@pytest.mark.gpu
+def test_reorder_that_would_write_its_own_parents():
+    """The parents and the used lengths are read while states are written: a list that writes them is refused, one that has them next door is not; six rows of 64 bytes, 32
+    bytes of parents (rows of three numbers, five apart), 8 of lengths, all in one allocation."""
+    L, stream = bd.lib(), torch.cuda.current_stream().cuda_stream
+    buf = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+    p, away = buf.data_ptr() + 8192, buf.data_ptr() + (1 << 19)
+    far = [(p + (i + 1) * 1024, p + (i + 1) * 1024 + 512) for i in range(300)]        # (more than what is sorted at a time)
+
+    def R(pairs, parent, used=None):
+        t = (bd.BeamState * len(pairs))(*(bd.BeamState(a, b, 64, 8) for a, b in pairs))
+        return L.lobra_beam_reorder(t, len(pairs), 2, 3, parent, 5, used, stream)
+
+    for pairs in ([(p, p)], [(p - 4096, p)], far + [(p, p)], [(p, p)] + far):
+        for at in (p, p + 380, p - 28):
+            assert R(pairs, at) == -2, at
+        for at in (p, p + 380, p - 4):
+            assert R(pairs, away, at) == -2, at
+        assert R(pairs, p + 384, p - 8) == 0 and R(pairs, p - 32, p + 384) == 0
+    assert R([(p, p + 4096)], p, p) == 0             # (what is only read may be both)
+    torch.cuda.synchronize()
+    row = torch.arange(6, dtype=torch.int32, device=DEV).repeat_interleave(16)
+    state, par = buf[8192:8192 + 384].view(torch.int32), buf[8192 - 32:8192].view(torch.int32)
+    state.copy_(row)
+    par.copy_(torch.tensor([2, 0, 1, 9, 9, 1, 1, 0], dtype=torch.int32))
+    assert R([(p, p)], p - 32) == 0
+    assert state.view(6, 16)[:, 0].tolist() == [2, 0, 1, 4, 4, 3] and par.tolist() == [2, 0, 1, 9, 9, 1, 1, 0]
