@@ -219,7 +219,7 @@ def validate(desc: Desc) -> int:
 
 
 def _ptr(t):
-    if t is None or isinstance(t, int):
+    if t is None or type(t) is int:
         return t
     assert t.is_contiguous(), "tensors must be contiguous"
     return t.data_ptr()
@@ -238,34 +238,12 @@ _KINDS = {F32: "fp32", BF16: "bf16"}
 
 def _typed(t, kind, least=0):
     """_ptr of a tensor that the library takes for `kind` ("fp32", "bf16", "int32", "int8"), of at least so many elements."""
-    if t is None or isinstance(t, int):
+    if t is None or type(t) is int:
         return t
     assert t.dtype is _torch_types[kind], "a %s tensor where the library reads or writes %s" % (t.dtype, kind)
     assert not least or t.numel() >= least, "a tensor of %d elements where the library reads or writes %d" % (t.numel(), least)
     assert t.is_contiguous(), "tensors must be contiguous"
     return t.data_ptr()
-
-
-_current_device = None
-
-
-def _here(*tensors):
-    """All tensors of a call have to lie on the device that it is launched on: the current one."""
-    global _current_device
-    device = None
-    for t in tensors:
-        if t is not None and t.__class__ is not int:
-            d = t.get_device()
-            if d != device:
-                assert d >= 0, "a host tensor where the library reads or writes device memory"
-                assert device is None, "tensors of different devices"
-                device = d
-    if device is not None:
-        if _current_device is None:
-            import torch
-            torch.cuda.current_device()           # (initialises, or says why it can't)
-            _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-        assert device == _current_device(), "a tensor of another device than the current one"
 
 
 _current_stream = None
@@ -283,6 +261,31 @@ def _stream(stream):
         # the handle without a Stream object around it: 3 us of an 8 us call
         _current_stream = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
     return _current_stream()
+
+
+_current_device = _raw_stream = None
+
+
+def _launched(stream, *tensors):
+    """The handle of the stream that a call is launched on, as _stream.  All of its tensors have to lie on the current device."""
+    global _current_device, _raw_stream
+    device = None
+    for t in tensors:
+        if t is not None and type(t) is not int:
+            d = t.get_device()
+            if d != device:
+                assert d >= 0, "a host tensor where the library reads or writes device memory"
+                assert device is None, "tensors of different devices"
+                device = d
+    if device is None:
+        return _stream(stream)
+    if _current_device is None:
+        import torch
+        torch.cuda.current_device()           # (initialises, or says why it can't)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    assert device == _current_device(), "a tensor of another device than the current one"
+    return _raw_stream(device) if stream is None else _stream(stream)
 
 
 class Plan:
@@ -492,7 +495,7 @@ def make_logprob_desc(dtype, T, V, ld=0, top_k=0) -> LogprobDesc:
 
 def _rows_ptr(t, desc, rows=None):
     """A [T, V] tensor of the descriptor's type whose rows are ld elements apart (a slice of wider rows, for one)."""
-    if t is None or isinstance(t, int):
+    if t is None or type(t) is int:
         return t
     T, V = t.shape
     ld, one = t.stride()
@@ -604,9 +607,8 @@ def lobra_quantise_weight(W, Wq, w_scale, stream=None, check=True):
     assert d_out <= 1 or W.stride(1) == 1, "rows of a weight must be contiguous"
     assert d_in <= 1 or W.stride(0) >= d_out, "rows of a weight that overlap"
     assert Wq.shape == (d_out, lobra_quant_pitch(d_in)), "Wq of another shape than [d_out, lobra_quant_pitch(d_in)]"
-    args = W.data_ptr(), _typed(Wq, "int8"), _typed(w_scale, "fp32", d_out)
-    _here(W, Wq, w_scale)
-    st = lib().lobra_quantise_weight(kind, d_in, d_out, W.stride(0) if d_in > 1 else 0, *args, _stream(stream))
+    st = lib().lobra_quantise_weight(kind, d_in, d_out, W.stride(0) if d_in > 1 else 0, W.data_ptr(), _typed(Wq, "int8"),
+                                        _typed(w_scale, "fp32", d_out), _launched(stream, W, Wq, w_scale))
     if check:
         _check(st, "lobra_quantise_weight")
     return st
@@ -633,10 +635,9 @@ def _saved(plan: Plan, h):
 
 def lobra_mlora_quant_fwd(plan: Plan, x, Wq, w_scale, A, B, s, y, h_save=None, ws=None, stream=None, check=True):
     """y = x W + s_t (A_t x) B_t with W and x in 8-bit integers in the first product.  Returns the status."""
-    args = (*_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(y, plan.kind, plan.T * plan.d_out), _saved(plan, h_save), _ptr(ws))
-    if not plan.host_only:
-        _here(x, Wq, w_scale, A, B, s, y, h_save, ws)
-    st = lib().lobra_mlora_quant_fwd(plan.handle, *args, _nbytes(ws), _stream(stream))
+    st = lib().lobra_mlora_quant_fwd(plan.handle, *_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(y, plan.kind, plan.T * plan.d_out),
+                                  _saved(plan, h_save), _ptr(ws), _nbytes(ws),
+                                  _stream(stream) if plan.host_only else _launched(stream, x, Wq, w_scale, A, B, s, y, h_save, ws))
     if check:
         _check(st, "lobra_mlora_quant_fwd")
     return st
@@ -645,11 +646,10 @@ def lobra_mlora_quant_fwd(plan: Plan, x, Wq, w_scale, A, B, s, y, h_save=None, w
 def lobra_mlora_quant_bwd(plan: Plan, x, Wq, w_scale, A, B, s, dy, h_saved, dx, dA, dB, flags=0, ws=None, stream=None, check=True):
     """dx, dA, dB of the layer on an 8-bit base.  Returns the status."""
     e, T, R = plan.kind, plan.T, plan.R_tot
-    args = (*_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(dy, e, T * plan.d_out), _saved(plan, h_saved), _typed(dx, e, T * plan.d_in),
-            _typed(dA, "fp32", R * plan.d_in), _typed(dB, "fp32", R * (plan.d_out // plan.desc.n_proj)), int(flags), _ptr(ws))
-    if not plan.host_only:
-        _here(x, Wq, w_scale, A, B, s, dy, h_saved, dx, dA, dB, ws)
-    st = lib().lobra_mlora_quant_bwd(plan.handle, *args, _nbytes(ws), _stream(stream))
+    st = lib().lobra_mlora_quant_bwd(plan.handle, *_quant_operands(plan, x, Wq, w_scale, A, B, s), _typed(dy, e, T * plan.d_out), _saved(plan, h_saved),
+                                  _typed(dx, e, T * plan.d_in), _typed(dA, "fp32", R * plan.d_in), _typed(dB, "fp32", R * (plan.d_out // plan.desc.n_proj)),
+                                  int(flags), _ptr(ws), _nbytes(ws),
+                                  _stream(stream) if plan.host_only else _launched(stream, x, Wq, w_scale, A, B, s, dy, h_saved, dx, dA, dB, ws))
     if check:
         _check(st, "lobra_mlora_quant_bwd")
     return st
@@ -669,9 +669,8 @@ def _teacher(desc: DistillDesc, teacher_logp, teacher_id):
 def lobra_token_distill_fwd(desc: DistillDesc, logits, teacher_logp, teacher_id, loss, stat=None, stream=None, check=True):
     """loss [T] of every row against the teacher's tokens [T, top_k]; stat (fp32 [T, 4]) for backward.  Returns the status."""
     T = desc.T
-    args = (_rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id), _typed(loss, "fp32", T), _typed(stat, "fp32", 4 * T))
-    _here(logits, teacher_logp, teacher_id, loss, stat)
-    st = lib().lobra_token_distill_fwd(ctypes.byref(desc), *args, _stream(stream))
+    st = lib().lobra_token_distill_fwd(ctypes.byref(desc), _rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id), _typed(loss, "fp32", T),
+                                       _typed(stat, "fp32", 4 * T), _launched(stream, logits, teacher_logp, teacher_id, loss, stat))
     if check:
         _check(st, "lobra_token_distill_fwd")
     return st
@@ -680,9 +679,9 @@ def lobra_token_distill_fwd(desc: DistillDesc, logits, teacher_logp, teacher_id,
 def lobra_token_distill_bwd(desc: DistillDesc, logits, teacher_logp, teacher_id, stat, dloss, dlogits, flags=0, stream=None, check=True):
     """dlogits (may be logits) from dloss [T].  Returns the status."""
     T = desc.T
-    args = (_rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id), _typed(stat, "fp32", 4 * T), _typed(dloss, "fp32", T), _rows_ptr(dlogits, desc))
-    _here(logits, teacher_logp, teacher_id, stat, dloss, dlogits)
-    st = lib().lobra_token_distill_bwd(ctypes.byref(desc), *args, int(flags), _stream(stream))
+    st = lib().lobra_token_distill_bwd(ctypes.byref(desc), _rows_ptr(logits, desc), *_teacher(desc, teacher_logp, teacher_id),
+                                       _typed(stat, "fp32", 4 * T), _typed(dloss, "fp32", T), _rows_ptr(dlogits, desc), int(flags),
+                                       _launched(stream, logits, teacher_logp, teacher_id, stat, dloss, dlogits))
     if check:
         _check(st, "lobra_token_distill_bwd")
     return st
@@ -702,10 +701,9 @@ def lobra_beam_workspace_bytes(desc: BeamDesc) -> int:
 def lobra_beam_select(desc: BeamDesc, logits, score, done, done_token, out_score, out_beam, out_token, ws, stream=None, check=True):
     """The n_out best continuations of every request: scores, beams within the request, tokens.  Returns the status."""
     rows, n = desc.n_req * desc.beams, desc.n_req * desc.n_out
-    args = (_rows_ptr(logits, desc, rows), _typed(score, "fp32", rows), _typed(done, "int32", rows), int(done_token), _typed(out_score, "fp32", n),
-            _typed(out_beam, "int32", n), _typed(out_token, "int32", n), _ptr(ws))
-    _here(logits, score, done, out_score, out_beam, out_token, ws)
-    st = lib().lobra_beam_select(ctypes.byref(desc), *args, _nbytes(ws), _stream(stream))
+    st = lib().lobra_beam_select(ctypes.byref(desc), _rows_ptr(logits, desc, rows), _typed(score, "fp32", rows), _typed(done, "int32", rows),
+                                 int(done_token), _typed(out_score, "fp32", n), _typed(out_beam, "int32", n), _typed(out_token, "int32", n), _ptr(ws),
+                                 _nbytes(ws), _launched(stream, logits, score, done, out_score, out_beam, out_token, ws))
     if check:
         _check(st, "lobra_beam_select")
     return st
@@ -736,10 +734,8 @@ def lobra_beam_reorder(states, n_req, beams, parent, used=None, stream=None, che
     assert parent.dtype is _torch_types["int32"] and parent.dim() == 2 and parent.shape[0] == n_req and parent.shape[1] >= beams, \
         "parents other than int32 [n_req, beams]"
     assert parent.shape[1] <= 1 or parent.stride(1) == 1, "rows of parents must be contiguous"
-    limit = _typed(used, "int32", n_req)
-    _here(*where)
-    st = lib().lobra_beam_reorder(arr, len(states), int(n_req), int(beams), parent.data_ptr(), parent.stride(0) if n_req > 1 else int(beams), limit,
-                                  _stream(stream))
+    st = lib().lobra_beam_reorder(arr, len(states), int(n_req), int(beams), parent.data_ptr(), parent.stride(0) if n_req > 1 else int(beams),
+                                  _typed(used, "int32", n_req), _launched(stream, *where))
     if check:
         _check(st, "lobra_beam_reorder")
     return st

@@ -194,7 +194,7 @@ void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* _
     }
 }
 
-// A continuation as two numbers: its value's order, and beam, logit and token, the lower the better: 5 bits of beam, the logit's order from the largest down, 24 bits of
+// A continuation as two numbers: its value's order, and beam, logit and token, the lower the better: 8 bits of beam, the logit's order from the largest down, 24 bits of
 // token (of a beam that is done: of no token).  Within a beam the logits' order is the values', also where those are equal in 64 bits because the score is far larger than
 // a logit, so that what a part hands on is what the request wants of it.
 struct Next {
