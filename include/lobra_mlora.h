@@ -410,8 +410,9 @@ LOBRA_API lobra_status lobra_token_logprob_bwd(const lobra_logprob_desc *desc, c
  *     y_i = sx_i sw (qx_i Wq) + s_t (A_t x_i) B_t          sx_i = max |x_i| / 127,  qx_i = x_i / sx_i
  *     dx_i = dy_i Ŵ^T + s_t (B_t dy_i) A_t                 Ŵ = sw Wq;  dA, dB as ever, from x
  * with quotients rounded to the nearest whole number, halves to the even one, and whole sums (d_in <= LOBRA_MAX_QUANT_IN).  Backward passes by the
- * rounding of x, as if it were none; Ŵ is rounded to bf16 there.  A token (channel) that holds NaN or infinity makes its row (column) of y NaN;
- * one whose largest magnitude is below 127 x 2^-126 counts as zeros.
+ * rounding of x, as if it were none; Ŵ is rounded to bf16 there.  The projections s_t A_t x and s_t B_t dy are rounded to bf16 as in the layer, but most
+ * forward calls of up to 64 tokens without h_save keep s_t A_t x in fp32: their y may differ in its last place from that of a call with it.
+ * A token (channel) that holds NaN or infinity makes its row (column) of y NaN; one whose largest magnitude is below 127 x 2^-126 counts as zeros.
  *
  * lobra_quantise_weight: once per weight, W [d_in, d_out] of element type `dtype`, row i at W + i ldw elements (0: d_out) ->
  *   Wq      : device int8 [d_out, lobra_quant_pitch(d_in)], 16-byte aligned: a row per channel, zero beyond d_in

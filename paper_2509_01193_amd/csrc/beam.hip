@@ -62,7 +62,8 @@ __device__ __forceinline__ bool looked_at(float score, const int32_t* done, size
 // Part blockIdx.x % parts of row blockIdx.x / parts: keys [n] (0: none left) in order, {max, sum exp(z - max)}.
 // 64 groups of four threads have a maximum each; what the n-th largest of these (or a little less) reaches, n logits at least, goes on a list and
 // finds its place there by counting who is larger.  Parts with more of them than the list holds (equal logits) take the largest n times over.
-// Bound: instructions as much as memory (VALUs busy for 65 %, 3.0 TB/s): 512 x 128000 bf16 of which a tenth is done 38 to 44 us, four rows of 32000 5.1.
+// Bound: neither is full, VALUs busy for 63 % and 2.8 TB/s, since a workgroup computes when its loads are there and has no others on their way: 512 x 128000 bf16 of which a
+// tenth is done 38 to 44 us, four rows of 32000 5.1.
 template <typename E>
 __global__ __launch_bounds__(kThreads)
 void beam_part_kernel(BeamShape sh, const E* __restrict__ logits, const float* __restrict__ score, const int32_t* __restrict__ done, int32_t parts,

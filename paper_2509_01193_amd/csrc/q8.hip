@@ -18,7 +18,8 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(int32_t T, int32_t d, int3
 }
 
 // 64 columns per workgroup, a lane each; its 16 waves share the rows, 16 neighbouring ones at a time, so that a lane's 16 values are 16 neighbouring
-// bytes of its column's row of q.  Done once per weight: 4096 x 11008 bf16 180 us (with four waves a workgroup 617).
+// bytes of its column's row of q.  Done once per weight: 4096 x 11008 bf16 183 us, fp32 78; 4096 x 4096 177 and 61;
+// 11008 x 4096 478 and 155 (with four waves a workgroup 617 for the first).  Bound: round trips; a column's 16 waves wait for each batch of 16 rows.
 constexpr int kWeightWaves = 16;
 template <typename E>
 __global__ __launch_bounds__(64 * kWeightWaves) void q8_weight_kernel(int32_t d_in, int32_t d_out, int32_t pitch, int64_t ldw, const E* __restrict__ W,

@@ -1,18 +1,24 @@
 // The layer on a base in 8-bit integers for few tokens (decoding), in two launches: tokens quantised and projected; then the product, which adds the
 // adapter term and writes y.
 //
-// The product reads W once and does next to nothing with it, so what counts is that all of W is on its way at once and that no sum goes
-// through memory.  A workgroup has 16 columns, its eight waves share K in pieces of 256, two of them on their way, and the waves' whole sums meet in LDS.  A lane of
-// the matrix instruction holds 16 k of a column of its own; read like that, each load touches 64 bytes of 16 lines, so four whole lines of each of four columns are read
-// instead and turned in LDS (40 x 4096 x 4096 15.7 -> 13.2, 40 x 11008 x 4096 29.9 -> 23.3, as for a W that lies in memory the way the instruction takes it: 14.2, 26.3 with
-// one piece on its way).  The tokens (a few hundred KB) come from the L2, in that form.
+// The product reads W once and does next to nothing with it, so what counts is that all of W is on its way at once and that no sum goes through
+// memory.  A workgroup has 16 columns, its eight waves share K in pieces of 256, two of them on their way, and the waves' whole sums meet in LDS.
+// A lane of the matrix instruction holds 16 k of a column of its own; read like that, each load touches 64 bytes of 16 lines, so four whole lines of
+// each of four columns are read instead and turned in LDS.  The tokens (a few hundred KB) come from the L2, as the instruction takes them.
 // The projection of a token has a workgroup per quarter of K, since one alone streams the 128 KiB of a rank-16 adapter at K = 4096 for longer than the
 // product takes; the quarters' fp32 sums are added where they are used.
-// Tokens x K x N, one-token segments, us, with the tiled product (q8.hip, gemm_tile_q8.hip) / these: rank 16, 1 x 4096 x 4096 13.6 / 9.6, 16 of them 15.3 / 10.9, 40
-// 15.4 / 13.3, 64 16.6 / 15.5; 64 x 1376 x 4096 14.0 / 10.5, 64 x 512 x 512 10.9 / 9.3, 32 x 2048 x 2048 12.3 / 9.0, 64 x 11008 x 4096 29.7 / 26.4; 1 x 4096 x 8192 15.9 / 12.4, 16 18.3 / 14.9,
-// 40 18.9 / 20.8.  Not where the columns are more than two workgroups' for every compute unit, each of which takes the tokens from the L2 once more (1 x 4096 x 11008 16.7 / 16.7, 16
-// 18.8 / 19.8, 40 20.2 / 27.3), nor for wide adapters, whose ranks are added one by one (rank 64, 1 x 4096 x 4096 16.9 / 14.3, 8 18.3 / 18.6, 40 19.5 / 22.6; rank 128, 8 x 1024 x 1024
-// 15.8 / 19.4).  Three pieces of W on their way instead of two 13.8 (40 x 4096 x 4096), tokens row by row instead of as the matrix instruction takes them 0.7 more, 32 columns a
+//
+// us, the tiled product (q8.hip, gemm_tile_q8.hip) / these; one-token segments, K x N:
+//     rank  tokens   1            16           40           64
+//     16    4096 x 4096     13.6 /  9.6  15.3 / 10.9  15.4 / 13.3  16.6 / 15.5
+//     16    4096 x 8192     15.9 / 12.4  18.3 / 14.9  18.9 / 20.8
+//     16    4096 x 11008    16.7 / 16.7  18.8 / 19.8  20.2 / 27.3
+//     64    4096 x 4096     16.9 / 14.3  18.3 / 18.6 (8 tokens)    19.5 / 22.6
+//     16    64 tokens: 1376 x 4096 14.0 / 10.5, 512 x 512 10.9 / 9.3, 11008 x 4096 29.7 / 26.4; 32 tokens: 2048 x 2048 12.3 / 9.0
+//     128   8 tokens: 1024 x 1024 15.8 / 19.4
+// So not where the columns are more than two workgroups' for every compute unit, each of which takes the tokens from the L2 once more, nor for wide
+// adapters, whose ranks are added one by one.
+// 40 x 4096 x 4096 otherwise: W read 64 bytes of a line at a time 15.7, three pieces of W on their way 13.8, tokens row by row 0.7 more, 32 columns a
 // workgroup half as much again.
 #include "gemm_common.h"
 #include "kernels.h"
