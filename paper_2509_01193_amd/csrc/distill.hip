@@ -188,14 +188,14 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
         ex = join[0][0] + join[0][1];
         own_sum = join[1][0] + join[1][1];
     }
-    double q = own, tl = 0.;                         // tl: the teacher's ln of the sum, in units of l
+    double q = own, tl = 0., ln_own = 0.;            // tl: the teacher's ln of the sum, in units of l
     if (TAIL) {
         S = (rest_s > 0. ? rest_s * exp((rest_m - M) * cd) : rest_s) + ex;
     } else {
         q = own / own_sum;
-        const double ln = log(own_sum);
-        tl = double(lm) + ln / cd;
-        ln_q = (ln_q - double(lm)) * cd - ln;
+        ln_own = log(own_sum);
+        tl = double(lm) + ln_own / cd;
+        ln_q = (ln_q - double(lm)) * cd - ln_own;
     }
     const double ln_s = log(S);
     // (a probability of 0 adds nothing, NaN everything)
@@ -207,10 +207,11 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
         total = join[2][0] + join[2][1];
     }
     if (tid != 0) return;
+    // What backward starts from, as two numbers each: ln of a sum next to a huge logit is nothing even in 64 bits, so the lower one takes it by itself.
     const double lse = S == 0. ? -INFINITY : M + ln_s / cd;
     float4 v;
     v.x = float(lse);
-    v.y = S == 0. ? 0.f : float(lse - double(v.x));
+    v.y = S == 0. ? 0.f : float((M - double(v.x)) + ln_s / cd);
     if (TAIL) {
         double qr = 1. - own_sum;
         if (!(qr > kNoTail)) qr = 0.;
@@ -219,12 +220,12 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
             total += qr * (log(qr) - ln_pr);
         }
         // in backward the tail's p_j / p_r q_r is exp(c (z_j - t)); +inf: there is none, and the sum of the list's q in its place
-        const double t = qr > 0. && rest_s > 0. ? rest_m + (log(rest_s) - log(qr)) / cd : INFINITY;
+        const double ln_t = (log(rest_s) - log(qr)) / cd, t = qr > 0. && rest_s > 0. ? rest_m + ln_t : INFINITY;
         v.z = float(t);
-        v.w = qr > 0. ? (rest_s > 0. ? float(t - double(v.z)) : 1.f) : float(own_sum);
+        v.w = qr > 0. ? (rest_s > 0. ? float((rest_m - double(v.z)) + ln_t) : 1.f) : float(own_sum);
     } else {
         v.z = float(tl);
-        v.w = float(tl - double(v.z));
+        v.w = float((double(lm) - double(v.z)) + ln_own / cd);
     }
     if (S == 0.) total = own_sum == own_sum ? INFINITY : NAN;       // (nothing but -inf: whatever the teacher likes has p = 0)
     if (!teacher) total = 0., v = make_float4(-INFINITY, 0.f, 0.f, 0.f);

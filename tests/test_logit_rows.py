@@ -694,3 +694,49 @@ def test_reorder_that_would_write_its_own_parents():
     par.copy_(torch.tensor([2, 0, 1, 9, 9, 1, 1, 0], dtype=torch.int32))
     assert R([(p, p)], p - 32) == 0
     assert state.view(6, 16)[:, 0].tolist() == [2, 0, 1, 4, 4, 3] and par.tolist() == [2, 0, 1, 9, 9, 1, 1, 0]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("T,V,k,temperature,teacher,pad", [(1, 6, 64, 1.0, "short", 8), (5, 1000, 20, 2.0, "full", 0), (12, 4099, 1, 4.0, "full", 3), (9, 32000, 65, 1.0, "short", 0),
+                                                           (3, 70000, 128, 2.0, "full", 0)])
+def test_distill_of_rows_of_the_lowest_value(dtype, tail, T, V, k, temperature, teacher, pad):
+    """A row of nothing but a mask's lowest value, with a teacher: its tokens are equally likely, though ln of their number is lost next to the logits."""
+    test_distill(dtype, tail, T, V, k, temperature, "lowest", teacher, pad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("far", [1e6, -1e12, 3e38, -3e38])
+def test_distill_far_from_0(dtype, tail, far):
+    """Logits of one huge value with a few that are a little apart from it or far below it, and without a tail a teacher of huge values too."""
+    T, V, k = 4, 300, 5
+    g = torch.Generator().manual_seed(1)
+    z = torch.full((T, V), far)
+    z[0, ::7] += abs(far) * 2.0 ** -7                # (a step of bf16: far beyond what exp survives)
+    z[1, 1::2] = -math.inf
+    z[2, :200] = torch.finfo(torch.float32).min
+    z = torch.nan_to_num(z.to(DT[dtype]).float(), posinf=3.3e38, neginf=-math.inf).to(DT[dtype])
+    ids = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(T)]).int()
+    ids[1] = ids[1] // 2 * 2
+    ids[2] = 200 + ids[2] % 100
+    ids[0] = ids[0] // 7 * 7                         # (elsewhere p is 0 and the loss beyond fp32)
+    tl = torch.log_softmax(torch.randn(T, k + 2, generator=g), dim=1)[:, :k].contiguous()
+    if not tail:
+        tl[3] = far if abs(far) < 1e7 else -1e30
+    desc = bd.make_distill_desc(dtype, T, V, k, tail=tail)
+    loss, grad, _ = ref_distill(z, tl, ids, tail, 1.0)
+    if tail:
+        assert bool((loss[[1, 3]].abs() < 100).all())
+    zd, td, idd = z.to(DEV), tl.to(DEV), ids.to(DEV)
+    ld, st, dz = torch.empty(T, device=DEV), torch.empty(T, 4, device=DEV), torch.empty(T, V, dtype=DT[dtype], device=DEV)
+    bd.lobra_token_distill_fwd(desc, zd, td, idd, ld, st)
+    bd.lobra_token_distill_bwd(desc, zd, td, idd, st, torch.ones(T, device=DEV), dz)
+    got = ld.double().cpu()
+    fine = loss.abs() < 3.4e38
+    assert bool((((got - loss).abs() <= 4e-6 + 2.0 ** -20 * loss.abs()) | ~fine).all()) and bool((got[~fine] > 3.3e38).all()), (got, loss)
+    # (what a listed token stands for is rounded once, by 2^-24 of ln k or of the logit's distance, all else as in test_distill)
+    off = (dz.double().cpu() - grad).abs()
+    assert bool((off <= 2e-6 * 2 + (grad.abs() * 2.0 ** -8 if dtype == "bf16" else 0)).all()), (off.max(dim=1).values, got, loss)
