@@ -175,7 +175,7 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
         bool first = id >= 0;
         if (first && times_listed(ids, k, id) > 1)
             for (int32_t i = 0; i < tid; ++i) first = first && ids[i] != id;
-        if (first) ex = M == -INFINITY ? 0. : exp((double(zj) - M) * cd);
+        if (first) ex = zj == -INFINITY ? 0. : exp((double(zj) - M) * cd);        // (NaN, also where nothing else is left)
         own = id >= 0 ? exp(ln_q) : 0.;
     } else {
         own = id >= 0 ? exp((ln_q - double(lm)) * cd) : 0.;
@@ -228,6 +228,7 @@ void distill_fwd_kernel(const E* __restrict__ logits, int64_t ld, int32_t V, int
         v.w = float((double(lm) - double(v.z)) + ln_own / cd);
     }
     if (S == 0.) total = own_sum == own_sum ? INFINITY : NAN;       // (nothing but -inf: whatever the teacher likes has p = 0)
+    if (total != total) v.x = NAN;                   // (its gradient is NaN too, and not that of a row of nothing)
     if (!teacher) total = 0., v = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     if (loss) loss[r] = float(total);
     if (stat) stat[r] = v;

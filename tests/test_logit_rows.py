@@ -740,3 +740,12 @@ def test_distill_far_from_0(dtype, tail, far):
     # (what a listed token stands for is rounded once, by 2^-24 of ln k or of the logit's distance, all else as in test_distill)
     off = (dz.double().cpu() - grad).abs()
     assert bool((off <= 2e-6 * 2 + (grad.abs() * 2.0 ** -8 if dtype == "bf16" else 0)).all()), (off.max(dim=1).values, got, loss)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("T,V,k,kind,teacher", [(4, 1, 2, "nan", "full"), (2, 1, 127, "nan", "short"), (10, 3, 63, "masked", "odd"), (10, 1, 128, "masked", "odd"), (3, 2, 3, "nan", "full")])
+def test_distill_of_nothing_but_nan(dtype, tail, T, V, k, kind, teacher):
+    """NaN that the tail leaves out of the sums, next to nothing; a teacher of NaN over logits of nothing."""
+    test_distill(dtype, tail, T, V, k, 1.0, kind, teacher, 0)
