@@ -453,7 +453,7 @@ LOBRA_API lobra_status lobra_mlora_quant_bwd(const lobra_mlora_plan *plan, const
  *   dloss           : device fp32 [T].  A row in which it is 0 gets a gradient of 0, whatever its logits
  *   flags           : LOBRA_FLAG_ACCUMULATE_GRADS: added to dlogits (the gradient of another loss of the same logits), which is not logits then
  * (LOBRA_ERR_SHAPE if it is)
- * LOBRA_ERR_SHAPE for a temperature that is not positive and finite, or 1 / temperature not finite. */
+ * LOBRA_ERR_SHAPE for a temperature that is not positive and finite, or log2 e / temperature not finite. */
 enum { LOBRA_MAX_TEACHER = 128 };
 typedef struct {
     int32_t dtype;           /* lobra_dtype of logits and dlogits */

@@ -21,7 +21,7 @@ lobra_status distill_shape(const lobra_distill_desc* d, DistillShape* s)
     const int64_t ld = d->ld == 0 ? d->V : d->ld;
     if (d->V < 1 || d->V > LOBRA_MAX_VOCAB || d->T < 0 || d->T >= (int64_t(1) << 31) || ld < d->V || d->top_k < 1 || d->top_k > LOBRA_MAX_TEACHER)
         return LOBRA_ERR_SHAPE;
-    if ((d->tail != 0 && d->tail != 1) || !(d->temperature > 0.f) || !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature))
+    if ((d->tail != 0 && d->tail != 1) || !(d->temperature > 0.f) || !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature * 1.4426950408889634f))
         return LOBRA_ERR_SHAPE;
     if (d->T > 0 && ld >= (int64_t(1) << 60) / d->T) return LOBRA_ERR_SHAPE;
     *s = DistillShape{d->dtype, d->V, d->top_k, d->tail != 0, d->T, ld, d->temperature};

@@ -749,3 +749,13 @@ def test_distill_far_from_0(dtype, tail, far):
 def test_distill_of_nothing_but_nan(dtype, tail, T, V, k, kind, teacher):
     """NaN that the tail leaves out of the sums, next to nothing; a teacher of NaN over logits of nothing."""
     test_distill(dtype, tail, T, V, k, 1.0, kind, teacher, 0)
+
+
+def test_temperatures_whose_exponents_are_not_finite():
+    """1 / temperature is finite from 2.94e-39 on, log2 e / temperature, which the exponentials take, from 4.24e-39."""
+    L, p = bd.lib(), 4096
+    for t, want in ((2e-39, -2), (3e-39, -2), (4.2e-39, -2), (4.3e-39, 0), (1e-38, 0), (3e38, 0)):
+        d = bd.make_distill_desc("bf16", 3, 100, 5, temperature=t)
+        assert L.lobra_token_distill_fwd(ctypes.byref(d), p, p, p, None, None, None) == want, t           # (without outputs: nothing is launched)
+        if want:
+            assert L.lobra_token_distill_bwd(ctypes.byref(d), p, p, p, p, p, p, 0, None) == want, t
